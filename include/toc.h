@@ -637,6 +637,106 @@ toc_status toc_mlp_epoch(const toc_dev *dev, int64_t b0, int64_t n_batches, int3
                          float *W3, float *b3, const int32_t *labels, float lr, void *ws,
                          size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Rows of a network over tokens.  A mini-batch of one-hot or sparse-text tuples
+ * decodes to its column numbers (toc_decode_csr): n tokens, each with a row of d
+ * numbers.  These calls are what a network does to such rows before and after its
+ * matrix products: the lookup of the rows in a table (the right product of tuples
+ * that hold one pair each, Theorem 1) and the table's gradient (the left product,
+ * Theorem 2), dropout, and the root-mean-square norm with the residual's addition.
+ *
+ * Matrices of rows are caller-owned device memory, row-major with a stride of
+ * ld >= d elements, aligned to their elements only.  `type` is that of all of a
+ * call's matrices unless it says otherwise; w, dw and the scales are binary32.
+ * Everything is computed and summed in binary32 and rounded once, to nearest even,
+ * where an output is stored; the squares of |h| above about 1e19 overflow.  Sums run
+ * in an order that depends on the sizes alone, so equal calls give equal bits.
+ * Limits (TOC_EUNSUPPORTED): n and n_vocab below 2^31, d at most 16384 for the norm and
+ * 2^20 for the table's gradient.
+ * An output may be the very matrix (pointer, stride and type) of one of the call's
+ * inputs except G and E; outputs overlap nothing else.
+ * ------------------------------------------------------------------------- */
+#define TOC_F32 0
+#define TOC_BF16 1
+#define TOC_F16 2
+#define TOC_E4M3 3   /* 8 bits, OCP: 4 of exponent, 3 of mantissa, largest 448      */
+
+/* A dropout mask, never stored: element (i, j) of a matrix is dropped when its
+ * 16-bit word is below round(65536 p), else kept and multiplied by
+ * 65536 / (65536 - round(65536 p)).  The words of columns 8 q .. 8 q + 7 of row i are the
+ * output of Philox4x32-10 for the counter (q, i, mask low, mask high) and the key (seed
+ * low, seed high), low half of the first word first.  So the mask depends on the
+ * element's row and column alone, and a gradient called with the same toc_drop sees
+ * the mask of the forward pass.  Use another `mask` for each layer and step.
+ * p in [0, 1]; a dropped element is 0 whatever it was, and p = 1 drops all. */
+typedef struct {
+  float p;
+  uint32_t reserved;
+  uint64_t seed, mask;
+} toc_drop;
+
+/* Embedding lookup: out[t, :] = drop(scale * E[ids[t], :]) for t < n.
+ *   ids   device, n integers of id_bits (32 or 64) signed bits; one outside
+ *         0 .. n_vocab-1 (say -1, to pad) gives a row of zeros
+ *   E     n_vocab x d    out   n x d    drop  host, or NULL
+ * Asynchronous on stream.  TOC_EINVAL for NULL or misaligned pointers, strides
+ * below d, unknown types or widths, a scale that is not finite, p outside 0..1. */
+toc_status toc_embed(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab, int32_t d,
+                     int32_t type, const void *E, int64_t lde, float scale, const toc_drop *drop,
+                     void *out, int64_t ldo, void *stream);
+
+/* Workspace bytes of toc_embed_grad for n tokens. */
+toc_status toc_embed_grad_workspace_size(int64_t n, int64_t n_vocab, int32_t d, size_t *bytes);
+
+/* The lookup's gradient for the table: dE[v, :] = scale * sum of drop(G)[t, :] over the
+ * tokens t with ids[t] = v, all n_vocab rows of it (zeros where v does not occur).
+ * accumulate != 0 adds to the rows of the numbers that occur and leaves the others
+ * alone: with dE = E and scale times -lr that is the table's step of mini-batch
+ * gradient descent.
+ *   G  n x d of `type`: the gradient of out    dE  n_vocab x d of de_type: type or TOC_F32
+ *   ws device, toc_embed_grad_workspace_size bytes, 16-byte aligned, scratch
+ * Errors as toc_embed; TOC_ESIZE for a small workspace. */
+toc_status toc_embed_grad(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab, int32_t d,
+                          int32_t type, const void *G, int64_t ldg, float scale, const toc_drop *drop,
+                          int32_t de_type, void *dE, int64_t lde, int32_t accumulate, void *ws,
+                          size_t ws_bytes, void *stream);
+
+/* Y = drop(X), n x d; its gradient is the same call on the gradient of Y. */
+toc_status toc_dropout(int64_t n, int32_t d, int32_t type, const void *X, int64_t ldx,
+                       const toc_drop *drop, void *Y, int64_t ldy, void *stream);
+
+/* Root-mean-square norm with the residual's addition, row by row:
+ *   h = R + drop(X)    y = w * h / sqrt(mean(h^2) + eps)
+ *   R     NULL: no residual    drop  NULL: none    w  device, d, or NULL: ones
+ *   H     receives h, or NULL
+ *   Y     n x d of y_type: `type`, or TOC_E4M3: then y_scale[i] = max(max_j |y_ij|, 2^-100)
+ *         / 448 and Y holds y / y_scale rounded to e4m3 (a row with a NaN or an infinity
+ *         has scale NaN or infinity); y_scale: device, n
+ *   eps   positive and finite
+ * Errors as toc_embed. */
+toc_status toc_rmsnorm(int64_t n, int32_t d, int32_t type, const void *X, int64_t ldx, const void *R,
+                       int64_t ldr, const toc_drop *drop, const float *w, float eps, void *H,
+                       int64_t ldh, int32_t y_type, void *Y, int64_t ldy, float *y_scale,
+                       void *stream);
+
+/* Workspace bytes of toc_rmsnorm_grad (with dw) for n rows of d columns. */
+toc_status toc_rmsnorm_grad_workspace_size(int64_t n, int32_t d, size_t *bytes);
+
+/* Gradients of toc_rmsnorm from its h and the gradient dY of y.  With
+ * r = 1 / sqrt(mean(h^2) + eps) and g = dY * w of a row:
+ *   dH = r g - h r^3 mean(g h) + dR    the gradient of h, so of R (dR: the gradient that
+ *                                      reaches h on other ways, or NULL)
+ *   dX = drop(dH)                      the gradient of X
+ *   dw[j] (+)= sum over rows of dY_j h_j r    (added to dw if accumulate != 0)
+ * dH, dX and dw: outputs, each may be NULL.  ws: device, 4-byte aligned,
+ * toc_rmsnorm_grad_workspace_size bytes (with dw NULL: not read).  Errors as toc_rmsnorm;
+ * TOC_ESIZE for a small workspace. */
+toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, int64_t ldh,
+                            const float *w, float eps, const void *dY, int64_t lddy, const void *dR,
+                            int64_t lddr, const toc_drop *drop, void *dH, int64_t lddh, void *dX,
+                            int64_t lddx, float *dw, int32_t accumulate, void *ws, size_t ws_bytes,
+                            void *stream);
+
 /* Message for the last non-OK status returned on this thread. */
 const char *toc_last_error(void);
 

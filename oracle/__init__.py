@@ -55,7 +55,21 @@ Parity status of each function (what pins it, see ``tests/test_oracle.py``):
                  every parameter (softmax and single-sigmoid outputs), the first
                  layer's gradient equal to Theorem 2's left product on (I, D)
                  (toc_left), the closed form at zero weights, lr = 0, an empty batch
+  rows.philox4x32, rows.kept, rows.dropout
+                 pinned (tests/test_rows_oracle.py): the generator's published
+                 known answers, the share kept, p = 0 and p = 1
+  rows.embed, rows.embed_grad
+                 pinned: toc dense_right and dense_left of the one-pair tuples,
+                 duality <G, embed(E)> = <embed_grad(G), E> with dropout
+  rows.rmsnorm, rows.rmsnorm_grad
+                 pinned: unit rows in closed form, central finite differences of
+                 every gradient
+  rows.e4m3_values
+                 pinned: the format's largest, smallest normal and smallest
+                 numbers, symmetry, increasing order
 """
+
+from . import rows_oracle as rows  # noqa: F401
 
 from .toc_oracle import (  # noqa: F401
     TocInputError,

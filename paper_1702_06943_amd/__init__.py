@@ -5,7 +5,9 @@ physical encoding and build the decoding tree C' and the whole upload image from
 it on the GPU; run
 mini-batch gradient descent steps of linear models and of a feed-forward neural
 network on the compressed batches;
-encode many mini-batches at once on the GPU.
+encode many mini-batches at once on the GPU.  For networks over the tokens of decoded
+mini-batches: embedding lookup and its gradient, dropout, and the residual
+root-mean-square norm and its gradient.
 
 The functions are those of include/toc.h, called through ctypes; see binding.py.
 """
@@ -30,5 +32,8 @@ from .binding import (  # noqa: F401
     TOC_ENCDEV_ROWPTR, TOC_ENCDEV_SIZE, TOC_ENCDEV_COLUMN, TOC_ENCDEV_VALUE,
     toc_encode_device_workspace_size, toc_encode_device,
     toc_mlp_workspace_size, toc_mlp_epoch,
+    TOC_F32, TOC_BF16, TOC_F16, TOC_E4M3, Drop,
+    toc_embed, toc_embed_grad_workspace_size, toc_embed_grad, toc_dropout,
+    toc_rmsnorm, toc_rmsnorm_grad_workspace_size, toc_rmsnorm_grad,
     TOC_INGEST_CHANGED, toc_ingest_workspace_size, toc_ingest_plan, toc_ingest_build,
 )

@@ -32,6 +32,7 @@ TOC_ENCDEV_ROWPTR, TOC_ENCDEV_SIZE, TOC_ENCDEV_COLUMN, TOC_ENCDEV_VALUE = range(
 TOC_CPRIME_COLUMN = 10
 TOC_INGEST_CHANGED = 11
 TOC_NOALLOC_SCRATCH_BYTES = 64 << 20
+TOC_F32, TOC_BF16, TOC_F16, TOC_E4M3 = range(4)
 STATUS_NAMES = {0: "TOC_OK", 1: "TOC_EINVAL", 2: "TOC_ENOMEM", 3: "TOC_ESIZE",
                 4: "TOC_EDEVICE", 5: "TOC_EUNSUPPORTED"}
 
@@ -60,6 +61,16 @@ class DevInfo(C.Structure):
 class PhysInfo(C.Structure):
     _fields_ = [(n, C.c_int64) for n in
                 ("n_rows", "n_first", "n_codes", "n_unique", "n_nodes", "max_col")]
+
+
+class Drop(C.Structure):
+    """A dropout mask (toc_drop): Drop(p, seed, mask).  seed and mask are taken modulo
+    2**64; the same three give the same mask."""
+    _fields_ = [("p", C.c_float), ("reserved", C.c_uint32), ("seed", C.c_uint64),
+                ("mask", C.c_uint64)]
+
+    def __init__(self, p, seed, mask=0):
+        super().__init__(p, 0, seed, mask)
 
 
 class Layout(C.Structure):
@@ -133,6 +144,15 @@ def lib():
         "toc_ingest_workspace_size": [P, I64, I32, P, P],
         "toc_ingest_plan": [P, P, P, I64, I32, P, SZ, P, P, P],
         "toc_ingest_build": [P, P, P, P, SZ, P, SZ, P],
+        "toc_embed": [I64, P, I32, I64, I32, I32, P, I64, C.c_float, P, P, I64, P],
+        "toc_embed_grad_workspace_size": [I64, I64, I32, P],
+        "toc_embed_grad": [I64, P, I32, I64, I32, I32, P, I64, C.c_float, P, I32, P, I64, I32,
+                           P, SZ, P],
+        "toc_dropout": [I64, I32, I32, P, I64, P, P, I64, P],
+        "toc_rmsnorm": [I64, I32, I32, P, I64, P, I64, P, P, C.c_float, P, I64, I32, P, I64, P, P],
+        "toc_rmsnorm_grad_workspace_size": [I64, I32, P],
+        "toc_rmsnorm_grad": [I64, I32, I32, P, I64, P, C.c_float, P, I64, P, I64, P, P, I64, P,
+                             I64, P, I32, P, SZ, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -622,3 +642,168 @@ def toc_level_right_mul(blobs, blob_off, node_off, d_off, row_off, max_levels, m
                                      _ptr(l_parent), _ptr(l_col), _ptr(l_val), _ptr(l_D), _ptr(w),
                                      _ptr(r), _ptr(status), _ptr(ws),
                                      ws.numel() * ws.element_size(), _stream(stream)))
+
+
+# --- rows of a network over tokens ---------------------------------------------
+
+_ROW_TYPES = {}
+
+
+def _row_types():
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.float32: TOC_F32, torch.bfloat16: TOC_BF16,
+                           torch.float16: TOC_F16, torch.float8_e4m3fn: TOC_E4M3})
+    return _ROW_TYPES
+
+
+def _here(t, name):
+    import torch
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise TocError(TOC_EINVAL, f"{name} must be on the current CUDA device")
+
+
+def _row_mat(t, name, n, d, *types):
+    """(pointer, row stride, type) of an n x d tensor of rows with unit column stride."""
+    _here(t, name)
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != d:
+        raise TocError(TOC_EINVAL, f"{name} must be {n} x {d}, not {tuple(t.shape)}")
+    kind = _row_types().get(t.dtype)
+    if kind not in types:
+        raise TocError(TOC_EINVAL, f"{name} has type {t.dtype}")
+    ld, cs = t.stride()
+    if cs != 1 and d > 1:
+        raise TocError(TOC_EINVAL, f"{name} must have unit column stride")
+    if n > 1 and ld < d:
+        raise TocError(TOC_EINVAL, f"{name}'s rows overlap")
+    return _ptr(t), max(ld, d), kind
+
+
+def _row_opt(t, name, n, d, kind):
+    return (None, d) if t is None else _row_mat(t, name, n, d, kind)[:2]
+
+
+def _row_vec(t, name, n):
+    """Pointer of a contiguous float32 vector of n entries (None -> NULL)."""
+    if t is None:
+        return None
+    import torch
+    _here(t, name)
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise TocError(TOC_EINVAL, f"{name} must be a contiguous float32 vector of {n}")
+    return _ptr(t)
+
+
+def _row_ws(t):
+    if t is None:
+        return None, 0
+    _here(t, "ws")
+    if not t.is_contiguous():
+        raise TocError(TOC_EINVAL, "ws must be contiguous")
+    return _ptr(t), t.numel() * t.element_size()
+
+
+def _row_ids(t):
+    import torch
+    _here(t, "ids")
+    if t.dtype not in (torch.int32, torch.int64) or t.dim() != 1 or not t.is_contiguous():
+        raise TocError(TOC_EINVAL, "ids must be a contiguous vector of int32 or int64")
+    return t.shape[0], _ptr(t), 32 if t.dtype == torch.int32 else 64
+
+
+def _row_drop(drop):
+    if drop is None:
+        return None
+    if not isinstance(drop, Drop):
+        raise TocError(TOC_EINVAL, "drop must be a Drop")
+    return C.addressof(drop)
+
+
+_ROWS = (TOC_F32, TOC_BF16, TOC_F16)
+
+
+def toc_embed(ids, E, out, scale=1.0, drop=None, stream=None):
+    """out[t, :] = drop(scale * E[ids[t], :]).  ids: device int32 or int64 vector; E:
+    n_vocab x d and out: n x d device tensors of one type (float32, bfloat16, float16); an
+    id outside 0 .. n_vocab-1 gives a row of zeros; drop: a Drop, or None."""
+    n, ip, bits = _row_ids(ids)
+    if E.dim() != 2:
+        raise TocError(TOC_EINVAL, "E must be a matrix")
+    v, d = E.shape
+    ep, lde, kind = _row_mat(E, "E", v, d, *_ROWS)
+    op_, ldo, _ = _row_mat(out, "out", n, d, kind)
+    _check(lib().toc_embed(n, ip, bits, v, d, kind, ep, lde, scale, _row_drop(drop), op_, ldo,
+                           _stream(stream)))
+
+
+def toc_embed_grad_workspace_size(n, n_vocab, d):
+    b = C.c_size_t()
+    _check(lib().toc_embed_grad_workspace_size(int(n), int(n_vocab), int(d), C.byref(b)))
+    return b.value
+
+
+def toc_embed_grad(ids, G, dE, ws, scale=1.0, drop=None, accumulate=False, stream=None):
+    """dE[v, :] = scale * sum of drop(G)[t, :] over ids[t] = v, or added to the rows of the
+    ids that occur with accumulate.  G: n x d; dE: n_vocab x d of G's type or float32; ws:
+    device tensor of toc_embed_grad_workspace_size bytes."""
+    n, ip, bits = _row_ids(ids)
+    if dE.dim() != 2:
+        raise TocError(TOC_EINVAL, "dE must be a matrix")
+    v, d = dE.shape
+    gp, ldg, kind = _row_mat(G, "G", n, d, *_ROWS)
+    ep, lde, ekind = _row_mat(dE, "dE", v, d, kind, TOC_F32)
+    wp, wn = _row_ws(ws)
+    _check(lib().toc_embed_grad(n, ip, bits, v, d, kind, gp, ldg, scale, _row_drop(drop), ekind,
+                                ep, lde, 1 if accumulate else 0, wp, wn, _stream(stream)))
+
+
+def toc_dropout(X, Y, drop, stream=None):
+    """Y = drop(X): n x d device tensors of one type; Y may be X."""
+    if X.dim() != 2:
+        raise TocError(TOC_EINVAL, "X must be a matrix")
+    n, d = X.shape
+    xp, ldx, kind = _row_mat(X, "X", n, d, *_ROWS)
+    yp, ldy, _ = _row_mat(Y, "Y", n, d, kind)
+    _check(lib().toc_dropout(n, d, kind, xp, ldx, _row_drop(drop), yp, ldy, _stream(stream)))
+
+
+def toc_rmsnorm(X, Y, R=None, H=None, w=None, eps=1e-5, drop=None, y_scale=None, stream=None):
+    """h = R + drop(X); Y = w * h / sqrt(mean(h^2) + eps) row by row.  X, R, H (receives h):
+    n x d device tensors of one type; w: device float32 vector of d, or None for ones; Y:
+    n x d of that type, or float8_e4m3fn with y_scale a device float32 vector of n."""
+    if X.dim() != 2:
+        raise TocError(TOC_EINVAL, "X must be a matrix")
+    n, d = X.shape
+    xp, ldx, kind = _row_mat(X, "X", n, d, *_ROWS)
+    rp, ldr = _row_opt(R, "R", n, d, kind)
+    hp, ldh = _row_opt(H, "H", n, d, kind)
+    yp, ldy, ykind = _row_mat(Y, "Y", n, d, kind, TOC_E4M3)
+    _check(lib().toc_rmsnorm(n, d, kind, xp, ldx, rp, ldr, _row_drop(drop), _row_vec(w, "w", d),
+                             eps, hp, ldh, ykind, yp, ldy, _row_vec(y_scale, "y_scale", n),
+                             _stream(stream)))
+
+
+def toc_rmsnorm_grad_workspace_size(n, d):
+    b = C.c_size_t()
+    _check(lib().toc_rmsnorm_grad_workspace_size(int(n), int(d), C.byref(b)))
+    return b.value
+
+
+def toc_rmsnorm_grad(H, dY, dH, ws, w=None, eps=1e-5, dR=None, dX=None, dw=None,
+                     accumulate=False, drop=None, stream=None):
+    """Gradients of toc_rmsnorm from its h (H) and the gradient dY of its output: dH of h
+    (with dR, the gradient that reaches h otherwise, added), dX = drop(dH) of X, dw of w
+    (added to with accumulate).  dH, dX, dw: outputs or None; ws: device tensor of
+    toc_rmsnorm_grad_workspace_size bytes, None without dw."""
+    if H.dim() != 2:
+        raise TocError(TOC_EINVAL, "H must be a matrix")
+    n, d = H.shape
+    hp, ldh, kind = _row_mat(H, "H", n, d, *_ROWS)
+    gp, ldg, _ = _row_mat(dY, "dY", n, d, kind)
+    rp, ldr = _row_opt(dR, "dR", n, d, kind)
+    dhp, lddh = _row_opt(dH, "dH", n, d, kind)
+    dxp, lddx = _row_opt(dX, "dX", n, d, kind)
+    wp, wn = _row_ws(ws)
+    _check(lib().toc_rmsnorm_grad(n, d, kind, hp, ldh, _row_vec(w, "w", d), eps, gp, ldg, rp, ldr,
+                                  _row_drop(drop), dhp, lddh, dxp, lddx, _row_vec(dw, "dw", d),
+                                  1 if accumulate else 0, wp, wn, _stream(stream)))

@@ -1,0 +1,464 @@
+// Root-mean-square norm of rows with the residual's addition, and its gradient.
+//   h = R + drop(X)       r = 1 / sqrt(mean_j h_j^2 + eps)       y_j = h_j r w_j
+// for a row of d columns; 8-bit output: s = max(max_j |y_j|, 2^-100) / 448 and y_j / s as
+// e4m3 numbers.  With g_j = dy_j w_j the gradients are
+//   dh_j = r g_j - h_j r^3 mean_i(g_i h_i) + dR_j     dX = drop(dh)     dw_j = sum over rows dy_j h_j r
+// A row stays in registers between its one read and its one write, as octets of a group of
+// lanes of one wave, or of the lanes of a workgroup; groups walk over the rows, so that w
+// (and, on the way back, the group's part of dw) is read once and kept.  Sums are binary32:
+// a lane's octets in order, then the lanes in a tree.  Bound by memory.
+#include "toc_rows_dev.h"
+
+namespace toc {
+namespace rows {
+namespace {
+
+constexpr float kE4m3Max = 448.0f;
+constexpr float kLeastMax = 0x1p-100f;   // keeps 448 / max finite; a row of zeros gets a scale too
+
+// The larger of a and b; NaN if either is, as the scale of a row that holds one has to be.
+__device__ inline float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+
+// Sum over a group of kLanes lanes (kLanes <= 64: of one wave; else the whole workgroup, by
+// way of lds, kLanes / 64 entries each of two used in turn), in every lane.
+template <int kLanes>
+__device__ inline float group_sum(float x, float *lds) {
+#pragma unroll
+  for (int o = (kLanes < 64 ? kLanes : 64) / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  if (kLanes > 64) {
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kLanes / 64; ++i) x += lds[i];
+  }
+  return x;
+}
+template <int kLanes>
+__device__ inline float group_max(float x, float *lds) {
+#pragma unroll
+  for (int o = (kLanes < 64 ? kLanes : 64) / 2; o > 0; o >>= 1) x = max_nan(x, __shfl_xor(x, o, 64));
+  if (kLanes > 64) {
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int i = 1; i < kLanes / 64; ++i) x = max_nan(x, lds[i]);
+  }
+  return x;
+}
+
+__device__ inline float inv_rms(float sum, float inv_d, float eps) {
+  return 1.0f / sqrtf(fmaf(sum, inv_d, eps));
+}
+
+template <typename T>
+struct NormArgs {
+  uint32_t n;
+  int d;
+  const T *X;
+  int64_t ldx;
+  const T *R;          // or NULL
+  int64_t ldr;
+  Mask m;
+  const float *w;      // or NULL: ones
+  float eps, inv_d;
+  T *H;                // or NULL
+  int64_t ldh;
+  int64_t ldy;
+  float *y_scale;
+};
+
+template <int kOct>
+__device__ inline void load_w(const float *w, int d, int lane, int lanes, float (&v)[kOct][8]) {
+#pragma unroll
+  for (int k = 0; k < kOct; ++k) {
+    const int c = 8 * (lane + k * lanes);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[k][i] = c + i < d ? 1.0f : 0.0f;
+    if (w && c < d) load8(w + c, d - c, v[k]);
+  }
+}
+
+// kLanes lanes to a row, kOct octets to a lane (8 kLanes kOct >= d).
+template <typename T, typename Y, int kLanes, int kOct, bool kDrop>
+__global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormArgs<T> a, Y *Yp) {
+  constexpr int kBlock = kLanes > 256 ? kLanes : 256;
+  constexpr int kGroups = kBlock / kLanes;
+  constexpr bool k8 = std::is_same<Y, E4m3>::value;
+  __shared__ float part[2][kLanes > 64 ? kLanes / 64 : 1];
+  const int lane = threadIdx.x % kLanes;
+  float w[kOct][8];
+  load_w<kOct>(a.w, a.d, lane, kLanes, w);
+  // (kLanes >= 64: all lanes of a wave, so all waves of a workgroup, share a row)
+  for (uint32_t row = blockIdx.x * kGroups + threadIdx.x / kLanes; row < a.n; row += gridDim.x * kGroups) {
+    float h[kOct][8];
+    float sum = 0.0f, most = 0.0f;
+    const T *x = a.X + (int64_t)row * a.ldx, *res = a.R + (int64_t)row * a.ldr;
+    Octet<T> in[kOct], rin[kOct];
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+      const int c = 8 * (lane + k * kLanes);
+      in[k] = fetch8(x + c, a.d - c);
+    }
+    if (a.R) {
+#pragma unroll
+      for (int k = 0; k < kOct; ++k) {
+        const int c = 8 * (lane + k * kLanes);
+        rin[k] = fetch8(res + c, a.d - c);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) widen(in[k], h[k]);
+    if (kDrop) {
+#pragma unroll
+      for (int k = 0; k < kOct; ++k) drop8(h[k], (uint32_t)(lane + k * kLanes), row, a.m);
+    }
+    if (a.R) {
+#pragma unroll
+      for (int k = 0; k < kOct; ++k) {
+        float v[8];
+        widen(rin[k], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] += v[i];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(h[k][i], h[k][i], sum);
+      if (k8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max_nan(fabsf(h[k][i] * w[k][i]), most);
+      }
+    }
+    // (the row before may still be reading the other reduction's words, never these: a
+    // barrier of that other reduction, or of this one, lies between)
+    sum = group_sum<kLanes>(sum, part[0]);
+    const float r = inv_rms(sum, a.inv_d, a.eps);
+    float s = 1.0f;
+    if (k8) {
+      most = group_max<kLanes>(most, part[1]) * r;
+      most = most < kLeastMax ? kLeastMax : most;
+      s = kE4m3Max / most;
+      if (lane == 0) a.y_scale[row] = most / kE4m3Max;
+    } else if (kLanes > 64) {
+      __syncthreads();   // part[0] is free again
+    }
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+      const int c = 8 * (lane + k * kLanes);
+      if (c >= a.d) continue;
+      if (a.H) store8(a.H + (int64_t)row * a.ldh + c, a.d - c, h[k]);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i] = h[k][i] * r * w[k][i];
+        if (k8) {
+          y[i] *= s;
+          // rounding may leave the largest just above 448; NaN stays
+          y[i] = y[i] > kE4m3Max ? kE4m3Max : y[i] < -kE4m3Max ? -kE4m3Max : y[i];
+        }
+      }
+      store8(Yp + (int64_t)row * a.ldy + c, a.d - c, y);
+    }
+  }
+}
+
+template <typename T>
+struct GradArgs {
+  uint32_t n;
+  int d;
+  const T *H;
+  int64_t ldh;
+  const float *w;      // or NULL: ones
+  float eps, inv_d;
+  const T *dY;
+  int64_t lddy;
+  const T *dR;         // or NULL
+  int64_t lddr;
+  Mask m;
+  T *dH;               // or NULL
+  int64_t lddh;
+  T *dX;               // or NULL
+  int64_t lddx;
+  float *part;         // NULL, or one row of d per group: its part of dw
+};
+
+template <typename T, int kLanes, int kOct, bool kDrop>
+__global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(GradArgs<T> a) {
+  constexpr int kBlock = kLanes > 256 ? kLanes : 256;
+  constexpr int kGroups = kBlock / kLanes;
+  __shared__ float part[2][kLanes > 64 ? kLanes / 64 : 1];
+  const int lane = threadIdx.x % kLanes;
+  const uint32_t group = blockIdx.x * kGroups + threadIdx.x / kLanes;
+  float w[kOct][8], dw[kOct][8];
+  load_w<kOct>(a.w, a.d, lane, kLanes, w);
+#pragma unroll
+  for (int k = 0; k < kOct; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[k][i] = 0.0f;
+  for (uint32_t row = group; row < a.n; row += gridDim.x * kGroups) {
+    float h[kOct][8], g[kOct][8];
+    float hh = 0.0f, gh = 0.0f;
+    Octet<T> hin[kOct], gin[kOct], rin[kOct];
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+      const int c = 8 * (lane + k * kLanes);
+      hin[k] = fetch8(a.H + (int64_t)row * a.ldh + c, a.d - c);
+      gin[k] = fetch8(a.dY + (int64_t)row * a.lddy + c, a.d - c);
+    }
+    if (a.dR) {
+#pragma unroll
+      for (int k = 0; k < kOct; ++k) {
+        const int c = 8 * (lane + k * kLanes);
+        rin[k] = fetch8(a.dR + (int64_t)row * a.lddr + c, a.d - c);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+      widen(hin[k], h[k]);
+      widen(gin[k], g[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kOct; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        hh = fmaf(h[k][i], h[k][i], hh);
+        gh = fmaf(g[k][i] * w[k][i], h[k][i], gh);
+      }
+    hh = group_sum<kLanes>(hh, part[0]);
+    gh = group_sum<kLanes>(gh, part[1]);
+    const float r = inv_rms(hh, a.inv_d, a.eps);
+    const float c3 = r * r * r * (gh * a.inv_d);
+#pragma unroll
+    for (int k = 0; k < kOct; ++k) {
+      const int c = 8 * (lane + k * kLanes);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        dw[k][i] = fmaf(g[k][i] * r, h[k][i], dw[k][i]);
+        h[k][i] = fmaf(g[k][i] * w[k][i], r, -h[k][i] * c3);
+      }
+      if (c >= a.d) continue;
+      if (a.dR) {
+        float v[8];
+        widen(rin[k], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] += v[i];
+      }
+      if (a.dH) store8(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k]);
+      if (a.dX) {
+        if (kDrop) drop8(h[k], (uint32_t)(c / 8), row, a.m);
+        store8(a.dX + (int64_t)row * a.lddx + c, a.d - c, h[k]);
+      }
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int k = 0; k < kOct; ++k) {
+    const int c = 8 * (lane + k * kLanes);
+    if (c < a.d) store8(a.part + (int64_t)group * a.d + c, a.d - c, dw[k]);
+  }
+}
+
+// dw (+)= the groups' parts, in the groups' order.
+constexpr int kJoinCols = 32, kJoinParts = 8;
+__global__ __launch_bounds__(kJoinCols * kJoinParts) void norm_join_kernel(
+    const float *__restrict__ part, int groups, int d, int accumulate, float *__restrict__ dw) {
+  __shared__ float sums[kJoinParts][kJoinCols];
+  const int c = blockIdx.x * kJoinCols + threadIdx.x % kJoinCols, p = threadIdx.x / kJoinCols;
+  const int per = (groups + kJoinParts - 1) / kJoinParts;
+  float s = 0.0f;
+  if (c < d) {
+    const int end = min(groups, (p + 1) * per);
+#pragma unroll 8
+    for (int g = p * per; g < end; ++g) s += part[(int64_t)g * d + c];
+  }
+  sums[p][threadIdx.x % kJoinCols] = s;
+  __syncthreads();
+  if (p != 0 || c >= d) return;
+#pragma unroll
+  for (int q = 1; q < kJoinParts; ++q) s += sums[q][threadIdx.x % kJoinCols];
+  dw[c] = accumulate ? dw[c] + s : s;
+}
+
+// Lanes to a row and octets to a lane: the fewest that hold the row.
+struct Shape {
+  int lanes, oct;
+};
+constexpr int32_t kMaxCols = 16384;
+Shape shape_of(int32_t d) {
+  const int octets = (d + 7) / 8;
+  if (octets <= 8) return {8, 1};
+  if (octets <= 32) return {32, 1};
+  if (octets <= 64) return {64, 1};
+  if (octets <= 128) return {64, 2};
+  if (octets <= 256) return {256, 1};
+  if (octets <= 512) return {256, 2};
+  if (octets <= 1024) return {1024, 1};
+  return {1024, 2};
+}
+
+// Workgroups of a launch: as many as the rows need, at most what fills the chip.
+int64_t blocks_for(int64_t n, Shape sh, int64_t most) {
+  const int64_t groups = sh.lanes > 256 ? 1 : 256 / sh.lanes;
+  return std::max<int64_t>(1, std::min((n + groups - 1) / groups, sh.lanes > 256 ? most / 4 : most));
+}
+constexpr int64_t kNormBlocks = 4096, kGradBlocks = 1024;
+
+#define TOC_SHAPES(F)                                                                     \
+  F(8, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(1024, 1) F(1024, 2)
+
+template <typename T, typename Y>
+toc_status norm(const NormArgs<T> &a, Y *y, hipStream_t s) {
+  const Shape sh = shape_of(a.d);
+  const dim3 grid((unsigned)blocks_for(a.n, sh, kNormBlocks)), block((unsigned)std::max(sh.lanes, 256));
+#define TOC_NORM(L, K)                                                                     \
+  if (sh.lanes == L && sh.oct == K) {                                                      \
+    if (a.m.thr)                                                                           \
+      hipLaunchKernelGGL((norm_kernel<T, Y, L, K, true>), grid, block, 0, s, a, y);        \
+    else                                                                                   \
+      hipLaunchKernelGGL((norm_kernel<T, Y, L, K, false>), grid, block, 0, s, a, y);       \
+  }
+  TOC_SHAPES(TOC_NORM)
+#undef TOC_NORM
+  return launched("norm_kernel");
+}
+
+template <typename T>
+toc_status norm_grad(const GradArgs<T> &a, hipStream_t s) {
+  const Shape sh = shape_of(a.d);
+  const dim3 grid((unsigned)blocks_for(a.n, sh, kGradBlocks)), block((unsigned)std::max(sh.lanes, 256));
+#define TOC_GRAD(L, K)                                                                     \
+  if (sh.lanes == L && sh.oct == K) {                                                      \
+    if (a.m.thr)                                                                           \
+      hipLaunchKernelGGL((norm_grad_kernel<T, L, K, true>), grid, block, 0, s, a);         \
+    else                                                                                   \
+      hipLaunchKernelGGL((norm_grad_kernel<T, L, K, false>), grid, block, 0, s, a);        \
+  }
+  TOC_SHAPES(TOC_GRAD)
+#undef TOC_GRAD
+  return launched("norm_grad_kernel");
+}
+
+// Rows of partial dw sums a call leaves in its workspace.
+int64_t grad_groups(int64_t n, int32_t d) {
+  const Shape sh = shape_of(d);
+  return n ? blocks_for(n, sh, kGradBlocks) * (sh.lanes > 256 ? 1 : 256 / sh.lanes) : 0;
+}
+
+template <typename T>
+toc_status norm_typed(int64_t n, int32_t d, const void *X, int64_t ldx, const void *R, int64_t ldr,
+                      const toc_drop *drop, const float *w, float eps, void *H, int64_t ldh, void *Y,
+                      int64_t ldy, bool eight, float *y_scale, void *stream) {
+  const NormArgs<T> a{(uint32_t)n, d, (const T *)X, ldx, (const T *)R, ldr, mask_of(drop), w, eps,
+                      1.0f / (float)d, (T *)H, ldh, ldy, y_scale};
+  if (eight) return norm(a, (E4m3 *)Y, (hipStream_t)stream);
+  return norm(a, (T *)Y, (hipStream_t)stream);
+}
+
+template <typename T>
+toc_status grad_typed(int64_t n, int32_t d, const void *H, int64_t ldh, const float *w, float eps,
+                      const void *dY, int64_t lddy, const void *dR, int64_t lddr, const toc_drop *drop,
+                      void *dH, int64_t lddh, void *dX, int64_t lddx, float *part, void *stream) {
+  const GradArgs<T> a{(uint32_t)n, d, (const T *)H, ldh, w, eps, 1.0f / (float)d, (const T *)dY, lddy,
+                      (const T *)dR, lddr, mask_of(drop), (T *)dH, lddh, (T *)dX, lddx, part};
+  return norm_grad(a, (hipStream_t)stream);
+}
+
+toc_status check_norm(int64_t n, int32_t d, int32_t type, const float *w, float eps) {
+  if (const toc_status st = check_sizes(n, d, type)) return st;
+  if (d > kMaxCols) return fail(TOC_EUNSUPPORTED, "rows of more than %d columns", kMaxCols);
+  if (!(eps > 0.0f) || !std::isfinite(eps)) return fail(TOC_EINVAL, "eps must be positive and finite");
+  if ((uintptr_t)w % 4) return fail(TOC_EINVAL, "w is not aligned to its elements");
+  return TOC_OK;
+}
+
+}  // namespace
+}  // namespace rows
+}  // namespace toc
+
+using namespace toc;
+using namespace toc::rows;
+
+extern "C" {
+
+toc_status toc_rmsnorm(int64_t n, int32_t d, int32_t type, const void *X, int64_t ldx, const void *R,
+                       int64_t ldr, const toc_drop *drop, const float *w, float eps, void *H,
+                       int64_t ldh, int32_t y_type, void *Y, int64_t ldy, float *y_scale,
+                       void *stream) {
+  clear_error();
+  toc_status st;
+  if ((st = check_norm(n, d, type, w, eps)) || (st = check_drop(drop))) return st;
+  if (y_type != type && y_type != TOC_E4M3)
+    return fail(TOC_EINVAL, "the output's type is the input's or TOC_E4M3, not %d", y_type);
+  const bool eight = y_type == TOC_E4M3;
+  const int size = type_size(type);
+  if ((st = check_rows("X", X, n, d, ldx, size)) || (R && (st = check_rows("R", R, n, d, ldr, size))) ||
+      (H && (st = check_rows("H", H, n, d, ldh, size))) ||
+      (st = check_rows("Y", Y, n, d, ldy, eight ? 1 : size)))
+    return st;
+  if (eight && n > 0 && !y_scale) return fail(TOC_EINVAL, "y_scale is NULL");
+  if ((uintptr_t)y_scale % 4) return fail(TOC_EINVAL, "y_scale is not aligned to its elements");
+  if (n == 0) return TOC_OK;
+  switch (type) {
+    case TOC_F32:
+      return norm_typed<float>(n, d, X, ldx, R, ldr, drop, w, eps, H, ldh, Y, ldy, eight, y_scale, stream);
+    case TOC_BF16:
+      return norm_typed<bf16>(n, d, X, ldx, R, ldr, drop, w, eps, H, ldh, Y, ldy, eight, y_scale, stream);
+    default:
+      return norm_typed<f16>(n, d, X, ldx, R, ldr, drop, w, eps, H, ldh, Y, ldy, eight, y_scale, stream);
+  }
+}
+
+toc_status toc_rmsnorm_grad_workspace_size(int64_t n, int32_t d, size_t *bytes) {
+  clear_error();
+  if (!bytes) return fail(TOC_EINVAL, "bytes is NULL");
+  if (const toc_status st = check_norm(n, d, TOC_F32, nullptr, 1.0f)) return st;
+  *bytes = (size_t)grad_groups(n, d) * (size_t)d * 4;
+  return TOC_OK;
+}
+
+toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, int64_t ldh,
+                            const float *w, float eps, const void *dY, int64_t lddy, const void *dR,
+                            int64_t lddr, const toc_drop *drop, void *dH, int64_t lddh, void *dX,
+                            int64_t lddx, float *dw, int32_t accumulate, void *ws, size_t ws_bytes,
+                            void *stream) {
+  clear_error();
+  toc_status st;
+  if ((st = check_norm(n, d, type, w, eps)) || (st = check_drop(drop))) return st;
+  const int size = type_size(type);
+  if ((st = check_rows("H", H, n, d, ldh, size)) || (st = check_rows("dY", dY, n, d, lddy, size)) ||
+      (dR && (st = check_rows("dR", dR, n, d, lddr, size))) ||
+      (dH && (st = check_rows("dH", dH, n, d, lddh, size))) ||
+      (dX && (st = check_rows("dX", dX, n, d, lddx, size))))
+    return st;
+  if ((uintptr_t)dw % 4) return fail(TOC_EINVAL, "dw is not aligned to its elements");
+  if (dw) {
+    const size_t need = (size_t)grad_groups(n, d) * (size_t)d * 4;
+    if (need && !ws) return fail(TOC_EINVAL, "workspace is NULL");
+    if (ws_bytes < need) return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, need);
+    if ((uintptr_t)ws % 4) return fail(TOC_EINVAL, "workspace is not 4-byte aligned");
+  }
+  float *part = dw ? (float *)ws : nullptr;
+  if (n > 0) {
+    switch (type) {
+      case TOC_F32:
+        st = grad_typed<float>(n, d, H, ldh, w, eps, dY, lddy, dR, lddr, drop, dH, lddh, dX, lddx, part, stream);
+        break;
+      case TOC_BF16:
+        st = grad_typed<bf16>(n, d, H, ldh, w, eps, dY, lddy, dR, lddr, drop, dH, lddh, dX, lddx, part, stream);
+        break;
+      default:
+        st = grad_typed<f16>(n, d, H, ldh, w, eps, dY, lddy, dR, lddr, drop, dH, lddh, dX, lddx, part, stream);
+    }
+    if (st) return st;
+  }
+  if (!dw) return TOC_OK;
+  hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((d + kJoinCols - 1) / kJoinCols)),
+                     dim3(kJoinCols * kJoinParts), 0, (hipStream_t)stream, part,
+                     (int)grad_groups(n, d), d, accumulate, dw);
+  return launched("norm_join_kernel");
+}
+
+}  // extern "C"

@@ -1,0 +1,241 @@
+// What the row operators share (embedding lookup and gradient, dropout, root-mean-square
+// norm): rows of binary32, bfloat16 or binary16 numbers read and written eight columns (an
+// octet) at a time in binary32, and the dropout mask.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "toc_internal.h"
+
+namespace toc {
+namespace rows {
+
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;   // a row's number is one 32-bit counter word
+
+// --- host ------------------------------------------------------------------
+
+inline bool type_ok(int32_t type) { return type == TOC_F32 || type == TOC_BF16 || type == TOC_F16; }
+inline int type_size(int32_t type) { return type == TOC_F32 ? 4 : 2; }
+
+// A dropout mask as the kernels take it.  An element is dropped when its 16-bit word is
+// below thr = round(65536 p): p is taken to the nearest 2^-16, and 65536 / (65536 - thr)
+// makes the kept elements' mean the input's exactly at that p.
+struct Mask {
+  uint32_t k0, k1, s0, s1;   // seed (the key) and mask number, low word first
+  uint32_t thr;
+  float keep;                // what a kept element is multiplied by
+};
+
+inline Mask mask_of(const toc_drop *drop) {
+  Mask m{0, 0, 0, 0, 0, 1.0f};
+  if (!drop) return m;
+  m.k0 = (uint32_t)drop->seed;
+  m.k1 = (uint32_t)(drop->seed >> 32);
+  m.s0 = (uint32_t)drop->mask;
+  m.s1 = (uint32_t)(drop->mask >> 32);
+  m.thr = (uint32_t)std::lrint((double)drop->p * 65536.0);
+  m.keep = m.thr < 65536u ? (float)(65536.0 / (65536.0 - (double)m.thr)) : 0.0f;
+  return m;
+}
+
+// The checks of one matrix argument of n rows and d columns.
+inline toc_status check_rows(const char *name, const void *p, int64_t n, int32_t d, int64_t ld,
+                             int size) {
+  if (n > 0 && !p) return fail(TOC_EINVAL, "%s is NULL", name);
+  if (ld < d) return fail(TOC_EINVAL, "row stride %lld of %s below %d columns", (long long)ld, name, d);
+  if ((uintptr_t)p % (uintptr_t)size) return fail(TOC_EINVAL, "%s is not aligned to its %d-byte elements", name, size);
+  return TOC_OK;
+}
+
+inline toc_status check_drop(const toc_drop *drop) {
+  if (drop && !(drop->p >= 0.0f && drop->p <= 1.0f))
+    return fail(TOC_EINVAL, "dropout probability outside 0..1");
+  return TOC_OK;
+}
+
+inline toc_status check_sizes(int64_t n, int32_t d, int32_t type) {
+  if (n < 0 || d < 1) return fail(TOC_EINVAL, "%lld rows of %d columns", (long long)n, d);
+  if (!type_ok(type)) return fail(TOC_EINVAL, "unknown element type %d", type);
+  if (n > kMaxRows) return fail(TOC_EUNSUPPORTED, "more than 2^31-1 rows");
+  return TOC_OK;
+}
+
+inline toc_status check_ids(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab) {
+  if (id_bits != 32 && id_bits != 64) return fail(TOC_EINVAL, "token numbers have 32 or 64 bits, not %d", id_bits);
+  if (n > 0 && !ids) return fail(TOC_EINVAL, "ids is NULL");
+  if ((uintptr_t)ids % (uintptr_t)(id_bits / 8)) return fail(TOC_EINVAL, "ids is not aligned to its elements");
+  if (n_vocab < 0) return fail(TOC_EINVAL, "%lld table rows", (long long)n_vocab);
+  if (n_vocab > kMaxRows) return fail(TOC_EUNSUPPORTED, "more than 2^31-1 table rows");
+  return TOC_OK;
+}
+
+inline toc_status launched(const char *what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TOC_OK : fail(TOC_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Division of o < 2^31 by a divisor known on the host: floor(2^32 / divisor) times o, high
+// word, is the quotient or one less.
+struct Divisor {
+  uint32_t d, inv;
+};
+inline Divisor divisor(uint32_t d) {
+  return Divisor{d, d > 1 ? (uint32_t)(((uint64_t)1 << 32) / d) : 0xffffffffu};
+}
+__device__ inline uint32_t divide(uint32_t o, Divisor by, uint32_t *rest) {
+  uint32_t q = __umulhi(o, by.inv), r = o - q * by.d;
+  if (r >= by.d) {
+    ++q;
+    r -= by.d;
+  }
+  *rest = r;
+  return q;
+}
+
+// --- elements ----------------------------------------------------------------
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// Rows start wherever the caller's strides put them, so an octet is aligned to its elements
+// only; the hardware takes 16-byte loads and stores at such addresses.
+template <typename T>
+struct Octet {
+  uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) PackedOctet {
+  Octet<T> o;
+};
+
+// Columns 0..left-1 (at most 8) of an octet as they are stored, the others 0.  Nothing here
+// uses what is loaded, so that the loads of several octets can fly together.
+template <typename T>
+__device__ inline Octet<T> fetch8(const T *p, int left) {
+  Octet<T> o;
+  if (left >= 8) {
+    o = ((const PackedOctet<T> *)p)->o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) o.w[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+      if (i >= left) continue;
+      if (sizeof(T) == 4) o.w[i] = ((const uint32_t *)p)[i];
+      else o.w[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
+    }
+  }
+  return o;
+}
+
+__device__ inline void widen(const Octet<float> &o, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o.w[i]);
+}
+__device__ inline void widen(const Octet<bf16> &o, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(o.w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(o.w[i] & 0xffff0000u);
+  }
+}
+__device__ inline void widen(const Octet<f16> &o, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (float)__builtin_bit_cast(f16, (uint16_t)o.w[i]);
+    v[2 * i + 1] = (float)__builtin_bit_cast(f16, (uint16_t)(o.w[i] >> 16));
+  }
+}
+
+template <typename T>
+__device__ inline void load8(const T *p, int left, float (&v)[8]) {
+  widen(fetch8(p, left), v);
+}
+
+// Rounds to nearest even; a NaN stays one.
+template <typename T>
+__device__ inline void store8(T *p, int left, const float (&v)[8]) {
+  Octet<T> o;
+#pragma unroll
+  for (int i = 0; i < (int)(2 * sizeof(T)); ++i) {
+    if constexpr (sizeof(T) == 4) {
+      o.w[i] = __float_as_uint(v[i]);
+    } else {
+      const T lo = (T)v[2 * i], hi = (T)v[2 * i + 1];
+      o.w[i] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
+    }
+  }
+  if (left >= 8) {
+    ((PackedOctet<T> *)p)->o = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+      if (i >= left) continue;
+      if (sizeof(T) == 4) ((uint32_t *)p)[i] = o.w[i];
+      else ((uint16_t *)p)[i] = (uint16_t)(o.w[i / 2] >> (16 * (i % 2)));
+    }
+  }
+}
+
+struct E4m3 {
+  uint8_t b;
+};
+
+// Eight numbers of magnitude at most 448 as e4m3 numbers, rounded to nearest even.
+__device__ inline void store8(E4m3 *p, int left, const float (&v)[8]) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+    x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], x, true);
+    w[i] = (uint32_t)x;
+  }
+  if (left >= 8) {
+    __builtin_memcpy(p, w, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i].b = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// --- the mask ------------------------------------------------------------------
+
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3",
+// SC 2011): ten rounds of two 32 x 32 -> 64 bit products on a 128-bit counter.  The counter
+// is (octet of the row, row, mask number), the key the seed, and the 128 bits are eight
+// 16-bit words, one per column: the mask depends on neither strides, launch shape nor type,
+// so a gradient makes the one its forward pass used again.
+__device__ inline uint4 philox(uint32_t octet, uint32_t row, const Mask &m) {
+  uint32_t c0 = octet, c1 = row, c2 = m.s0, c3 = m.s1, k0 = m.k0, k1 = m.k1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return make_uint4(c0, c1, c2, c3);
+}
+
+// v = kept ? v * keep : 0, selected and not multiplied: a dropped infinity or NaN is 0.
+__device__ inline void drop8(float (&v)[8], uint32_t octet, uint32_t row, const Mask &m) {
+  const uint4 w = philox(octet, row, m);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (u[i] & 0xffffu) >= m.thr ? v[2 * i] * m.keep : 0.0f;
+    v[2 * i + 1] = (u[i] >> 16) >= m.thr ? v[2 * i + 1] * m.keep : 0.0f;
+  }
+}
+
+}  // namespace rows
+}  // namespace toc
