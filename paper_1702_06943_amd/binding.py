@@ -646,69 +646,86 @@ def toc_level_right_mul(blobs, blob_off, node_off, d_off, row_off, max_levels, m
 
 # --- rows of a network over tokens ---------------------------------------------
 
+# These calls are short enough for the binding's own time to count (a single token's
+# lookup runs for 3 us), so torch is looked up once and the current device once a call.
+_torch = None
 _ROW_TYPES = {}
+_raw_stream = None
 
 
-def _row_types():
-    if not _ROW_TYPES:
+def _row_device():
+    """The current device's index."""
+    global _torch, _raw_stream
+    if _torch is None:
         import torch
         _ROW_TYPES.update({torch.float32: TOC_F32, torch.bfloat16: TOC_BF16,
                            torch.float16: TOC_F16, torch.float8_e4m3fn: TOC_E4M3})
-    return _ROW_TYPES
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _torch = torch
+    return _torch.cuda.current_device()
 
 
-def _here(t, name):
-    import torch
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise TocError(TOC_EINVAL, f"{name} must be on the current CUDA device")
+def _row_stream(stream, dev):
+    """As _stream; torch's stream object costs 2.7 us, the handle alone 0.1."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
 
 
-def _row_mat(t, name, n, d, *types):
+def _row_mat(t, name, n, d, dev, types):
     """(pointer, row stride, type) of an n x d tensor of rows with unit column stride."""
-    _here(t, name)
-    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != d:
+    if t.get_device() != dev:
+        raise TocError(TOC_EINVAL, f"{name} must be on the current CUDA device")
+    if t.shape != (n, d):
         raise TocError(TOC_EINVAL, f"{name} must be {n} x {d}, not {tuple(t.shape)}")
-    kind = _row_types().get(t.dtype)
+    kind = _ROW_TYPES.get(t.dtype)
     if kind not in types:
         raise TocError(TOC_EINVAL, f"{name} has type {t.dtype}")
     ld, cs = t.stride()
     if cs != 1 and d > 1:
         raise TocError(TOC_EINVAL, f"{name} must have unit column stride")
-    if n > 1 and ld < d:
-        raise TocError(TOC_EINVAL, f"{name}'s rows overlap")
-    return _ptr(t), max(ld, d), kind
+    if ld < d:
+        if n > 1:
+            raise TocError(TOC_EINVAL, f"{name}'s rows overlap")
+        ld = d
+    return t.data_ptr() or None, ld, kind
 
 
-def _row_opt(t, name, n, d, kind):
-    return (None, d) if t is None else _row_mat(t, name, n, d, kind)[:2]
+def _row_opt(t, name, n, d, dev, kind):
+    return (None, d) if t is None else _row_mat(t, name, n, d, dev, (kind,))[:2]
 
 
-def _row_vec(t, name, n):
+def _row_shape(t, name):
+    if t.dim() != 2:
+        raise TocError(TOC_EINVAL, f"{name} must be a matrix")
+    return t.shape
+
+
+def _row_vec(t, name, n, dev):
     """Pointer of a contiguous float32 vector of n entries (None -> NULL)."""
     if t is None:
         return None
-    import torch
-    _here(t, name)
-    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise TocError(TOC_EINVAL, f"{name} must be a contiguous float32 vector of {n}")
-    return _ptr(t)
+    if (t.get_device() != dev or t.dtype != _torch.float32 or t.shape != (n,)
+            or not t.is_contiguous()):
+        raise TocError(TOC_EINVAL, f"{name} must be a contiguous float32 vector of {n} on the "
+                                   "current CUDA device")
+    return t.data_ptr() or None
 
 
-def _row_ws(t):
+def _row_ws(t, dev):
     if t is None:
         return None, 0
-    _here(t, "ws")
-    if not t.is_contiguous():
-        raise TocError(TOC_EINVAL, "ws must be contiguous")
-    return _ptr(t), t.numel() * t.element_size()
+    if t.get_device() != dev or not t.is_contiguous():
+        raise TocError(TOC_EINVAL, "ws must be contiguous, on the current CUDA device")
+    return t.data_ptr() or None, t.numel() * t.element_size()
 
 
-def _row_ids(t):
-    import torch
-    _here(t, "ids")
-    if t.dtype not in (torch.int32, torch.int64) or t.dim() != 1 or not t.is_contiguous():
-        raise TocError(TOC_EINVAL, "ids must be a contiguous vector of int32 or int64")
-    return t.shape[0], _ptr(t), 32 if t.dtype == torch.int32 else 64
+def _row_ids(t, dev):
+    bits = {_torch.int32: 32, _torch.int64: 64}.get(t.dtype)
+    if bits is None or t.get_device() != dev or t.dim() != 1 or not t.is_contiguous():
+        raise TocError(TOC_EINVAL, "ids must be a contiguous vector of int32 or int64 on the "
+                                   "current CUDA device")
+    return t.shape[0], t.data_ptr() or None, bits
 
 
 def _row_drop(drop):
@@ -726,14 +743,13 @@ def toc_embed(ids, E, out, scale=1.0, drop=None, stream=None):
     """out[t, :] = drop(scale * E[ids[t], :]).  ids: device int32 or int64 vector; E:
     n_vocab x d and out: n x d device tensors of one type (float32, bfloat16, float16); an
     id outside 0 .. n_vocab-1 gives a row of zeros; drop: a Drop, or None."""
-    n, ip, bits = _row_ids(ids)
-    if E.dim() != 2:
-        raise TocError(TOC_EINVAL, "E must be a matrix")
-    v, d = E.shape
-    ep, lde, kind = _row_mat(E, "E", v, d, *_ROWS)
-    op_, ldo, _ = _row_mat(out, "out", n, d, kind)
+    dev = _row_device()
+    n, ip, bits = _row_ids(ids, dev)
+    v, d = _row_shape(E, "E")
+    ep, lde, kind = _row_mat(E, "E", v, d, dev, _ROWS)
+    op_, ldo, _ = _row_mat(out, "out", n, d, dev, (kind,))
     _check(lib().toc_embed(n, ip, bits, v, d, kind, ep, lde, scale, _row_drop(drop), op_, ldo,
-                           _stream(stream)))
+                           _row_stream(stream, dev)))
 
 
 def toc_embed_grad_workspace_size(n, n_vocab, d):
@@ -746,41 +762,38 @@ def toc_embed_grad(ids, G, dE, ws, scale=1.0, drop=None, accumulate=False, strea
     """dE[v, :] = scale * sum of drop(G)[t, :] over ids[t] = v, or added to the rows of the
     ids that occur with accumulate.  G: n x d; dE: n_vocab x d of G's type or float32; ws:
     device tensor of toc_embed_grad_workspace_size bytes."""
-    n, ip, bits = _row_ids(ids)
-    if dE.dim() != 2:
-        raise TocError(TOC_EINVAL, "dE must be a matrix")
-    v, d = dE.shape
-    gp, ldg, kind = _row_mat(G, "G", n, d, *_ROWS)
-    ep, lde, ekind = _row_mat(dE, "dE", v, d, kind, TOC_F32)
-    wp, wn = _row_ws(ws)
+    dev = _row_device()
+    n, ip, bits = _row_ids(ids, dev)
+    v, d = _row_shape(dE, "dE")
+    gp, ldg, kind = _row_mat(G, "G", n, d, dev, _ROWS)
+    ep, lde, ekind = _row_mat(dE, "dE", v, d, dev, (kind, TOC_F32))
+    wp, wn = _row_ws(ws, dev)
     _check(lib().toc_embed_grad(n, ip, bits, v, d, kind, gp, ldg, scale, _row_drop(drop), ekind,
-                                ep, lde, 1 if accumulate else 0, wp, wn, _stream(stream)))
+                                ep, lde, 1 if accumulate else 0, wp, wn, _row_stream(stream, dev)))
 
 
 def toc_dropout(X, Y, drop, stream=None):
     """Y = drop(X): n x d device tensors of one type; Y may be X."""
-    if X.dim() != 2:
-        raise TocError(TOC_EINVAL, "X must be a matrix")
-    n, d = X.shape
-    xp, ldx, kind = _row_mat(X, "X", n, d, *_ROWS)
-    yp, ldy, _ = _row_mat(Y, "Y", n, d, kind)
-    _check(lib().toc_dropout(n, d, kind, xp, ldx, _row_drop(drop), yp, ldy, _stream(stream)))
+    dev = _row_device()
+    n, d = _row_shape(X, "X")
+    xp, ldx, kind = _row_mat(X, "X", n, d, dev, _ROWS)
+    yp, ldy, _ = _row_mat(Y, "Y", n, d, dev, (kind,))
+    _check(lib().toc_dropout(n, d, kind, xp, ldx, _row_drop(drop), yp, ldy, _row_stream(stream, dev)))
 
 
 def toc_rmsnorm(X, Y, R=None, H=None, w=None, eps=1e-5, drop=None, y_scale=None, stream=None):
     """h = R + drop(X); Y = w * h / sqrt(mean(h^2) + eps) row by row.  X, R, H (receives h):
     n x d device tensors of one type; w: device float32 vector of d, or None for ones; Y:
     n x d of that type, or float8_e4m3fn with y_scale a device float32 vector of n."""
-    if X.dim() != 2:
-        raise TocError(TOC_EINVAL, "X must be a matrix")
-    n, d = X.shape
-    xp, ldx, kind = _row_mat(X, "X", n, d, *_ROWS)
-    rp, ldr = _row_opt(R, "R", n, d, kind)
-    hp, ldh = _row_opt(H, "H", n, d, kind)
-    yp, ldy, ykind = _row_mat(Y, "Y", n, d, kind, TOC_E4M3)
-    _check(lib().toc_rmsnorm(n, d, kind, xp, ldx, rp, ldr, _row_drop(drop), _row_vec(w, "w", d),
-                             eps, hp, ldh, ykind, yp, ldy, _row_vec(y_scale, "y_scale", n),
-                             _stream(stream)))
+    dev = _row_device()
+    n, d = _row_shape(X, "X")
+    xp, ldx, kind = _row_mat(X, "X", n, d, dev, _ROWS)
+    rp, ldr = _row_opt(R, "R", n, d, dev, kind)
+    hp, ldh = _row_opt(H, "H", n, d, dev, kind)
+    yp, ldy, ykind = _row_mat(Y, "Y", n, d, dev, (kind, TOC_E4M3))
+    _check(lib().toc_rmsnorm(n, d, kind, xp, ldx, rp, ldr, _row_drop(drop), _row_vec(w, "w", d, dev),
+                             eps, hp, ldh, ykind, yp, ldy, _row_vec(y_scale, "y_scale", n, dev),
+                             _row_stream(stream, dev)))
 
 
 def toc_rmsnorm_grad_workspace_size(n, d):
@@ -795,15 +808,14 @@ def toc_rmsnorm_grad(H, dY, dH, ws, w=None, eps=1e-5, dR=None, dX=None, dw=None,
     (with dR, the gradient that reaches h otherwise, added), dX = drop(dH) of X, dw of w
     (added to with accumulate).  dH, dX, dw: outputs or None; ws: device tensor of
     toc_rmsnorm_grad_workspace_size bytes, None without dw."""
-    if H.dim() != 2:
-        raise TocError(TOC_EINVAL, "H must be a matrix")
-    n, d = H.shape
-    hp, ldh, kind = _row_mat(H, "H", n, d, *_ROWS)
-    gp, ldg, _ = _row_mat(dY, "dY", n, d, kind)
-    rp, ldr = _row_opt(dR, "dR", n, d, kind)
-    dhp, lddh = _row_opt(dH, "dH", n, d, kind)
-    dxp, lddx = _row_opt(dX, "dX", n, d, kind)
-    wp, wn = _row_ws(ws)
-    _check(lib().toc_rmsnorm_grad(n, d, kind, hp, ldh, _row_vec(w, "w", d), eps, gp, ldg, rp, ldr,
-                                  _row_drop(drop), dhp, lddh, dxp, lddx, _row_vec(dw, "dw", d),
-                                  1 if accumulate else 0, wp, wn, _stream(stream)))
+    dev = _row_device()
+    n, d = _row_shape(H, "H")
+    hp, ldh, kind = _row_mat(H, "H", n, d, dev, _ROWS)
+    gp, ldg, _ = _row_mat(dY, "dY", n, d, dev, (kind,))
+    rp, ldr = _row_opt(dR, "dR", n, d, dev, kind)
+    dhp, lddh = _row_opt(dH, "dH", n, d, dev, kind)
+    dxp, lddx = _row_opt(dX, "dX", n, d, dev, kind)
+    wp, wn = _row_ws(ws, dev)
+    _check(lib().toc_rmsnorm_grad(n, d, kind, hp, ldh, _row_vec(w, "w", d, dev), eps, gp, ldg, rp, ldr,
+                                  _row_drop(drop), dhp, lddh, dxp, lddx, _row_vec(dw, "dw", d, dev),
+                                  1 if accumulate else 0, wp, wn, _row_stream(stream, dev)))
