@@ -20,7 +20,8 @@ constexpr float kLeastMax = 0x1p-100f;   // keeps 448 / max finite; a row of zer
 __device__ inline float max_nan(float a, float b) { return a > b || a != a ? a : b; }
 
 // Sum over a group of kLanes lanes (kLanes <= 64: of one wave; else the whole workgroup, by
-// way of lds, kLanes / 64 entries each of two used in turn), in every lane.
+// way of kLanes / 64 words of lds), in every lane.  A caller's next use of the same words
+// must lie behind another barrier of the workgroup.
 template <int kLanes>
 __device__ inline float group_sum(float x, float *lds) {
 #pragma unroll
@@ -31,6 +32,26 @@ __device__ inline float group_sum(float x, float *lds) {
     x = 0.0f;
 #pragma unroll
     for (int i = 0; i < kLanes / 64; ++i) x += lds[i];
+  }
+  return x;
+}
+// Two sums at once; lds: two of kLanes / 64 pairs, used in turn.
+template <int kLanes>
+__device__ inline float2 group_sum2(float2 x, float2 *lds) {
+#pragma unroll
+  for (int o = (kLanes < 64 ? kLanes : 64) / 2; o > 0; o >>= 1) {
+    x.x += __shfl_xor(x.x, o, 64);
+    x.y += __shfl_xor(x.y, o, 64);
+  }
+  if (kLanes > 64) {
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kLanes / 64; ++i) {
+      x.x += lds[i].x;
+      x.y += lds[i].y;
+    }
   }
   return x;
 }
@@ -182,16 +203,17 @@ struct GradArgs {
   int64_t lddh;
   T *dX;               // or NULL
   int64_t lddx;
-  float *part;         // NULL, or one row of d per group: its part of dw
+  float *part;         // NULL, or one row of d per workgroup: its part of dw
 };
 
 template <typename T, int kLanes, int kOct, bool kDrop>
 __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(GradArgs<T> a) {
   constexpr int kBlock = kLanes > 256 ? kLanes : 256;
   constexpr int kGroups = kBlock / kLanes;
-  __shared__ float part[2][kLanes > 64 ? kLanes / 64 : 1];
+  __shared__ float2 part[2][kLanes > 64 ? kLanes / 64 : 1];
   const int lane = threadIdx.x % kLanes;
   const uint32_t group = blockIdx.x * kGroups + threadIdx.x / kLanes;
+  int turn = 0;
   float w[kOct][8], dw[kOct][8];
   load_w<kOct>(a.w, a.d, lane, kLanes, w);
 #pragma unroll
@@ -200,7 +222,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     for (int i = 0; i < 8; ++i) dw[k][i] = 0.0f;
   for (uint32_t row = group; row < a.n; row += gridDim.x * kGroups) {
     float h[kOct][8], g[kOct][8];
-    float hh = 0.0f, gh = 0.0f;
+    float2 sum = make_float2(0.0f, 0.0f);   // of h^2 and of g h
     Octet<T> hin[kOct], gin[kOct], rin[kOct];
 #pragma unroll
     for (int k = 0; k < kOct; ++k) {
@@ -224,13 +246,14 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     for (int k = 0; k < kOct; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        hh = fmaf(h[k][i], h[k][i], hh);
-        gh = fmaf(g[k][i] * w[k][i], h[k][i], gh);
+        sum.x = fmaf(h[k][i], h[k][i], sum.x);
+        sum.y = fmaf(g[k][i] * w[k][i], h[k][i], sum.y);
       }
-    hh = group_sum<kLanes>(hh, part[0]);
-    gh = group_sum<kLanes>(gh, part[1]);
-    const float r = inv_rms(hh, a.inv_d, a.eps);
-    const float c3 = r * r * r * (gh * a.inv_d);
+    // (two rows' words: the row before this one's may still be read)
+    sum = group_sum2<kLanes>(sum, part[turn]);
+    turn ^= 1;
+    const float r = inv_rms(sum.x, a.inv_d, a.eps);
+    const float c3 = r * r * r * (sum.y * a.inv_d);
 #pragma unroll
     for (int k = 0; k < kOct; ++k) {
       const int c = 8 * (lane + k * kLanes);
@@ -254,32 +277,54 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     }
   }
   if (!a.part) return;
+  float *to = a.part + (int64_t)blockIdx.x * a.d;
+  if (kGroups == 1) {
 #pragma unroll
-  for (int k = 0; k < kOct; ++k) {
-    const int c = 8 * (lane + k * kLanes);
-    if (c < a.d) store8(a.part + (int64_t)group * a.d + c, a.d - c, dw[k]);
+    for (int k = 0; k < kOct; ++k) {
+      const int c = 8 * (lane + k * kLanes);
+      if (c < a.d) store8(to + c, a.d - c, dw[k]);
+    }
+    return;
+  }
+  // the workgroup's groups, in order
+  constexpr int kCols = 8 * kLanes * kOct;
+  __shared__ float all[kGroups > 1 ? kGroups * kCols : 1];
+#pragma unroll
+  for (int k = 0; k < kOct; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all[threadIdx.x / kLanes * kCols + 8 * (lane + k * kLanes) + i] = dw[k][i];
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.d; c += kBlock) {
+    float s = all[c];
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) s += all[g * kCols + c];
+    to[c] = s;
   }
 }
 
-// dw (+)= the groups' parts, in the groups' order.
-constexpr int kJoinCols = 32, kJoinParts = 8;
+// dw (+)= the workgroups' parts, in their order: kJoinParts runs of them at once, then the
+// runs.
+constexpr int kJoinCols = 16, kJoinParts = 64;
 __global__ __launch_bounds__(kJoinCols * kJoinParts) void norm_join_kernel(
-    const float *__restrict__ part, int groups, int d, int accumulate, float *__restrict__ dw) {
-  __shared__ float sums[kJoinParts][kJoinCols];
-  const int c = blockIdx.x * kJoinCols + threadIdx.x % kJoinCols, p = threadIdx.x / kJoinCols;
-  const int per = (groups + kJoinParts - 1) / kJoinParts;
+    const float *__restrict__ part, int parts, int d, int accumulate, float *__restrict__ dw) {
+  __shared__ float sums[kJoinParts][kJoinCols + 1];
+  const int col = threadIdx.x % kJoinCols, p = threadIdx.x / kJoinCols;
+  const int c = blockIdx.x * kJoinCols + col;
+  const int per = (parts + kJoinParts - 1) / kJoinParts;
   float s = 0.0f;
   if (c < d) {
-    const int end = min(groups, (p + 1) * per);
+    const int end = min(parts, (p + 1) * per);
 #pragma unroll 8
     for (int g = p * per; g < end; ++g) s += part[(int64_t)g * d + c];
   }
-  sums[p][threadIdx.x % kJoinCols] = s;
+  sums[p][col] = s;
   __syncthreads();
-  if (p != 0 || c >= d) return;
 #pragma unroll
-  for (int q = 1; q < kJoinParts; ++q) s += sums[q][threadIdx.x % kJoinCols];
-  dw[c] = accumulate ? dw[c] + s : s;
+  for (int n = kJoinParts / 2; n > 0; n /= 2) {
+    if (p < n) sums[p][col] += sums[p + n][col];
+    __syncthreads();
+  }
+  if (p == 0 && c < d) dw[c] = accumulate ? dw[c] + sums[0][col] : sums[0][col];
 }
 
 // Lanes to a row and octets to a lane: the fewest that hold the row.
@@ -342,10 +387,7 @@ toc_status norm_grad(const GradArgs<T> &a, hipStream_t s) {
 }
 
 // Rows of partial dw sums a call leaves in its workspace.
-int64_t grad_groups(int64_t n, int32_t d) {
-  const Shape sh = shape_of(d);
-  return n ? blocks_for(n, sh, kGradBlocks) * (sh.lanes > 256 ? 1 : 256 / sh.lanes) : 0;
-}
+int64_t grad_parts(int64_t n, int32_t d) { return n ? blocks_for(n, shape_of(d), kGradBlocks) : 0; }
 
 template <typename T>
 toc_status norm_typed(int64_t n, int32_t d, const void *X, int64_t ldx, const void *R, int64_t ldr,
@@ -415,7 +457,7 @@ toc_status toc_rmsnorm_grad_workspace_size(int64_t n, int32_t d, size_t *bytes) 
   clear_error();
   if (!bytes) return fail(TOC_EINVAL, "bytes is NULL");
   if (const toc_status st = check_norm(n, d, TOC_F32, nullptr, 1.0f)) return st;
-  *bytes = (size_t)grad_groups(n, d) * (size_t)d * 4;
+  *bytes = (size_t)grad_parts(n, d) * (size_t)d * 4;
   return TOC_OK;
 }
 
@@ -435,7 +477,7 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
     return st;
   if ((uintptr_t)dw % 4) return fail(TOC_EINVAL, "dw is not aligned to its elements");
   if (dw) {
-    const size_t need = (size_t)grad_groups(n, d) * (size_t)d * 4;
+    const size_t need = (size_t)grad_parts(n, d) * (size_t)d * 4;
     if (need && !ws) return fail(TOC_EINVAL, "workspace is NULL");
     if (ws_bytes < need) return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, need);
     if ((uintptr_t)ws % 4) return fail(TOC_EINVAL, "workspace is not 4-byte aligned");
@@ -457,7 +499,7 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
   if (!dw) return TOC_OK;
   hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((d + kJoinCols - 1) / kJoinCols)),
                      dim3(kJoinCols * kJoinParts), 0, (hipStream_t)stream, part,
-                     (int)grad_groups(n, d), d, accumulate, dw);
+                     (int)grad_parts(n, d), d, accumulate, dw);
   return launched("norm_join_kernel");
 }
 
