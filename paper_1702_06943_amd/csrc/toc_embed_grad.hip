@@ -5,7 +5,7 @@
 //          of every digit (count_kernel), then each tile places its pairs (scatter_kernel);
 //          numbers outside the table sort last, as number V
 //   sum    the sorted list cut into chunks of equal length, so that a frequent number costs
-//          no more than others: a group of lanes walks a chunk, its octets of dE's row in
+//          no more than others: a group of lanes walks a chunk, its chunks of dE's row in
 //          registers, and writes a row when its number ends.  A number that crosses chunks
 //          leaves one partial row in each
 //   join   partial rows added in the chunks' order
@@ -183,50 +183,50 @@ struct SumArgs {
   int accumulate;
 };
 
-template <typename TO>
-__device__ inline void write_row(TO *p, int left, float (&v)[8], float scale, int accumulate) {
+template <typename TO, int N>
+__device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, int accumulate) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= scale;
+  for (int i = 0; i < N; ++i) v[i] *= scale;
   if (accumulate) {
-    float old[8];
-    load8((const TO *)p, left, old);
+    float old[N];
+    load((const TO *)p, left, old);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += old[i];
+    for (int i = 0; i < N; ++i) v[i] += old[i];
   }
-  store8(p, left, v);
+  store(p, left, v);
 }
 
-// Chunk blockIdx.x * (256 / lanes) + group, columns from 8 lanes blockIdx.y.
+// Chunk blockIdx.x * (256 / lanes) + group, columns from kCols lanes blockIdx.y.
 template <typename T, typename TO, bool kDrop>
 __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde) {
   const uint32_t chunk = blockIdx.x * (uint32_t)(kSumBlock / a.lanes) + threadIdx.x / a.lanes;
-  const uint32_t oct = blockIdx.y * a.lanes + threadIdx.x % a.lanes;
-  const int c = (int)oct * 8, left = a.d - c;
+  constexpr int N = kCols<T>;
+  const int c = (int)(blockIdx.y * a.lanes + threadIdx.x % a.lanes) * N, left = a.d - c;
   if (chunk >= a.chunks || left <= 0) return;
   const uint32_t e0 = chunk * a.chunk, e1 = min(a.n, e0 + a.chunk);
   const uint32_t after = e1 < a.n ? a.key[e1] : kNone;
   uint32_t cur = a.key[e0];
   bool from_before = e0 > 0 && a.key[e0 - 1] == cur;
-  float acc[8];
+  float acc[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+  for (int i = 0; i < N; ++i) acc[i] = 0.0f;
   auto flush = [&](bool goes_on) {
     if (cur >= a.n_vocab) return;
     if (from_before || goes_on)
-      store8(a.part + ((int64_t)chunk * 2 + (from_before ? 0 : 1)) * a.d + c, left, acc);
+      store(a.part + ((int64_t)chunk * 2 + (from_before ? 0 : 1)) * a.d + c, left, acc);
     else
       write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
   };
   for (uint32_t e = e0; e < e1; e += kAhead) {
     uint32_t k[kAhead], p[kAhead];
-    Octet<T> in[kAhead];
+    Chunk in[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       k[u] = e + u < e1 ? a.key[e + u] : kNone;
       p[u] = e + u < e1 ? a.pos[e + u] : 0u;
     }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) in[u] = fetch8(a.G + (int64_t)p[u] * a.ldg + c, k[u] < a.n_vocab ? left : 0);
+    for (int u = 0; u < kAhead; ++u) in[u] = fetch(a.G + (int64_t)p[u] * a.ldg + c, k[u] < a.n_vocab ? left : 0);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (e + u >= e1) break;
@@ -235,13 +235,13 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
         cur = k[u];
         from_before = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
       }
-      float v[8];
-      widen(in[u], v);
-      if (kDrop) drop8(v, oct, p[u], a.m);
+      float v[N];
+      widen<T>(in[u], v);
+      if (kDrop) drop_cols(v, (uint32_t)c, p[u], a.m);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      for (int i = 0; i < N; ++i) acc[i] += v[i];
     }
   }
   flush(after == cur);
@@ -252,7 +252,8 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
 // workgroup's groups of lanes.
 template <typename T, typename TO>
 __global__ __launch_bounds__(kSumBlock) void join_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde) {
-  __shared__ float sums[kSumBlock][8];
+  constexpr int N = kCols<T>;
+  __shared__ float sums[kSumBlock][N];
   const uint32_t chunk = blockIdx.x;
   const uint32_t e0 = chunk * a.chunk, e1 = min(a.n, e0 + a.chunk);
   if (e1 >= a.n) return;
@@ -267,68 +268,66 @@ __global__ __launch_bounds__(kSumBlock) void join_kernel(SumArgs<T> a, TO *__res
   }
   const uint32_t parts = (lo - 1) / a.chunk - chunk;                 // starts of later chunks
   const uint32_t groups = kSumBlock / a.lanes, group = threadIdx.x / a.lanes;
-  const uint32_t oct = blockIdx.y * a.lanes + threadIdx.x % a.lanes;
-  const int c = (int)oct * 8, left = a.d - c;
+  const int c = (int)(blockIdx.y * a.lanes + threadIdx.x % a.lanes) * N, left = a.d - c;
   const uint32_t per = (parts + groups - 1) / groups;
-  float acc[8];
+  float acc[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+  for (int i = 0; i < N; ++i) acc[i] = 0.0f;
   if (left > 0) {
-    if (group == 0) load8((const float *)a.part + ((int64_t)chunk * 2 + 1) * a.d + c, left, acc);
+    if (group == 0) load((const float *)a.part + ((int64_t)chunk * 2 + 1) * a.d + c, left, acc);
     const uint32_t q1 = min(parts, (group + 1) * per);
 #pragma unroll 4
     for (uint32_t q = group * per; q < q1; ++q) {
-      float v[8];
-      load8((const float *)a.part + ((int64_t)(chunk + 1 + q) * 2) * a.d + c, left, v);
+      float v[N];
+      load((const float *)a.part + ((int64_t)(chunk + 1 + q) * 2) * a.d + c, left, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      for (int i = 0; i < N; ++i) acc[i] += v[i];
     }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = acc[i];
+  for (int i = 0; i < N; ++i) sums[threadIdx.x][i] = acc[i];
   __syncthreads();
   if (group != 0 || left <= 0) return;
   for (uint32_t g = 1; g < groups; ++g)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += sums[g * a.lanes + threadIdx.x][i];
+    for (int i = 0; i < N; ++i) acc[i] += sums[g * a.lanes + threadIdx.x][i];
   write_row(dE + (int64_t)key * lde + c, left, acc, a.scale, a.accumulate);
 }
 
 // Rows row0 .. of dE whose number does not occur.  present: NULL when none does.
 template <typename TO>
 __global__ __launch_bounds__(kZeroBlock) void zero_kernel(const uint8_t *__restrict__ present, uint32_t total,
-                                                          int d, Divisor octets, TO *__restrict__ dE,
+                                                          int d, Divisor chunks, TO *__restrict__ dE,
                                                           int64_t lde) {
-  const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const float zero[kCols<TO>] = {};
 #pragma unroll
   for (int k = 0; k < kZeroPer; ++k) {
     const uint32_t o = blockIdx.x * (uint32_t)(kZeroBlock * kZeroPer) + k * kZeroBlock + threadIdx.x;
     if (o >= total) return;
-    uint32_t oct;
-    const uint32_t row = divide(o, octets, &oct);
+    uint32_t at;
+    const uint32_t row = divide(o, chunks, &at);
     if (present && present[row]) continue;
-    const int c = (int)oct * 8;
-    store8(dE + (int64_t)row * lde + c, d - c, zero);
+    const int c = (int)at * kCols<TO>;
+    store(dE + (int64_t)row * lde + c, d - c, zero);
   }
 }
 
 template <typename TO>
 void zero_rows(int64_t n_vocab, int32_t d, const uint8_t *present, TO *dE, int64_t lde, hipStream_t s) {
-  const uint32_t octets = (uint32_t)((d + 7) / 8);
-  const int64_t most = ((int64_t)1 << 30) / octets;
+  const uint32_t chunks = chunks_of<TO>(d);
+  const int64_t most = ((int64_t)1 << 30) / chunks;
   for (int64_t r = 0; r < n_vocab; r += most) {
-    const uint32_t total = (uint32_t)(std::min(most, n_vocab - r) * octets);
+    const uint32_t total = (uint32_t)(std::min(most, n_vocab - r) * chunks);
     hipLaunchKernelGGL(zero_kernel<TO>, dim3((total + kZeroBlock * kZeroPer - 1) / (kZeroBlock * kZeroPer)),
-                       dim3(kZeroBlock), 0, s, present ? present + r : nullptr, total, d, divisor(octets),
+                       dim3(kZeroBlock), 0, s, present ? present + r : nullptr, total, d, divisor(chunks),
                        dE + r * lde, lde);
   }
 }
 
-// Lanes that walk a chunk: a power of two that holds a row's octets, at most a wave.
-int lanes_of(int32_t d) {
-  const int octets = (d + 7) / 8;
+// Lanes that walk a chunk: a power of two that holds a row's chunks, at most a wave.
+int lanes_of(uint32_t chunks) {
   int lanes = 8;
-  while (lanes < octets && lanes < 64) lanes *= 2;
+  while ((uint32_t)lanes < chunks && lanes < 64) lanes *= 2;
   return lanes;
 }
 
@@ -371,9 +370,9 @@ toc_status grad(const Plan &p, int64_t n, const void *ids, int32_t id_bits, int6
   else sort_ids(p, n, (const int64_t *)ids, n_vocab, ws, s);
   const int last = (p.passes - 1) % 2;
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
-               (uint32_t)n_vocab, (uint32_t)p.chunk, (uint32_t)p.chunks, d, lanes_of(d), G, ldg, scale,
+               (uint32_t)n_vocab, (uint32_t)p.chunk, (uint32_t)p.chunks, d, lanes_of(chunks_of<T>(d)), G, ldg, scale,
                mask_of(drop), (float *)(ws + p.part), accumulate};
-  const unsigned slices = (unsigned)((d + 8 * a.lanes - 1) / (8 * a.lanes));
+  const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
   const unsigned per = (unsigned)(kSumBlock / a.lanes);
   const dim3 grid((unsigned)((p.chunks + per - 1) / per), slices);
   if (!accumulate) zero_rows(n_vocab, d, ws + p.present, dE, lde, s);

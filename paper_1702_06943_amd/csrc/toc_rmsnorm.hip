@@ -3,10 +3,10 @@
 // for a row of d columns; 8-bit output: s = max(max_j |y_j|, 2^-100) / 448 and y_j / s as
 // e4m3 numbers.  With g_j = dy_j w_j the gradients are
 //   dh_j = r g_j - h_j r^3 mean_i(g_i h_i) + dR_j     dX = drop(dh)     dw_j = sum over rows dy_j h_j r
-// A row stays in registers between its one read and its one write, as octets of a group of
+// A row stays in registers between its one read and its one write, as chunks of a group of
 // lanes of one wave, or of the lanes of a workgroup; groups walk over the rows, so that w
 // (and, on the way back, the group's part of dw) is read once and kept.  Sums are binary32:
-// a lane's octets in order, then the lanes in a tree.  Bound by memory.
+// a lane's chunks in order, then the lanes in a tree.  Bound by memory.
 #include "toc_rows_dev.h"
 
 namespace toc {
@@ -90,67 +90,68 @@ struct NormArgs {
   float *y_scale;
 };
 
-template <int kOct>
-__device__ inline void load_w(const float *w, int d, int lane, int lanes, float (&v)[kOct][8]) {
+template <int kPer, int N>
+__device__ inline void load_w(const float *w, int d, int lane, int lanes, float (&v)[kPer][N]) {
 #pragma unroll
-  for (int k = 0; k < kOct; ++k) {
-    const int c = 8 * (lane + k * lanes);
+  for (int k = 0; k < kPer; ++k) {
+    const int c = N * (lane + k * lanes);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = c + i < d ? 1.0f : 0.0f;
-    if (w && c < d) load8(w + c, d - c, v[k]);
+    for (int i = 0; i < N; ++i) v[k][i] = c + i < d ? 1.0f : 0.0f;
+    if (w && c < d) load(w + c, d - c, v[k]);
   }
 }
 
-// kLanes lanes to a row, kOct octets to a lane (8 kLanes kOct >= d).
-template <typename T, typename Y, int kLanes, int kOct, bool kDrop>
+// kLanes lanes to a row, kPer chunks to a lane (kCols kLanes kPer >= d).
+template <typename T, typename Y, int kLanes, int kPer, bool kDrop>
 __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormArgs<T> a, Y *Yp) {
   constexpr int kBlock = kLanes > 256 ? kLanes : 256;
   constexpr int kGroups = kBlock / kLanes;
+  constexpr int N = kCols<T>;
   constexpr bool k8 = std::is_same<Y, E4m3>::value;
   __shared__ float part[2][kLanes > 64 ? kLanes / 64 : 1];
   const int lane = threadIdx.x % kLanes;
-  float w[kOct][8];
-  load_w<kOct>(a.w, a.d, lane, kLanes, w);
+  float w[kPer][N];
+  load_w(a.w, a.d, lane, kLanes, w);
   // (kLanes >= 64: all lanes of a wave, so all waves of a workgroup, share a row)
   for (uint32_t row = blockIdx.x * kGroups + threadIdx.x / kLanes; row < a.n; row += gridDim.x * kGroups) {
-    float h[kOct][8];
+    float h[kPer][N];
     float sum = 0.0f, most = 0.0f;
     const T *x = a.X + (int64_t)row * a.ldx, *res = a.R + (int64_t)row * a.ldr;
-    Octet<T> in[kOct], rin[kOct];
+    Chunk in[kPer], rin[kPer];
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      const int c = 8 * (lane + k * kLanes);
-      in[k] = fetch8(x + c, a.d - c);
+    for (int k = 0; k < kPer; ++k) {
+      const int c = N * (lane + k * kLanes);
+      in[k] = fetch(x + c, a.d - c);
     }
     if (a.R) {
 #pragma unroll
-      for (int k = 0; k < kOct; ++k) {
-        const int c = 8 * (lane + k * kLanes);
-        rin[k] = fetch8(res + c, a.d - c);
+      for (int k = 0; k < kPer; ++k) {
+        const int c = N * (lane + k * kLanes);
+        rin[k] = fetch(res + c, a.d - c);
       }
     }
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) widen(in[k], h[k]);
+    for (int k = 0; k < kPer; ++k) widen<T>(in[k], h[k]);
     if (kDrop) {
 #pragma unroll
-      for (int k = 0; k < kOct; ++k) drop8(h[k], (uint32_t)(lane + k * kLanes), row, a.m);
+      for (int k = 0; k < kPer; ++k) drop_cols(h[k], (uint32_t)(N * (lane + k * kLanes)), row, a.m);
     }
     if (a.R) {
 #pragma unroll
-      for (int k = 0; k < kOct; ++k) {
-        float v[8];
-        widen(rin[k], v);
+      for (int k = 0; k < kPer; ++k) {
+        float v[N];
+        widen<T>(rin[k], v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[k][i] += v[i];
+        for (int i = 0; i < N; ++i) h[k][i] += v[i];
       }
     }
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
+    for (int k = 0; k < kPer; ++k) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(h[k][i], h[k][i], sum);
+      for (int i = 0; i < N; ++i) sum = fmaf(h[k][i], h[k][i], sum);
       if (k8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = max_nan(fabsf(h[k][i] * w[k][i]), most);
+        for (int i = 0; i < N; ++i) most = max_nan(fabsf(h[k][i] * w[k][i]), most);
       }
     }
     // (the row before may still be reading the other reduction's words, never these: a
@@ -167,13 +168,13 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
       __syncthreads();   // part[0] is free again
     }
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      const int c = 8 * (lane + k * kLanes);
+    for (int k = 0; k < kPer; ++k) {
+      const int c = N * (lane + k * kLanes);
       if (c >= a.d) continue;
-      if (a.H) store8(a.H + (int64_t)row * a.ldh + c, a.d - c, h[k]);
-      float y[8];
+      if (a.H) store(a.H + (int64_t)row * a.ldh + c, a.d - c, h[k]);
+      float y[N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         y[i] = h[k][i] * r * w[k][i];
         if (k8) {
           y[i] *= s;
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
           y[i] = y[i] > kE4m3Max ? kE4m3Max : y[i] < -kE4m3Max ? -kE4m3Max : y[i];
         }
       }
-      store8(Yp + (int64_t)row * a.ldy + c, a.d - c, y);
+      store(Yp + (int64_t)row * a.ldy + c, a.d - c, y);
     }
   }
 }
@@ -206,46 +207,47 @@ struct GradArgs {
   float *part;         // NULL, or one row of d per workgroup: its part of dw
 };
 
-template <typename T, int kLanes, int kOct, bool kDrop>
+template <typename T, int kLanes, int kPer, bool kDrop>
 __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(GradArgs<T> a) {
   constexpr int kBlock = kLanes > 256 ? kLanes : 256;
   constexpr int kGroups = kBlock / kLanes;
+  constexpr int N = kCols<T>;
   __shared__ float2 part[2][kLanes > 64 ? kLanes / 64 : 1];
   const int lane = threadIdx.x % kLanes;
   const uint32_t group = blockIdx.x * kGroups + threadIdx.x / kLanes;
   int turn = 0;
-  float w[kOct][8], dw[kOct][8];
-  load_w<kOct>(a.w, a.d, lane, kLanes, w);
+  float w[kPer][N], dw[kPer][N];
+  load_w(a.w, a.d, lane, kLanes, w);
 #pragma unroll
-  for (int k = 0; k < kOct; ++k)
+  for (int k = 0; k < kPer; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw[k][i] = 0.0f;
+    for (int i = 0; i < N; ++i) dw[k][i] = 0.0f;
   for (uint32_t row = group; row < a.n; row += gridDim.x * kGroups) {
-    float h[kOct][8], g[kOct][8];
+    float h[kPer][N], g[kPer][N];
     float2 sum = make_float2(0.0f, 0.0f);   // of h^2 and of g h
-    Octet<T> hin[kOct], gin[kOct], rin[kOct];
+    Chunk hin[kPer], gin[kPer], rin[kPer];
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      const int c = 8 * (lane + k * kLanes);
-      hin[k] = fetch8(a.H + (int64_t)row * a.ldh + c, a.d - c);
-      gin[k] = fetch8(a.dY + (int64_t)row * a.lddy + c, a.d - c);
+    for (int k = 0; k < kPer; ++k) {
+      const int c = N * (lane + k * kLanes);
+      hin[k] = fetch(a.H + (int64_t)row * a.ldh + c, a.d - c);
+      gin[k] = fetch(a.dY + (int64_t)row * a.lddy + c, a.d - c);
     }
     if (a.dR) {
 #pragma unroll
-      for (int k = 0; k < kOct; ++k) {
-        const int c = 8 * (lane + k * kLanes);
-        rin[k] = fetch8(a.dR + (int64_t)row * a.lddr + c, a.d - c);
+      for (int k = 0; k < kPer; ++k) {
+        const int c = N * (lane + k * kLanes);
+        rin[k] = fetch(a.dR + (int64_t)row * a.lddr + c, a.d - c);
       }
     }
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      widen(hin[k], h[k]);
-      widen(gin[k], g[k]);
+    for (int k = 0; k < kPer; ++k) {
+      widen<T>(hin[k], h[k]);
+      widen<T>(gin[k], g[k]);
     }
 #pragma unroll
-    for (int k = 0; k < kOct; ++k)
+    for (int k = 0; k < kPer; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         sum.x = fmaf(h[k][i], h[k][i], sum.x);
         sum.y = fmaf(g[k][i] * w[k][i], h[k][i], sum.y);
       }
@@ -255,24 +257,24 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     const float r = inv_rms(sum.x, a.inv_d, a.eps);
     const float c3 = r * r * r * (sum.y * a.inv_d);
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      const int c = 8 * (lane + k * kLanes);
+    for (int k = 0; k < kPer; ++k) {
+      const int c = N * (lane + k * kLanes);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         dw[k][i] = fmaf(g[k][i] * r, h[k][i], dw[k][i]);
         h[k][i] = fmaf(g[k][i] * w[k][i], r, -h[k][i] * c3);
       }
       if (c >= a.d) continue;
       if (a.dR) {
-        float v[8];
-        widen(rin[k], v);
+        float v[N];
+        widen<T>(rin[k], v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[k][i] += v[i];
+        for (int i = 0; i < N; ++i) h[k][i] += v[i];
       }
-      if (a.dH) store8(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k]);
+      if (a.dH) store(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k]);
       if (a.dX) {
-        if (kDrop) drop8(h[k], (uint32_t)(c / 8), row, a.m);
-        store8(a.dX + (int64_t)row * a.lddx + c, a.d - c, h[k]);
+        if (kDrop) drop_cols(h[k], (uint32_t)c, row, a.m);
+        store(a.dX + (int64_t)row * a.lddx + c, a.d - c, h[k]);
       }
     }
   }
@@ -280,19 +282,19 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
   float *to = a.part + (int64_t)blockIdx.x * a.d;
   if (kGroups == 1) {
 #pragma unroll
-    for (int k = 0; k < kOct; ++k) {
-      const int c = 8 * (lane + k * kLanes);
-      if (c < a.d) store8(to + c, a.d - c, dw[k]);
+    for (int k = 0; k < kPer; ++k) {
+      const int c = N * (lane + k * kLanes);
+      if (c < a.d) store(to + c, a.d - c, dw[k]);
     }
     return;
   }
   // the workgroup's groups, in order
-  constexpr int kCols = 8 * kLanes * kOct;
+  constexpr int kCols = N * kLanes * kPer;
   __shared__ float all[kGroups > 1 ? kGroups * kCols : 1];
 #pragma unroll
-  for (int k = 0; k < kOct; ++k)
+  for (int k = 0; k < kPer; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) all[threadIdx.x / kLanes * kCols + 8 * (lane + k * kLanes) + i] = dw[k][i];
+    for (int i = 0; i < N; ++i) all[threadIdx.x / kLanes * kCols + N * (lane + k * kLanes) + i] = dw[k][i];
   __syncthreads();
   for (int c = threadIdx.x; c < a.d; c += kBlock) {
     float s = all[c];
@@ -327,67 +329,85 @@ __global__ __launch_bounds__(kJoinCols * kJoinParts) void norm_join_kernel(
   if (p == 0 && c < d) dw[c] = accumulate ? dw[c] + sums[0][col] : sums[0][col];
 }
 
-// Lanes to a row and octets to a lane: the fewest that hold the row.
+// Lanes to a row and chunks to a lane.
 struct Shape {
-  int lanes, oct;
+  int lanes, per;
 };
 constexpr int32_t kMaxCols = 16384;
-Shape shape_of(int32_t d) {
-  const int octets = (d + 7) / 8;
-  if (octets <= 8) return {8, 1};
-  if (octets <= 32) return {32, 1};
-  if (octets <= 64) return {64, 1};
-  if (octets <= 128) return {64, 2};
-  if (octets <= 256) return {256, 1};
-  if (octets <= 512) return {256, 2};
-  if (octets <= 1024) return {1024, 1};
-  return {1024, 2};
+Shape shape_of(uint32_t chunks, bool grad) {
+  if (chunks <= 8) return {8, 1};
+  if (chunks <= 32) return {32, 1};
+  if (chunks <= 64) return {64, 1};
+  if (chunks <= 128) return {64, 2};
+  if (chunks <= 256) return {256, 1};
+  if (chunks <= 512) return {256, 2};
+  if (chunks <= 1024) return grad ? Shape{1024, 1} : Shape{512, 2};
+  if (chunks <= 2048) return {1024, 2};
+  return {1024, 4};   // binary32 only
 }
+// F(lanes, per) for each shape that rows of T can take
+#define TOC_SHAPES(F) F(8, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(1024, 2)
 
-// Workgroups of a launch: as many as the rows need, at most what fills the chip.
+// Workgroups of a launch: as many as the rows need, at most `most`.  Forward, rows of at most
+// 256 lanes get a workgroup each (32,768 x 2,048 bf16 with dropout: 93.5 us, 101 with 4,096
+// workgroups that walk), longer ones walk (8,192 x 8,192: 93 us, 98.5 with a workgroup each).
+// Backward all walk, since each workgroup leaves a row of dw's parts (2,048: 142 us, 1,024:
+// 133, 512: 135 for 32,768 x 2,048).
 int64_t blocks_for(int64_t n, Shape sh, int64_t most) {
   const int64_t groups = sh.lanes > 256 ? 1 : 256 / sh.lanes;
-  return std::max<int64_t>(1, std::min((n + groups - 1) / groups, sh.lanes > 256 ? most / 4 : most));
+  return std::max<int64_t>(1, std::min((n + groups - 1) / groups, most));
 }
-constexpr int64_t kNormBlocks = 4096, kGradBlocks = 1024;
-
-#define TOC_SHAPES(F)                                                                     \
-  F(8, 1) F(32, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(1024, 1) F(1024, 2)
+int64_t norm_blocks(int64_t n, Shape sh) { return blocks_for(n, sh, sh.lanes > 256 ? 1024 : 1 << 22); }
+int64_t grad_blocks(int64_t n, Shape sh) { return blocks_for(n, sh, sh.lanes > 256 ? 256 : 1024); }
 
 template <typename T, typename Y>
 toc_status norm(const NormArgs<T> &a, Y *y, hipStream_t s) {
-  const Shape sh = shape_of(a.d);
-  const dim3 grid((unsigned)blocks_for(a.n, sh, kNormBlocks)), block((unsigned)std::max(sh.lanes, 256));
+  const Shape sh = shape_of(chunks_of<T>(a.d), false);
+  const dim3 grid((unsigned)norm_blocks(a.n, sh)), block((unsigned)std::max(sh.lanes, 256));
 #define TOC_NORM(L, K)                                                                     \
-  if (sh.lanes == L && sh.oct == K) {                                                      \
+  if (sh.lanes == L && sh.per == K) {                                                      \
     if (a.m.thr)                                                                           \
       hipLaunchKernelGGL((norm_kernel<T, Y, L, K, true>), grid, block, 0, s, a, y);        \
     else                                                                                   \
       hipLaunchKernelGGL((norm_kernel<T, Y, L, K, false>), grid, block, 0, s, a, y);       \
   }
   TOC_SHAPES(TOC_NORM)
+  TOC_NORM(512, 2)
+  if constexpr (sizeof(T) == 4) {
+    TOC_NORM(1024, 4)
+  }
 #undef TOC_NORM
   return launched("norm_kernel");
 }
 
 template <typename T>
 toc_status norm_grad(const GradArgs<T> &a, hipStream_t s) {
-  const Shape sh = shape_of(a.d);
-  const dim3 grid((unsigned)blocks_for(a.n, sh, kGradBlocks)), block((unsigned)std::max(sh.lanes, 256));
+  const Shape sh = shape_of(chunks_of<T>(a.d), true);
+  const dim3 grid((unsigned)grad_blocks(a.n, sh)), block((unsigned)std::max(sh.lanes, 256));
 #define TOC_GRAD(L, K)                                                                     \
-  if (sh.lanes == L && sh.oct == K) {                                                      \
+  if (sh.lanes == L && sh.per == K) {                                                      \
     if (a.m.thr)                                                                           \
       hipLaunchKernelGGL((norm_grad_kernel<T, L, K, true>), grid, block, 0, s, a);         \
     else                                                                                   \
       hipLaunchKernelGGL((norm_grad_kernel<T, L, K, false>), grid, block, 0, s, a);        \
   }
   TOC_SHAPES(TOC_GRAD)
+  TOC_GRAD(1024, 1)
+  if constexpr (sizeof(T) == 4) {
+    TOC_GRAD(1024, 4)
+  }
 #undef TOC_GRAD
   return launched("norm_grad_kernel");
 }
 
 // Rows of partial dw sums a call leaves in its workspace.
-int64_t grad_parts(int64_t n, int32_t d) { return n ? blocks_for(n, shape_of(d), kGradBlocks) : 0; }
+template <typename T>
+int64_t grad_parts(int64_t n, int32_t d) {
+  return n ? grad_blocks(n, shape_of(chunks_of<T>(d), true)) : 0;
+}
+int64_t grad_parts(int64_t n, int32_t d, int32_t type) {
+  return type == TOC_F32 ? grad_parts<float>(n, d) : grad_parts<bf16>(n, d);
+}
 
 template <typename T>
 toc_status norm_typed(int64_t n, int32_t d, const void *X, int64_t ldx, const void *R, int64_t ldr,
@@ -457,7 +477,7 @@ toc_status toc_rmsnorm_grad_workspace_size(int64_t n, int32_t d, size_t *bytes) 
   clear_error();
   if (!bytes) return fail(TOC_EINVAL, "bytes is NULL");
   if (const toc_status st = check_norm(n, d, TOC_F32, nullptr, 1.0f)) return st;
-  *bytes = (size_t)grad_parts(n, d) * (size_t)d * 4;
+  *bytes = (size_t)std::max(grad_parts<float>(n, d), grad_parts<bf16>(n, d)) * (size_t)d * 4;
   return TOC_OK;
 }
 
@@ -477,7 +497,7 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
     return st;
   if ((uintptr_t)dw % 4) return fail(TOC_EINVAL, "dw is not aligned to its elements");
   if (dw) {
-    const size_t need = (size_t)grad_parts(n, d) * (size_t)d * 4;
+    const size_t need = (size_t)grad_parts(n, d, type) * (size_t)d * 4;
     if (need && !ws) return fail(TOC_EINVAL, "workspace is NULL");
     if (ws_bytes < need) return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, need);
     if ((uintptr_t)ws % 4) return fail(TOC_EINVAL, "workspace is not 4-byte aligned");
@@ -499,7 +519,7 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
   if (!dw) return TOC_OK;
   hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((d + kJoinCols - 1) / kJoinCols)),
                      dim3(kJoinCols * kJoinParts), 0, (hipStream_t)stream, part,
-                     (int)grad_parts(n, d), d, accumulate, dw);
+                     (int)grad_parts(n, d, type), d, accumulate, dw);
   return launched("norm_join_kernel");
 }
 
