@@ -680,7 +680,8 @@ typedef struct {
  *         0 .. n_vocab-1 (say -1, to pad) gives a row of zeros
  *   E     n_vocab x d    out   n x d    drop  host, or NULL
  * Asynchronous on stream.  TOC_EINVAL for NULL or misaligned pointers, strides
- * below d, unknown types or widths, a scale that is not finite, p outside 0..1. */
+ * below d, unknown types or widths, p outside 0..1, a scale that is not finite, also
+ * once multiplied by what the mask multiplies kept elements by. */
 toc_status toc_embed(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab, int32_t d,
                      int32_t type, const void *E, int64_t lde, float scale, const toc_drop *drop,
                      void *out, int64_t ldo, void *stream);

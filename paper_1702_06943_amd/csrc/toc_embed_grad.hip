@@ -238,8 +238,8 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
         for (int i = 0; i < N; ++i) acc[i] = 0.0f;
       }
       float v[N];
+      if (kDrop) drop<T>(in[u], (uint32_t)c, p[u], a.m);
       widen<T>(in[u], v);
-      if (kDrop) drop_cols(v, (uint32_t)c, p[u], a.m);
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] += v[i];
     }
@@ -368,15 +368,16 @@ toc_status grad(const Plan &p, int64_t n, const void *ids, int32_t id_bits, int6
   }
   if (id_bits == 32) sort_ids(p, n, (const int32_t *)ids, n_vocab, ws, s);
   else sort_ids(p, n, (const int64_t *)ids, n_vocab, ws, s);
+  const Mask m = mask_of(drop);
   const int last = (p.passes - 1) % 2;
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
-               (uint32_t)n_vocab, (uint32_t)p.chunk, (uint32_t)p.chunks, d, lanes_of(chunks_of<T>(d)), G, ldg, scale,
-               mask_of(drop), (float *)(ws + p.part), accumulate};
+               (uint32_t)n_vocab, (uint32_t)p.chunk, (uint32_t)p.chunks, d, lanes_of(chunks_of<T>(d)), G, ldg, scale * m.keep,
+               m, (float *)(ws + p.part), accumulate};
   const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
   const unsigned per = (unsigned)(kSumBlock / a.lanes);
   const dim3 grid((unsigned)((p.chunks + per - 1) / per), slices);
   if (!accumulate) zero_rows(n_vocab, d, ws + p.present, dE, lde, s);
-  if (a.m.thr)
+  if (a.m.on)
     hipLaunchKernelGGL((sum_kernel<T, TO, true>), grid, dim3(kSumBlock), 0, s, a, dE, lde);
   else
     hipLaunchKernelGGL((sum_kernel<T, TO, false>), grid, dim3(kSumBlock), 0, s, a, dE, lde);
@@ -436,7 +437,7 @@ toc_status toc_embed_grad(int64_t n, const void *ids, int32_t id_bits, int64_t n
   if ((st = check_rows("G", G, n, d, ldg, type_size(type))) ||
       (st = check_rows("dE", dE, n_vocab, d, lde, type_size(de_type))))
     return st;
-  if (!std::isfinite(scale)) return fail(TOC_EINVAL, "scale not finite");
+  if ((st = check_scale(scale, drop))) return st;
   const Plan p = plan_of(n, n_vocab, d);
   if (n > 0 && !ws) return fail(TOC_EINVAL, "workspace is NULL");
   if (n > 0 && ws_bytes < p.end) return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, p.end);

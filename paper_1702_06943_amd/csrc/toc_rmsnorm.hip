@@ -131,10 +131,9 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
       }
     }
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) widen<T>(in[k], h[k]);
-    if (kDrop) {
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) drop_cols(h[k], (uint32_t)(N * (lane + k * kLanes)), row, a.m);
+    for (int k = 0; k < kPer; ++k) {
+      if (kDrop) drop<T>(in[k], (uint32_t)(N * (lane + k * kLanes)), row, a.m);
+      widen<T>(in[k], h[k]);
     }
     if (a.R) {
 #pragma unroll
@@ -142,8 +141,13 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
         float v[N];
         widen<T>(rin[k], v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[k][i] += v[i];
+        for (int i = 0; i < N; ++i) h[k][i] = kDrop ? fmaf(h[k][i], a.m.keep, v[i]) : h[k][i] + v[i];
       }
+    } else if (kDrop) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[k][i] *= a.m.keep;
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
@@ -273,8 +277,13 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
       }
       if (a.dH) store(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k]);
       if (a.dX) {
-        if (kDrop) drop_cols(h[k], (uint32_t)c, row, a.m);
-        store(a.dX + (int64_t)row * a.lddx + c, a.d - c, h[k]);
+        if (kDrop) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) h[k][i] *= a.m.keep;
+        }
+        Chunk x = narrow<T>(h[k]);
+        if (kDrop) drop<T>(x, (uint32_t)c, row, a.m);
+        put(a.dX + (int64_t)row * a.lddx + c, a.d - c, x);
       }
     }
   }
@@ -366,7 +375,7 @@ toc_status norm(const NormArgs<T> &a, Y *y, hipStream_t s) {
   const dim3 grid((unsigned)norm_blocks(a.n, sh)), block((unsigned)std::max(sh.lanes, 256));
 #define TOC_NORM(L, K)                                                                     \
   if (sh.lanes == L && sh.per == K) {                                                      \
-    if (a.m.thr)                                                                           \
+    if (a.m.on)                                                                           \
       hipLaunchKernelGGL((norm_kernel<T, Y, L, K, true>), grid, block, 0, s, a, y);        \
     else                                                                                   \
       hipLaunchKernelGGL((norm_kernel<T, Y, L, K, false>), grid, block, 0, s, a, y);       \
@@ -386,7 +395,7 @@ toc_status norm_grad(const GradArgs<T> &a, hipStream_t s) {
   const dim3 grid((unsigned)grad_blocks(a.n, sh)), block((unsigned)std::max(sh.lanes, 256));
 #define TOC_GRAD(L, K)                                                                     \
   if (sh.lanes == L && sh.per == K) {                                                      \
-    if (a.m.thr)                                                                           \
+    if (a.m.on)                                                                           \
       hipLaunchKernelGGL((norm_grad_kernel<T, L, K, true>), grid, block, 0, s, a);         \
     else                                                                                   \
       hipLaunchKernelGGL((norm_grad_kernel<T, L, K, false>), grid, block, 0, s, a);        \

@@ -54,10 +54,10 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(const Id *__restrict__ ids
     if (o0 + (uint32_t)(k * kBlock) >= total) continue;
     const int c = (int)at[k] * kCols<T>;
     float v[kCols<T>];
+    if (kDrop) drop<T>(in[k], (uint32_t)c, row0 + row[k], m);
     widen<T>(in[k], v);
 #pragma unroll
     for (int i = 0; i < kCols<T>; ++i) v[i] *= scale;
-    if (kDrop) drop_cols(v, (uint32_t)c, row0 + row[k], m);
     store(out + (int64_t)row[k] * ldo + c, d - c, v);
   }
 }
@@ -67,6 +67,7 @@ template <typename T, typename Id>
 toc_status map_rows(int64_t n, int32_t d, const Id *ids, int64_t n_vocab, const T *src, int64_t lds,
                     float scale, const toc_drop *drop, T *out, int64_t ldo, hipStream_t s) {
   const Mask m = mask_of(drop);
+  scale *= m.keep;
   const uint32_t chunks = chunks_of<T>(d);
   const int64_t most = ((int64_t)1 << 30) / chunks;
   constexpr bool same = std::is_same<Id, Same>::value;
@@ -77,7 +78,7 @@ toc_status map_rows(int64_t n, int32_t d, const Id *ids, int64_t n_vocab, const 
     const Id *i = same ? ids : ids + r;
     const T *x = same ? src + r * lds : src;
     T *y = out + r * ldo;
-    if (m.thr)
+    if (m.on)
       hipLaunchKernelGGL((rows_kernel<T, Id, true>), grid, dim3(kBlock), 0, s, i, n_vocab, x, lds, scale,
                          m, (uint32_t)r, total, d, divisor(chunks), y, ldo);
     else
@@ -121,7 +122,7 @@ toc_status toc_embed(int64_t n, const void *ids, int32_t id_bits, int64_t n_voca
       (st = check_rows("E", E, n_vocab, d, lde, type_size(type))) ||
       (st = check_rows("out", out, n, d, ldo, type_size(type))))
     return st;
-  if (!std::isfinite(scale)) return fail(TOC_EINVAL, "scale not finite");
+  if ((st = check_scale(scale, drop))) return st;
   if (n == 0) return TOC_OK;
   if (id_bits == 32)
     return map_typed<int32_t>(type, n, d, ids, n_vocab, E, lde, scale, drop, out, ldo, stream);

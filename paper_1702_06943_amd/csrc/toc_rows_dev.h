@@ -23,23 +23,30 @@ inline bool type_ok(int32_t type) { return type == TOC_F32 || type == TOC_BF16 |
 inline int type_size(int32_t type) { return type == TOC_F32 ? 4 : 2; }
 
 // A dropout mask as the kernels take it.  An element is dropped when its 16-bit word is
-// below thr = round(65536 p): p is taken to the nearest 2^-16, and 65536 / (65536 - thr)
-// makes the kept elements' mean the input's exactly at that p.
+// below round(65536 p): p is taken to the nearest 2^-16, and 65536 / (65536 - that) makes the
+// kept elements' mean the input's exactly at that p.
 struct Mask {
   uint32_t k0, k1, s0, s1;   // seed (the key) and mask number, low word first
-  uint32_t thr;
-  float keep;                // what a kept element is multiplied by
+  uint32_t last;             // the largest word that drops
+  uint32_t limit;            // last in both halves, as signed numbers of the same order
+  float keep;                // what a kept element is multiplied by; 1 where `on` is not set
+  bool on;                   // whether any word drops
 };
 
 inline Mask mask_of(const toc_drop *drop) {
-  Mask m{0, 0, 0, 0, 0, 1.0f};
+  Mask m{};
+  m.keep = 1.0f;
   if (!drop) return m;
+  const uint32_t below = (uint32_t)std::lrint((double)drop->p * 65536.0);
+  if (below == 0) return m;
   m.k0 = (uint32_t)drop->seed;
   m.k1 = (uint32_t)(drop->seed >> 32);
   m.s0 = (uint32_t)drop->mask;
   m.s1 = (uint32_t)(drop->mask >> 32);
-  m.thr = (uint32_t)std::lrint((double)drop->p * 65536.0);
-  m.keep = m.thr < 65536u ? (float)(65536.0 / (65536.0 - (double)m.thr)) : 0.0f;
+  m.last = below - 1;
+  m.limit = (m.last ^ 0x8000u) * 0x10001u;
+  m.keep = below < 65536u ? (float)(65536.0 / (65536.0 - (double)below)) : 0.0f;
+  m.on = true;
   return m;
 }
 
@@ -55,6 +62,12 @@ inline toc_status check_rows(const char *name, const void *p, int64_t n, int32_t
 inline toc_status check_drop(const toc_drop *drop) {
   if (drop && !(drop->p >= 0.0f && drop->p <= 1.0f))
     return fail(TOC_EINVAL, "dropout probability outside 0..1");
+  return TOC_OK;
+}
+
+// The scale and the kept elements' factor are one product.
+inline toc_status check_scale(float scale, const toc_drop *drop) {
+  if (!std::isfinite(scale * mask_of(drop).keep)) return fail(TOC_EINVAL, "scale, times the mask's factor, not finite");
   return TOC_OK;
 }
 
@@ -176,32 +189,42 @@ __device__ inline void load(const T *p, int left, float (&v)[N]) {
   }
 }
 
+template <typename T>
+__device__ inline Chunk narrow(const float *v) {
+  typedef float Two __attribute__((ext_vector_type(2)));
+  Chunk c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      c.w[i] = __float_as_uint(v[i]);
+    } else {
+      typedef T TwoT __attribute__((ext_vector_type(2)));
+      const Two x = {v[2 * i], v[2 * i + 1]};
+      c.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, TwoT));
+    }
+  }
+  return c;
+}
+
+template <typename T>
+__device__ inline void put(T *p, int left, const Chunk &c) {
+  if (left >= kCols<T>) {
+    const Words4 x = {c.w[0], c.w[1], c.w[2], c.w[3]};
+    __builtin_nontemporal_store(x, (Words4 *)p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kCols<T> - 1; ++i) {
+      if (i >= left) continue;
+      if (sizeof(T) == 4) ((uint32_t *)p)[i] = c.w[i];
+      else ((uint16_t *)p)[i] = (uint16_t)(c.w[i / 2] >> (16 * (i % 2)));
+    }
+  }
+}
+
 template <typename T, int N>
 __device__ inline void store(T *p, int left, const float (&v)[N]) {
 #pragma unroll
-  for (int j = 0; j < N; j += kCols<T>) {
-    Chunk c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        c.w[i] = __float_as_uint(v[j + i]);
-      } else {
-        const T lo = (T)v[j + 2 * i], hi = (T)v[j + 2 * i + 1];
-        c.w[i] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
-      }
-    }
-    if (left - j >= kCols<T>) {
-      const Words4 x = {c.w[0], c.w[1], c.w[2], c.w[3]};
-      __builtin_nontemporal_store(x, (Words4 *)(p + j));
-    } else {
-#pragma unroll
-      for (int i = 0; i < kCols<T> - 1; ++i) {
-        if (i >= left - j) continue;
-        if (sizeof(T) == 4) ((uint32_t *)(p + j))[i] = c.w[i];
-        else ((uint16_t *)(p + j))[i] = (uint16_t)(c.w[i / 2] >> (16 * (i % 2)));
-      }
-    }
-  }
+  for (int j = 0; j < N; j += kCols<T>) put(p + j, left - j, narrow<T>(v + j));
 }
 
 struct E4m3 {
@@ -252,20 +275,31 @@ __device__ inline uint4 philox(uint32_t eight, uint32_t row, const Mask &m) {
   return make_uint4(c0, c1, c2, c3);
 }
 
-// v = kept ? v * keep : 0 for the N columns from c (a multiple of N) on, selected and not
-// multiplied: a dropped infinity or NaN is 0.  Four columns take half of a block's words.
-template <int N>
-__device__ inline void drop_cols(float (&v)[N], uint32_t c, uint32_t row, const Mask &m) {
+// Clears the dropped elements of the chunk of row `row` from column c on: cleared and not
+// multiplied by 0, so a dropped infinity or NaN is 0.  The caller multiplies by m.keep.  Two
+// bytes an element: word i of the block holds the words of the elements in word i of the
+// chunk, compared two at a time by the sign of a saturated 16-bit difference.  Four: half of
+// the block's words are the chunk's.
+template <typename T>
+__device__ inline void drop(Chunk &x, uint32_t c, uint32_t row, const Mask &m) {
   const uint4 w = philox(c / 8, row, m);
-  uint32_t u[4] = {w.x, w.y, w.z, w.w};
-  if (N == 4 && (c & 4u)) {
-    u[0] = u[2];
-    u[1] = u[3];
-  }
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (sizeof(T) == 4) {
+    const bool high = c & 4u;
+    const uint32_t lo = high ? u[2] : u[0], hi = high ? u[3] : u[1];
+    x.w[0] = (lo & 0xffffu) > m.last ? x.w[0] : 0u;
+    x.w[1] = (lo >> 16) > m.last ? x.w[1] : 0u;
+    x.w[2] = (hi & 0xffffu) > m.last ? x.w[2] : 0u;
+    x.w[3] = (hi >> 16) > m.last ? x.w[3] : 0u;
+  } else {
+    typedef int16_t Two __attribute__((ext_vector_type(2)));
+    const Two limit = __builtin_bit_cast(Two, m.limit);
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    v[2 * i] = (u[i] & 0xffffu) >= m.thr ? v[2 * i] * m.keep : 0.0f;
-    v[2 * i + 1] = (u[i] >> 16) >= m.thr ? v[2 * i + 1] * m.keep : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+      const Two word = __builtin_bit_cast(Two, u[i] ^ 0x80008000u);
+      const Two kept = __builtin_elementwise_sub_sat(limit, word) >> 15;
+      x.w[i] &= __builtin_bit_cast(uint32_t, kept);
+    }
   }
 }
 
