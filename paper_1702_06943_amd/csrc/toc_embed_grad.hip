@@ -1,15 +1,17 @@
 // Gradient of the embedding lookup by sorted token numbers:
 //   dE[v, :] (+)= scale * sum of drop(G)[t, :] over the tokens t with ids[t] = v
 // the left product G^T.A (Theorem 2) of tuples that hold one pair each, in a fixed order:
-//   sort   (number, token) pairs stably by number, 9 bits or fewer a pass: each tile's count
-//          of every digit (count_kernel), then each tile places its pairs (scatter_kernel);
-//          numbers outside the table sort last, as number V
-//   sum    the sorted list cut into chunks of equal length, so that a frequent number costs
-//          no more than others: a group of lanes walks a chunk, its chunks of dE's row in
-//          registers, and writes a row when its number ends.  A number that crosses chunks
-//          leaves one partial row in each
-//   join   partial rows added in the chunks' order
-//   zero   rows of numbers that do not occur (unless accumulating)
+//   sort   (number, token) pairs stably by number, 9 bits or fewer a pass; numbers outside
+//          the table sort last, as number V.  Up to 4,096 pairs in one workgroup's LDS, else
+//          in tiles: each tile's count of every digit, then each tile places its pairs
+//   sum    the sorted list cut into spans of equal length, so that a frequent number costs
+//          no more than others: a group of lanes walks a span, its chunk of dE's row in
+//          registers, and writes a row when its number ends.  A number that crosses spans
+//          of one workgroup is put together in LDS, one that crosses workgroups leaves a
+//          partial row in each
+//   join   partial rows added in order
+//   zero   rows of numbers that do not occur (unless accumulating), by workgroups of the
+//          sort's and the sums' launches: the sort leaves most of the chip idle
 // Bound by memory: G is read once and every row of dE written once.
 #include "toc_rows_dev.h"
 
@@ -19,22 +21,52 @@ namespace {
 
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / 64;
 constexpr int kMaxBits = 9;                  // digit bits a pass
-constexpr int64_t kMaxTiles = 256;
-constexpr int kSumBlock = 256;
+constexpr int kMaxDigits = 1 << kMaxBits;
+constexpr int kTileKeys = 2;                 // pairs of a thread, in registers
+constexpr uint32_t kTile = kTileKeys * kSortBlock;
+constexpr int kSmallKeys = 4;
+constexpr uint32_t kSmall = kSmallKeys * kSortBlock;
+constexpr uint32_t kFewTiles = 64;           // above, the tiles' counts are summed by scan_kernel
+constexpr int kSumBlock = 512;
+constexpr uint32_t kSpan = 16;               // entries of a span
 constexpr int kAhead = 8;                    // entries whose rows' loads fly together
-constexpr int kZeroBlock = 256, kZeroPer = 4;
+constexpr int kJoinBlock = 256;
+constexpr int kZeroPer = 4;                  // chunks a thread of the zero workgroups writes
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr int32_t kMaxGradCols = 1 << 20;
 
-// The sort's shape, the chunks and where the workspace's parts lie (bytes).
+// The sort's shape, and where the workspace's parts lie (bytes).
 struct Plan {
   int bits, passes;       // digit bits of a pass
-  int64_t tile, tiles;    // entries of a tile
-  int64_t chunk, chunks;  // entries of a chunk
-  size_t key[2], pos[2], count, present, part, end;
+  bool small;
+  uint32_t tiles;
+  size_t key[2], pos[2], count, total, slot, part, end;
 };
 
 size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
+
+// Lanes that walk a span, a power of two of a wave at most: the most lanes of which a row's
+// chunks leave no more than a sixth idle, or else those that leave the fewest.
+int lanes_of(uint32_t chunks) {
+  int best = 64;
+  uint32_t best_used = 0;                    // of 64ths, rounded
+  for (int lanes = 64; lanes >= 8; lanes /= 2) {
+    const uint32_t room = (chunks + lanes - 1) / lanes * lanes;
+    const uint32_t used = (uint32_t)((uint64_t)chunks * 60 / room);
+    if (used >= 50) return lanes;
+    if (used > best_used) {
+      best_used = used;
+      best = lanes;
+    }
+  }
+  return best;
+}
+
+// Entries of the sorted list that a workgroup of sum_kernel walks.
+template <typename T>
+uint32_t block_span(int32_t d) {
+  return (uint32_t)(kSumBlock / lanes_of(chunks_of<T>(d))) * kSpan;
+}
 
 Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   Plan p{};
@@ -42,11 +74,10 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   while (width < 32 && ((int64_t)1 << width) <= n_vocab) ++width;
   p.passes = (width + kMaxBits - 1) / kMaxBits;
   p.bits = (width + p.passes - 1) / p.passes;
-  p.tiles = std::max<int64_t>(1, std::min(kMaxTiles, (n + 2047) / 2048));
-  p.tile = ((n + p.tiles - 1) / p.tiles + kSortBlock - 1) / kSortBlock * kSortBlock;
-  p.chunk = std::max<int64_t>(16, std::min<int64_t>((n + 4095) / 4096, 64));
-  p.chunk = std::max(p.chunk, (n + (1 << 22) - 1) >> 22);
-  p.chunks = (n + p.chunk - 1) / p.chunk;
+  p.small = n <= (int64_t)kSmall;
+  p.tiles = p.small ? 0 : (uint32_t)((n + kTile - 1) / kTile);
+  const int64_t least = std::min(block_span<float>(d), block_span<bf16>(d));
+  const int64_t blocks = (n + least - 1) / least;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -54,12 +85,14 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
     return here;
   };
   for (int i = 0; i < 2; ++i) {
-    p.key[i] = take((size_t)n * 4);
-    p.pos[i] = take((size_t)n * 4);
+    // (a small sort keeps all passes but the last in LDS)
+    p.key[i] = i == 0 || !p.small ? take((size_t)n * 4) : p.key[0];
+    p.pos[i] = i == 0 || !p.small ? take((size_t)n * 4) : p.pos[0];
   }
-  p.count = take((size_t)p.tiles << (p.bits + 2));
-  p.present = take((size_t)n_vocab);
-  p.part = take((size_t)p.chunks * 2 * (size_t)d * 4);
+  p.count = take(((size_t)p.tiles << p.bits) * 4);
+  p.total = take(p.tiles > kFewTiles ? (size_t)4 << p.bits : 0);
+  p.slot = take(p.small ? 0 : (size_t)n_vocab * 4);
+  p.part = take(blocks > 1 ? (size_t)blocks * 2 * (size_t)d * 4 : 0);
   p.end = at;
   return p;
 }
@@ -71,115 +104,293 @@ __device__ inline uint32_t key_at(const Id *ids, uint32_t i, uint32_t n_vocab) {
 }
 __device__ inline uint32_t key_at(const uint32_t *keys, uint32_t i, uint32_t) { return keys[i]; }
 
-// Workgroups 0..tiles-1: the tile's count of each digit.  The others (first pass only) clear
-// `present`, which the first scatter fills.
-template <typename Id>
-__global__ __launch_bounds__(kSortBlock) void count_kernel(const Id *__restrict__ ids, uint32_t n,
-                                                           uint32_t n_vocab, uint32_t tile,
-                                                           uint32_t tiles, int shift, int bits,
-                                                           uint32_t *__restrict__ count,
-                                                           uint8_t *__restrict__ present) {
-  __shared__ uint32_t c[1 << kMaxBits];
-  if (blockIdx.x >= tiles) {
-    // (the workspace keeps `present` 16-byte aligned and rounded up)
-    const uint32_t words = (n_vocab + 3u) / 4u;
-    for (uint32_t i = (blockIdx.x - tiles) * kSortBlock + threadIdx.x; i < words;
-         i += (gridDim.x - tiles) * kSortBlock)
-      ((uint32_t *)present)[i] = 0u;
-    return;
+// --- zero ----------------------------------------------------------------------
+
+// Chunks first .. first + count - 1 of dE, counted row by row.  ids NULL: all of them are
+// written.  Else those of rows whose number does not occur: count_kernel left in slot[v] some
+// token of number v if there is one, and whatever else a slot holds is no such token, since
+// the token's own number is looked up again (so the slots need no clearing).
+template <typename TO, typename Id>
+struct ZeroArgs {
+  TO *dE;
+  int64_t lde;
+  int d;
+  Divisor chunks;
+  const uint32_t *slot;
+  const Id *ids;
+  uint32_t n, n_vocab;
+  int64_t row0;            // the row of chunk 0
+  uint32_t first, count;
+};
+
+template <int kBlock, typename TO, typename Id>
+__device__ inline void zero_rows(const ZeroArgs<TO, Id> &z, uint32_t block) {
+  const Chunk zero = {{0u, 0u, 0u, 0u}};
+  const uint32_t o0 = block * (uint32_t)(kBlock * kZeroPer) + threadIdx.x;
+  uint32_t row[kZeroPer], at[kZeroPer], t[kZeroPer];
+#pragma unroll
+  for (int k = 0; k < kZeroPer; ++k) {
+    const uint32_t o = o0 + (uint32_t)(k * kBlock);
+    row[k] = divide(z.first + (o < z.count ? o : 0u), z.chunks, &at[k]);
+    t[k] = z.ids ? z.slot[z.row0 + row[k]] : kNone;
   }
-  const uint32_t digits = 1u << bits;
-  for (uint32_t i = threadIdx.x; i < digits; i += kSortBlock) c[i] = 0u;
-  __syncthreads();
-  const uint32_t end = min(n, (blockIdx.x + 1) * tile);
-  for (uint32_t i = blockIdx.x * tile + threadIdx.x; i < end; i += kSortBlock)
-    atomicAdd(&c[key_at(ids, i, n_vocab) >> shift & (digits - 1)], 1u);
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < digits; i += kSortBlock)
-    count[(size_t)blockIdx.x * digits + i] = c[i];
+#pragma unroll
+  for (int k = 0; k < kZeroPer; ++k) {
+    if (o0 + (uint32_t)(k * kBlock) >= z.count) return;
+    if (t[k] < z.n && (int64_t)key_at(z.ids, t[k], z.n_vocab) == z.row0 + row[k]) continue;
+    const int c = (int)at[k] * kCols<TO>;
+    put(z.dE + (z.row0 + row[k]) * z.lde + c, z.d - c, zero);
+  }
 }
 
-// Places a tile's entries.  A digit's entries of this tile start after all entries of lower
-// digits and this digit's of earlier tiles; inside the tile each wave owns a run of entries,
-// and a wave's 64 entries are ranked by comparing digits across its lanes, so equal digits
-// keep their order.
-template <typename Id, bool kFirst>
-__global__ __launch_bounds__(kSortBlock) void scatter_kernel(
-    const Id *__restrict__ ids, const uint32_t *__restrict__ pos, uint32_t n, uint32_t n_vocab,
-    uint32_t tile, uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
-    uint32_t *__restrict__ key_out, uint32_t *__restrict__ pos_out, uint8_t *__restrict__ present) {
-  __shared__ uint32_t at[kSortWaves][1 << kMaxBits];
-  __shared__ uint32_t wave_sum[kSortWaves];
-  const uint32_t digits = 1u << bits;
-  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  for (uint32_t i = threadIdx.x; i < kSortWaves * (1u << kMaxBits); i += kSortBlock) (&at[0][0])[i] = 0u;
-  uint32_t before = 0, total = 0;
-  if (threadIdx.x < digits) {
-#pragma unroll 8
-    for (uint32_t t = 0; t < tiles; ++t) {
-      const uint32_t x = count[(size_t)t * digits + threadIdx.x];
-      before += t < blockIdx.x ? x : 0u;
-      total += x;
-    }
-  }
-  uint32_t incl = total;
+template <int kBlock>
+uint32_t zero_blocks(uint32_t count) { return (count + kBlock * kZeroPer - 1) / (kBlock * kZeroPer); }
+
+template <typename TO, typename Id>
+__global__ __launch_bounds__(256) void zero_kernel(ZeroArgs<TO, Id> z) {
+  zero_rows<256>(z, blockIdx.x);
+}
+
+// --- sort ------------------------------------------------------------------------
+
+// Exclusive sums of x over the first `digits` threads (a multiple of 64, or fewer than 64);
+// lds: a word per wave.
+__device__ inline uint32_t digits_before(uint32_t x, uint32_t *lds) {
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint32_t incl = x;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t x = __shfl_up(incl, o, 64);
-    if ((int)lane >= o) incl += x;
+    const uint32_t y = __shfl_up(incl, o, 64);
+    if ((int)lane >= o) incl += y;
   }
-  if (lane == 63) wave_sum[wave] = incl;
+  if (lane == 63) lds[wave] = incl;
   __syncthreads();
-  uint32_t base = incl - total + before;
-  for (uint32_t w = 0; w < wave; ++w) base += wave_sum[w];
-  const uint32_t per = tile / kSortWaves;
-  const uint64_t first = (uint64_t)blockIdx.x * tile + (uint64_t)wave * per;
-  const uint32_t i0 = (uint32_t)min(first, (uint64_t)n), i1 = (uint32_t)min(first + per, (uint64_t)n);
-  for (uint32_t i = i0 + lane; i < i1; i += 64)
-    atomicAdd(&at[wave][key_at(ids, i, n_vocab) >> shift & (digits - 1)], 1u);
-  __syncthreads();
-  if (threadIdx.x < digits) {
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t x = at[w][threadIdx.x];
-      at[w][threadIdx.x] = base;
-      base += x;
-    }
-  }
-  __syncthreads();
-  for (uint32_t s = i0; s < i1; s += 64) {
-    const uint32_t i = s + lane;
-    const bool in = i < i1;
-    const uint32_t key = in ? key_at(ids, i, n_vocab) : 0u;
-    const uint32_t digit = key >> shift & (digits - 1);
-    uint64_t same = __ballot(in);
+  uint32_t base = incl - x;
+  for (uint32_t w = 0; w < wave && w < kMaxDigits / 64; ++w) base += lds[w];
+  return base;
+}
+
+// For each of a wave's K * 64 entries, in their order, how many before it have its digit;
+// at: the wave's count of each digit, 0 before and the wave's counts after.  64 entries are
+// compared across the lanes, a ballot a bit.
+template <int K>
+__device__ inline void wave_ranks(const uint32_t (&digit)[K], const bool (&in)[K], int bits,
+                                  uint16_t *at, uint32_t (&rank)[K]) {
+  const uint64_t below = ((uint64_t)1 << (threadIdx.x % 64)) - 1;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    uint64_t same = __ballot(in[k]);
     for (int b = 0; b < bits; ++b) {
-      const uint64_t ones = __ballot(digit >> b & 1u);
-      same &= digit >> b & 1u ? ones : ~ones;
+      const uint64_t ones = __ballot(digit[k] >> b & 1u);
+      same &= digit[k] >> b & 1u ? ones : ~ones;
     }
-    const uint32_t rank = (uint32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
-    if (in) {
-      const uint32_t to = at[wave][digit] + rank;
-      key_out[to] = key;
-      pos_out[to] = kFirst ? i : pos[i];
-      if (kFirst && key < n_vocab) present[key] = 1;
-    }
-    // all lanes have read their digit's place before its first entry's lane moves it on
+    rank[k] = in[k] ? at[digit[k]] + (uint32_t)__popcll(same & below) : 0u;
+    // every lane has its digit's count before the digit's first lane moves it on
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (in && rank == 0) at[wave][digit] += (uint32_t)__popcll(same);
+    if (in[k] && !(same & below)) at[digit[k]] += (uint16_t)__popcll(same);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
+
+// The waves' counts of digit threadIdx.x become the counts of the waves before; returns all.
+__device__ inline uint32_t waves_before(uint16_t (*at)[kMaxDigits]) {
+  uint32_t run = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    const uint32_t x = at[w][threadIdx.x];
+    at[w][threadIdx.x] = (uint16_t)run;
+    run += x;
+  }
+  return run;
+}
+
+// Workgroup 0: all passes over n <= kSmall pairs in LDS.  The others write zeros to all of dE
+// (rows of numbers that occur are written later): they end with the sort, or soon after.
+template <typename TO, typename Id>
+__global__ __launch_bounds__(kSortBlock) void small_kernel(const Id *__restrict__ ids, uint32_t n,
+                                                           uint32_t n_vocab, int bits, int passes,
+                                                           uint32_t *__restrict__ key_out,
+                                                           uint32_t *__restrict__ pos_out,
+                                                           ZeroArgs<TO, Id> z) {
+  __shared__ uint16_t at[kSortWaves][kMaxDigits];
+  __shared__ uint32_t base[kMaxDigits], sums[kSortWaves];
+  __shared__ uint32_t keys[kSmall];
+  __shared__ uint16_t from[kSmall];
+  if (blockIdx.x > 0) {
+    zero_rows<kSortBlock>(z, blockIdx.x - 1);
+    return;
+  }
+  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, digits = 1u << bits;
+  // a wave's entries; few enough are spread over all waves
+  const uint32_t per = (n + kSortWaves * 64 - 1) / (kSortWaves * 64);
+  uint32_t key[kSmallKeys], pos[kSmallKeys], digit[kSmallKeys], rank[kSmallKeys], i[kSmallKeys];
+  bool in[kSmallKeys];
+#pragma unroll
+  for (int k = 0; k < kSmallKeys; ++k) {
+    i[k] = (wave * per + k) * 64 + lane;
+    in[k] = (uint32_t)k < per && i[k] < n;
+    key[k] = in[k] ? key_at(ids, i[k], n_vocab) : 0u;
+    pos[k] = i[k];
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    for (uint32_t j = threadIdx.x; j < kSortWaves * kMaxDigits; j += kSortBlock) (&at[0][0])[j] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallKeys; ++k) digit[k] = key[k] >> (pass * bits) & (digits - 1);
+    wave_ranks(digit, in, bits, at[wave], rank);
+    __syncthreads();
+    const uint32_t count = threadIdx.x < digits ? waves_before(at) : 0u;
+    const uint32_t before = digits_before(count, sums);
+    if (threadIdx.x < digits) base[threadIdx.x] = before;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallKeys; ++k) {
+      if (!in[k]) continue;
+      const uint32_t to = base[digit[k]] + at[wave][digit[k]] + rank[k];
+      if (pass + 1 == passes) {
+        key_out[to] = key[k];
+        pos_out[to] = pos[k];
+      } else {
+        keys[to] = key[k];
+        from[to] = (uint16_t)pos[k];
+      }
+    }
+    if (pass + 1 == passes) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSmallKeys; ++k) {
+      if (!in[k]) continue;
+      key[k] = keys[i[k]];
+      pos[k] = from[i[k]];
+    }
+  }
+}
+
+// The tile's count of each digit; in the first pass also a token of each number (slot, or
+// NULL when accumulating).
+template <typename Id>
+__global__ __launch_bounds__(kSortBlock) void count_kernel(const Id *__restrict__ ids, uint32_t n,
+                                                           uint32_t n_vocab, int shift, int bits,
+                                                           uint32_t *__restrict__ count,
+                                                           uint32_t *__restrict__ slot) {
+  __shared__ uint32_t c[kMaxDigits];
+  const uint32_t digits = 1u << bits;
+  if (threadIdx.x < digits) c[threadIdx.x] = 0u;
+  uint32_t key[kTileKeys];
+#pragma unroll
+  for (int k = 0; k < kTileKeys; ++k) {
+    const uint32_t i = blockIdx.x * kTile + k * kSortBlock + threadIdx.x;
+    key[k] = i < n ? key_at(ids, i, n_vocab) : kNone;
+    if (slot && key[k] < n_vocab) slot[key[k]] = i;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kTileKeys; ++k)
+    if (key[k] != kNone) atomicAdd(&c[key[k] >> shift & (digits - 1)], 1u);
+  __syncthreads();
+  if (threadIdx.x < digits) count[(size_t)blockIdx.x * digits + threadIdx.x] = c[threadIdx.x];
+}
+
+// Digit blockIdx.x: its tiles' counts become the counts of the tiles before; total: of all.
+__global__ __launch_bounds__(256) void scan_kernel(uint32_t *__restrict__ count, uint32_t tiles, int bits,
+                                                   uint32_t *__restrict__ total) {
+  __shared__ uint32_t sums[kSortWaves];
+  uint32_t carry = 0;
+  for (uint32_t t0 = 0; t0 < tiles; t0 += 256) {
+    const uint32_t t = t0 + threadIdx.x;
+    const size_t at = ((size_t)t << bits) + blockIdx.x;
+    const uint32_t x = t < tiles ? count[at] : 0u;
+    const uint32_t before = digits_before(x, sums);
+    if (t < tiles) count[at] = carry + before;
+    const uint32_t all = sums[0] + sums[1] + sums[2] + sums[3];
+    __syncthreads();                         // sums are free again
+    carry += all;
+  }
+  if (threadIdx.x == 0) total[blockIdx.x] = carry;
+}
+
+// Workgroups 0 .. tiles-1 place a tile's pairs: a digit's pairs of the tile come after all
+// pairs of lower digits and the digit's of earlier tiles, waves and lanes.  total: NULL, or
+// scan_kernel's, and count then holds the counts before.  The other workgroups write zeros.
+template <typename TO, typename Id, typename Key, bool kFirst>
+__global__ __launch_bounds__(kSortBlock) void scatter_kernel(
+    const Key *__restrict__ ids, const uint32_t *__restrict__ pos, uint32_t n, uint32_t n_vocab,
+    uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
+    const uint32_t *__restrict__ total, uint32_t *__restrict__ key_out, uint32_t *__restrict__ pos_out,
+    ZeroArgs<TO, Id> z) {
+  __shared__ uint16_t at[kSortWaves][kMaxDigits];
+  __shared__ uint32_t base[kMaxDigits], sums[kSortWaves];
+  __shared__ uint32_t before[kSortBlock], all[kSortBlock];
+  if (blockIdx.x >= tiles) {
+    zero_rows<kSortBlock>(z, blockIdx.x - tiles);
+    return;
+  }
+  const uint32_t digits = 1u << bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  uint32_t key[kTileKeys], from[kTileKeys], digit[kTileKeys], rank[kTileKeys];
+  bool in[kTileKeys];
+#pragma unroll
+  for (int k = 0; k < kTileKeys; ++k) {
+    const uint32_t i = blockIdx.x * kTile + (wave * kTileKeys + k) * 64 + lane;
+    in[k] = i < n;
+    key[k] = in[k] ? key_at(ids, i, n_vocab) : 0u;
+    from[k] = kFirst || !in[k] ? i : pos[i];
+    digit[k] = key[k] >> shift & (digits - 1);
+  }
+  uint32_t b = 0, a = 0;
+  if (total) {
+    if (threadIdx.x < digits) {
+      b = count[(size_t)blockIdx.x * digits + threadIdx.x];
+      a = total[threadIdx.x];
+    }
+  } else {
+    // the counts of a digit split over kSortBlock / digits threads
+    const uint32_t d = threadIdx.x & (digits - 1), parts = kSortBlock >> bits;
+#pragma unroll 8
+    for (uint32_t t = threadIdx.x >> bits; t < tiles; t += parts) {
+      const uint32_t x = count[(size_t)t * digits + d];
+      b += t < blockIdx.x ? x : 0u;
+      a += x;
+    }
+    before[threadIdx.x] = b;
+    all[threadIdx.x] = a;
+  }
+  for (uint32_t j = threadIdx.x; j < kSortWaves * kMaxDigits; j += kSortBlock) (&at[0][0])[j] = 0;
+  __syncthreads();
+  if (!total && threadIdx.x < digits) {
+    b = a = 0;
+    for (uint32_t j = threadIdx.x; j < kSortBlock; j += digits) {
+      b += before[j];
+      a += all[j];
+    }
+  }
+  wave_ranks(digit, in, bits, at[wave], rank);
+  const uint32_t lower = digits_before(threadIdx.x < digits ? a : 0u, sums);   // (a barrier)
+  if (threadIdx.x < digits) {
+    waves_before(at);
+    base[threadIdx.x] = lower + b;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kTileKeys; ++k) {
+    if (!in[k]) continue;
+    const uint32_t to = base[digit[k]] + at[wave][digit[k]] + rank[k];
+    key_out[to] = key[k];
+    pos_out[to] = from[k];
+  }
+}
+
+// --- sums --------------------------------------------------------------------------
 
 template <typename T>
 struct SumArgs {
   const uint32_t *key, *pos;
-  uint32_t n, n_vocab, chunk, chunks;
-  int d, lanes;
+  uint32_t n, n_vocab, blocks;   // workgroups along the list
+  int d, lanes, shift;           // lanes = 1 << shift
   const T *G;
   int64_t ldg;
   float scale;
   Mask m;
-  float *part;
+  float *part;                   // two rows a workgroup: its first number's, its last number's
   int accumulate;
 };
 
@@ -196,90 +407,134 @@ __device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, in
   store(p, left, v);
 }
 
-// Chunk blockIdx.x * (256 / lanes) + group, columns from kCols lanes blockIdx.y.
-template <typename T, typename TO, bool kDrop>
-__global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde) {
-  const uint32_t chunk = blockIdx.x * (uint32_t)(kSumBlock / a.lanes) + threadIdx.x / a.lanes;
+// Workgroups 0 .. a.blocks-1 of a slice (blockIdx.y) of `lanes` chunks of the columns: group g
+// walks entries (blockIdx.x groups + g) kSpan onwards.  The others write zeros.
+template <typename T, typename TO, typename Id, bool kDrop>
+__global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde,
+                                                        ZeroArgs<TO, Id> z) {
   constexpr int N = kCols<T>;
-  const int c = (int)(blockIdx.y * a.lanes + threadIdx.x % a.lanes) * N, left = a.d - c;
-  if (chunk >= a.chunks || left <= 0) return;
-  const uint32_t e0 = chunk * a.chunk, e1 = min(a.n, e0 + a.chunk);
-  const uint32_t after = e1 < a.n ? a.key[e1] : kNone;
-  uint32_t cur = a.key[e0];
-  bool from_before = e0 > 0 && a.key[e0 - 1] == cur;
+  __shared__ float heads[kSumBlock][N];          // each group's part of a number from before
+  __shared__ uint8_t through[kSumBlock / 8];     // ... which goes on after the group
+  if (blockIdx.x >= a.blocks) {
+    zero_rows<kSumBlock>(z, (blockIdx.x - a.blocks) * gridDim.y + blockIdx.y);
+    return;
+  }
+  const uint32_t groups = kSumBlock >> a.shift, group = threadIdx.x >> a.shift;
+  const int lane = threadIdx.x & (a.lanes - 1);
+  const int c = (int)(blockIdx.y * a.lanes + lane) * N, left = a.d - c;
+  const uint64_t first = ((uint64_t)blockIdx.x * groups + group) * kSpan;
+  const uint32_t e0 = (uint32_t)min(first, (uint64_t)a.n), e1 = min(a.n, e0 + kSpan);
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-  auto flush = [&](bool goes_on) {
-    if (cur >= a.n_vocab) return;
-    if (from_before || goes_on)
-      store(a.part + ((int64_t)chunk * 2 + (from_before ? 0 : 1)) * a.d + c, left, acc);
-    else
-      write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
-  };
-  for (uint32_t e = e0; e < e1; e += kAhead) {
-    uint32_t k[kAhead], p[kAhead];
-    Chunk in[kAhead];
+  uint32_t cur = kNone;
+  bool from_before = false, goes_on = false;
+  if (e0 < e1) {
+    cur = a.key[e0];
+    from_before = e0 > 0 && a.key[e0 - 1] == cur;
+    for (uint32_t e = e0; e < e1; e += kAhead) {
+      uint32_t k[kAhead], p[kAhead];
+      Chunk in[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      k[u] = e + u < e1 ? a.key[e + u] : kNone;
-      p[u] = e + u < e1 ? a.pos[e + u] : 0u;
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) in[u] = fetch(a.G + (int64_t)p[u] * a.ldg + c, k[u] < a.n_vocab ? left : 0);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (e + u >= e1) break;
-      if (k[u] != cur) {
-        flush(false);
-        cur = k[u];
-        from_before = false;
-#pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+      for (int u = 0; u < kAhead; ++u) {
+        k[u] = a.key[min(e + u, e1 - 1)];
+        p[u] = a.pos[min(e + u, e1 - 1)];
       }
-      float v[N];
-      if (kDrop) drop<T>(in[u], (uint32_t)c, p[u], a.m);
-      widen<T>(in[u], v);
 #pragma unroll
-      for (int i = 0; i < N; ++i) acc[i] += v[i];
+      for (int u = 0; u < kAhead; ++u) in[u] = fetch(a.G + (int64_t)p[u] * a.ldg + c, left);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (e + u >= e1) break;
+        if (k[u] != cur) {
+          if (from_before) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
+          } else if (left > 0) {                 // (cur < V: a larger number sorts after it)
+            write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+          }
+          cur = k[u];
+          from_before = false;
+#pragma unroll
+          for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+        }
+        float v[N];
+        if (kDrop) drop<T>(in[u], (uint32_t)c, p[u], a.m);
+        widen<T>(in[u], v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] += v[i];
+      }
+    }
+    goes_on = e1 < a.n && a.key[e1] == cur;
+    if (from_before) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
+    } else if (!goes_on && cur < a.n_vocab && left > 0) {
+      write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
     }
   }
-  flush(after == cur);
+  if (lane == 0) through[group] = from_before && goes_on;
+  __syncthreads();
+  if (left <= 0 || e0 >= e1) return;
+  // A group whose last number begins in it and goes on adds the parts of the groups that
+  // follow; group 0 does so for a number from before the workgroup.
+  const bool at_start = group == 0 && e0 > 0 && a.key[e0 - 1] == a.key[e0];
+  if (at_start) {
+    const uint32_t key = a.key[e0];
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = heads[threadIdx.x][i];
+    for (uint32_t g = 0; g + 1 < groups && through[g]; ++g)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += heads[(g + 1) * a.lanes + lane][i];
+    if (key < a.n_vocab) store(a.part + (int64_t)blockIdx.x * 2 * a.d + c, left, v);
+  }
+  if (goes_on && !from_before && cur < a.n_vocab) {
+    uint32_t g = group + 1;
+    bool open = true;                            // whether the number reaches group g
+    for (; g < groups && open; ++g) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] += heads[g * a.lanes + lane][i];
+      open = through[g];
+    }
+    if (open) store(a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d + c, left, acc);
+    else write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+  }
 }
 
-// The row of a number that begins in chunk blockIdx.x and goes on in later ones: its part at
-// that chunk's end, then those at the next chunks' starts, their sum split over the
-// workgroup's groups of lanes.
+// The row of a number that begins in workgroup blockIdx.x's entries and goes on after them: its
+// part there, then those of the workgroups that follow, split over this one's groups of lanes.
 template <typename T, typename TO>
-__global__ __launch_bounds__(kSumBlock) void join_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde) {
+__global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t span,
+                                                          TO *__restrict__ dE, int64_t lde) {
   constexpr int N = kCols<T>;
-  __shared__ float sums[kSumBlock][N];
-  const uint32_t chunk = blockIdx.x;
-  const uint32_t e0 = chunk * a.chunk, e1 = min(a.n, e0 + a.chunk);
-  if (e1 >= a.n) return;
-  const uint32_t key = a.key[e1 - 1];
-  if (key >= a.n_vocab || a.key[e1] != key) return;
-  if (a.key[e0] == key && e0 > 0 && a.key[e0 - 1] == key) return;   // it began earlier
-  uint32_t lo = e1, hi = a.n;                                        // the first entry above key
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (a.key[mid] > key) hi = mid;
-    else lo = mid + 1;
+  __shared__ float sums[kJoinBlock][N];
+  const uint32_t e0 = blockIdx.x * span, e1 = e0 + span;          // (the last one has no later)
+  const uint32_t key = a.key[e1 - 1], next = a.key[e1], head = a.key[e0];
+  const uint32_t prev = e0 > 0 ? a.key[e0 - 1] : kNone;
+  if (key >= a.n_vocab || next != key || (head == key && prev == key)) return;
+  // one part in each later workgroup up to the first whose last entry is another number
+  uint32_t parts = 0;
+  for (bool more = true; more;) {
+    const uint32_t b = blockIdx.x + 1 + parts + threadIdx.x % 64;
+    const uint64_t end = ((uint64_t)b + 1) * span;
+    const bool full = b < a.blocks && end < a.n && a.key[end - 1] == key && a.key[end] == key;
+    const uint64_t stop = ~__ballot(full);
+    more = stop == 0;
+    parts += more ? 64 : (uint32_t)__builtin_ctzll(stop) + 1;
   }
-  const uint32_t parts = (lo - 1) / a.chunk - chunk;                 // starts of later chunks
-  const uint32_t groups = kSumBlock / a.lanes, group = threadIdx.x / a.lanes;
-  const int c = (int)(blockIdx.y * a.lanes + threadIdx.x % a.lanes) * N, left = a.d - c;
+  const uint32_t groups = kJoinBlock >> a.shift, group = threadIdx.x >> a.shift;
+  const int c = (int)(blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * N, left = a.d - c;
   const uint32_t per = (parts + groups - 1) / groups;
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.0f;
   if (left > 0) {
-    if (group == 0) load((const float *)a.part + ((int64_t)chunk * 2 + 1) * a.d + c, left, acc);
+    if (group == 0) load((const float *)a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d + c, left, acc);
     const uint32_t q1 = min(parts, (group + 1) * per);
 #pragma unroll 4
     for (uint32_t q = group * per; q < q1; ++q) {
       float v[N];
-      load((const float *)a.part + ((int64_t)(chunk + 1 + q) * 2) * a.d + c, left, v);
+      load((const float *)a.part + ((int64_t)(blockIdx.x + 1 + q) * 2) * a.d + c, left, v);
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] += v[i];
     }
@@ -294,108 +549,139 @@ __global__ __launch_bounds__(kSumBlock) void join_kernel(SumArgs<T> a, TO *__res
   write_row(dE + (int64_t)key * lde + c, left, acc, a.scale, a.accumulate);
 }
 
-// Rows row0 .. of dE whose number does not occur.  present: NULL when none does.
-template <typename TO>
-__global__ __launch_bounds__(kZeroBlock) void zero_kernel(const uint8_t *__restrict__ present, uint32_t total,
-                                                          int d, Divisor chunks, TO *__restrict__ dE,
-                                                          int64_t lde) {
-  const float zero[kCols<TO>] = {};
-#pragma unroll
-  for (int k = 0; k < kZeroPer; ++k) {
-    const uint32_t o = blockIdx.x * (uint32_t)(kZeroBlock * kZeroPer) + k * kZeroBlock + threadIdx.x;
-    if (o >= total) return;
-    uint32_t at;
-    const uint32_t row = divide(o, chunks, &at);
-    if (present && present[row]) continue;
-    const int c = (int)at * kCols<TO>;
-    store(dE + (int64_t)row * lde + c, d - c, zero);
+// --- launches -----------------------------------------------------------------------
+
+// dE's rows that a call has to write zeros to, handed out to its launches.  Rows go in slabs of
+// fewer than 2^31 chunks; all but the last slab get launches of their own.
+template <typename TO, typename Id>
+struct Zeros {
+  ZeroArgs<TO, Id> z;
+  uint32_t left = 0;
+  hipStream_t s;
+
+  // present: whether slots tell the rows that occur
+  Zeros(TO *dE, int64_t lde, int64_t n_vocab, int32_t d, const uint32_t *slot, const Id *ids,
+        int64_t n, bool present, hipStream_t stream)
+      : s(stream) {
+    const uint32_t chunks = chunks_of<TO>(d);
+    z = ZeroArgs<TO, Id>{dE, lde, d, divisor(chunks), slot, present ? ids : nullptr, (uint32_t)n,
+                         (uint32_t)n_vocab, 0, 0, 0};
+    slab = ((int64_t)1 << 30) / chunks;
+    rows = n_vocab;
+    left = (uint32_t)(std::min(slab, rows) * chunks);
   }
-}
-
-template <typename TO>
-void zero_rows(int64_t n_vocab, int32_t d, const uint8_t *present, TO *dE, int64_t lde, hipStream_t s) {
-  const uint32_t chunks = chunks_of<TO>(d);
-  const int64_t most = ((int64_t)1 << 30) / chunks;
-  for (int64_t r = 0; r < n_vocab; r += most) {
-    const uint32_t total = (uint32_t)(std::min(most, n_vocab - r) * chunks);
-    hipLaunchKernelGGL(zero_kernel<TO>, dim3((total + kZeroBlock * kZeroPer - 1) / (kZeroBlock * kZeroPer)),
-                       dim3(kZeroBlock), 0, s, present ? present + r : nullptr, total, d, divisor(chunks),
-                       dE + r * lde, lde);
+  // The next `most` chunks at most.
+  ZeroArgs<TO, Id> take(uint32_t most) {
+    ZeroArgs<TO, Id> t = z;
+    t.count = std::min(most, left);
+    z.first += t.count;
+    left -= t.count;
+    return t;
   }
-}
+  // Launches of their own for what is left, but for the first slab's when keep is set.
+  void rest(bool keep) {
+    int64_t r = slab;
+    if (!keep) launch(take(left));
+    for (; r < rows; r += slab) {
+      ZeroArgs<TO, Id> t = z;
+      t.row0 = r;
+      t.first = 0;
+      t.count = (uint32_t)(std::min(slab, rows - r) * t.chunks.d);
+      launch(t);
+    }
+  }
 
-// Lanes that walk a chunk: a power of two that holds a row's chunks, at most a wave.
-int lanes_of(uint32_t chunks) {
-  int lanes = 8;
-  while ((uint32_t)lanes < chunks && lanes < 64) lanes *= 2;
-  return lanes;
-}
+ private:
+  int64_t slab, rows;
+  void launch(const ZeroArgs<TO, Id> &t) {
+    if (t.count) hipLaunchKernelGGL((zero_kernel<TO, Id>), dim3(zero_blocks<256>(t.count)), dim3(256), 0, s, t);
+  }
+};
 
-template <typename Id>
-void sort_ids(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, uint8_t *ws, hipStream_t s) {
+// What a sort launch writes beside its own work (24 MB): it takes some 4 us, in which the
+// chip writes that much.
+constexpr uint32_t kBeside = 3 << 19;
+
+template <typename TO, typename Id>
+void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool slots, uint8_t *ws,
+                Zeros<TO, Id> &zeros, hipStream_t s) {
   uint32_t *count = (uint32_t *)(ws + p.count);
-  uint8_t *present = ws + p.present;
+  uint32_t *total = p.tiles > kFewTiles ? (uint32_t *)(ws + p.total) : nullptr;
+  uint32_t *slot = slots ? (uint32_t *)(ws + p.slot) : nullptr;
   for (int pass = 0; pass < p.passes; ++pass) {
     const uint32_t *kin = (const uint32_t *)(ws + p.key[(pass + 1) % 2]);
     const uint32_t *pin = (const uint32_t *)(ws + p.pos[(pass + 1) % 2]);
     uint32_t *kout = (uint32_t *)(ws + p.key[pass % 2]), *pout = (uint32_t *)(ws + p.pos[pass % 2]);
-    const uint32_t tile = (uint32_t)p.tile, tiles = (uint32_t)p.tiles;
     const int shift = pass * p.bits;
-    if (pass == 0) {
-      const unsigned clear = (unsigned)std::min<int64_t>(256, (n_vocab + 4 * kSortBlock - 1) / (4 * kSortBlock));
-      hipLaunchKernelGGL(count_kernel<Id>, dim3(tiles + clear), dim3(kSortBlock), 0, s, ids, (uint32_t)n,
-                         (uint32_t)n_vocab, tile, tiles, shift, p.bits, count, present);
-      hipLaunchKernelGGL((scatter_kernel<Id, true>), dim3(tiles), dim3(kSortBlock), 0, s, ids,
-                         (const uint32_t *)nullptr, (uint32_t)n, (uint32_t)n_vocab, tile, tiles, shift,
-                         p.bits, count, kout, pout, present);
-    } else {
-      hipLaunchKernelGGL(count_kernel<uint32_t>, dim3(tiles), dim3(kSortBlock), 0, s, kin, (uint32_t)n,
-                         (uint32_t)n_vocab, tile, tiles, shift, p.bits, count, present);
-      hipLaunchKernelGGL((scatter_kernel<uint32_t, false>), dim3(tiles), dim3(kSortBlock), 0, s, kin, pin,
-                         (uint32_t)n, (uint32_t)n_vocab, tile, tiles, shift, p.bits, count, kout, pout,
-                         present);
-    }
+    if (pass == 0)
+      hipLaunchKernelGGL(count_kernel<Id>, dim3(p.tiles), dim3(kSortBlock), 0, s, ids, n, n_vocab, shift,
+                         p.bits, count, slot);
+    else
+      hipLaunchKernelGGL(count_kernel<uint32_t>, dim3(p.tiles), dim3(kSortBlock), 0, s, kin, n, n_vocab,
+                         shift, p.bits, count, (uint32_t *)nullptr);
+    if (total)
+      hipLaunchKernelGGL(scan_kernel, dim3(1u << p.bits), dim3(256), 0, s, count, p.tiles, p.bits, total);
+    const ZeroArgs<TO, Id> z = zeros.take(kBeside);
+    const dim3 grid(p.tiles + zero_blocks<kSortBlock>(z.count));
+    if (pass == 0)
+      hipLaunchKernelGGL((scatter_kernel<TO, Id, Id, true>), grid, dim3(kSortBlock), 0, s, ids,
+                         (const uint32_t *)nullptr, n, n_vocab, p.tiles, shift, p.bits, count, total, kout,
+                         pout, z);
+    else
+      hipLaunchKernelGGL((scatter_kernel<TO, Id, uint32_t, false>), grid, dim3(kSortBlock), 0, s, kin, pin,
+                         n, n_vocab, p.tiles, shift, p.bits, count, total, kout, pout, z);
   }
 }
 
-template <typename T, typename TO>
-toc_status grad(const Plan &p, int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab, int32_t d,
-                const T *G, int64_t ldg, float scale, const toc_drop *drop, TO *dE, int64_t lde,
-                int32_t accumulate, uint8_t *ws, hipStream_t s) {
+template <typename T, typename TO, typename Id>
+toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_t d, const T *G,
+                int64_t ldg, float scale, const toc_drop *drop, TO *dE, int64_t lde, bool accumulate,
+                uint8_t *ws, hipStream_t s) {
+  Zeros<TO, Id> zeros(dE, lde, accumulate ? 0 : n_vocab, d, (const uint32_t *)(ws + p.slot), ids, n,
+                      n > 0 && !p.small, s);
   if (n == 0) {
-    if (!accumulate) zero_rows(n_vocab, d, nullptr, dE, lde, s);
+    zeros.rest(false);
     return launched("zero_kernel");
   }
-  if (id_bits == 32) sort_ids(p, n, (const int32_t *)ids, n_vocab, ws, s);
-  else sort_ids(p, n, (const int64_t *)ids, n_vocab, ws, s);
+  if (p.small) {
+    zeros.rest(true);
+    const ZeroArgs<TO, Id> z = zeros.take(zeros.left);
+    hipLaunchKernelGGL((small_kernel<TO, Id>), dim3(1 + zero_blocks<kSortBlock>(z.count)), dim3(kSortBlock), 0,
+                       s, ids, (uint32_t)n, (uint32_t)n_vocab, p.bits, p.passes,
+                       (uint32_t *)(ws + p.key[0]), (uint32_t *)(ws + p.pos[0]), z);
+  } else {
+    sort_tiles(p, (uint32_t)n, ids, (uint32_t)n_vocab, !accumulate, ws, zeros, s);
+    zeros.rest(true);
+  }
   const Mask m = mask_of(drop);
-  const int last = (p.passes - 1) % 2;
+  const int last = p.small ? 0 : (p.passes - 1) % 2;
+  const uint32_t span = block_span<T>(d);
+  const int lanes = lanes_of(chunks_of<T>(d));
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
-               (uint32_t)n_vocab, (uint32_t)p.chunk, (uint32_t)p.chunks, d, lanes_of(chunks_of<T>(d)), G, ldg, scale * m.keep,
-               m, (float *)(ws + p.part), accumulate};
+               (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), d, lanes,
+               __builtin_ctz(lanes), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
   const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
-  const unsigned per = (unsigned)(kSumBlock / a.lanes);
-  const dim3 grid((unsigned)((p.chunks + per - 1) / per), slices);
-  if (!accumulate) zero_rows(n_vocab, d, ws + p.present, dE, lde, s);
-  if (a.m.on)
-    hipLaunchKernelGGL((sum_kernel<T, TO, true>), grid, dim3(kSumBlock), 0, s, a, dE, lde);
+  const ZeroArgs<TO, Id> z = zeros.take(zeros.left);
+  const dim3 grid(a.blocks + (zero_blocks<kSumBlock>(z.count) + slices - 1) / slices, slices);
+  if (m.on)
+    hipLaunchKernelGGL((sum_kernel<T, TO, Id, true>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);
   else
-    hipLaunchKernelGGL((sum_kernel<T, TO, false>), grid, dim3(kSumBlock), 0, s, a, dE, lde);
-  if (p.chunks > 1)
-    hipLaunchKernelGGL((join_kernel<T, TO>), dim3((unsigned)p.chunks, slices), dim3(kSumBlock), 0, s, a, dE, lde);
+    hipLaunchKernelGGL((sum_kernel<T, TO, Id, false>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);
+  if (a.blocks > 1)
+    hipLaunchKernelGGL((join_kernel<T, TO>), dim3(a.blocks - 1, slices), dim3(kJoinBlock), 0, s, a, span, dE,
+                       lde);
   return launched("embed gradient kernels");
 }
 
-template <typename T>
-toc_status grad_typed(const Plan &p, int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab,
-                      int32_t d, const void *G, int64_t ldg, float scale, const toc_drop *drop,
-                      bool f32, void *dE, int64_t lde, int32_t accumulate, void *ws, void *stream) {
-  const hipStream_t s = (hipStream_t)stream;
-  if (f32)
-    return grad(p, n, ids, id_bits, n_vocab, d, (const T *)G, ldg, scale, drop, (float *)dE, lde, accumulate,
-                (uint8_t *)ws, s);
-  return grad(p, n, ids, id_bits, n_vocab, d, (const T *)G, ldg, scale, drop, (T *)dE, lde, accumulate,
-              (uint8_t *)ws, s);
+template <typename T, typename TO>
+toc_status grad_ids(const Plan &p, int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab,
+                    int32_t d, const void *G, int64_t ldg, float scale, const toc_drop *drop, void *dE,
+                    int64_t lde, int32_t accumulate, void *ws, void *stream) {
+  if (id_bits == 32)
+    return grad(p, n, (const int32_t *)ids, n_vocab, d, (const T *)G, ldg, scale, drop, (TO *)dE, lde,
+                accumulate != 0, (uint8_t *)ws, (hipStream_t)stream);
+  return grad(p, n, (const int64_t *)ids, n_vocab, d, (const T *)G, ldg, scale, drop, (TO *)dE, lde,
+              accumulate != 0, (uint8_t *)ws, (hipStream_t)stream);
 }
 
 toc_status check_grad(int64_t n, int64_t n_vocab, int32_t d) {
@@ -444,14 +730,17 @@ toc_status toc_embed_grad(int64_t n, const void *ids, int32_t id_bits, int64_t n
   if ((uintptr_t)ws % 16) return fail(TOC_EINVAL, "workspace is not 16-byte aligned");
   if (n_vocab == 0) return TOC_OK;
   const bool f32 = de_type == TOC_F32;
+#define TOC_GRAD(T, TO) \
+  grad_ids<T, TO>(p, n, ids, id_bits, n_vocab, d, G, ldg, scale, drop, dE, lde, accumulate, ws, stream)
   switch (type) {
     case TOC_F32:
-      return grad_typed<float>(p, n, ids, id_bits, n_vocab, d, G, ldg, scale, drop, f32, dE, lde, accumulate, ws, stream);
+      return TOC_GRAD(float, float);
     case TOC_BF16:
-      return grad_typed<bf16>(p, n, ids, id_bits, n_vocab, d, G, ldg, scale, drop, f32, dE, lde, accumulate, ws, stream);
+      return f32 ? TOC_GRAD(bf16, float) : TOC_GRAD(bf16, bf16);
     default:
-      return grad_typed<f16>(p, n, ids, id_bits, n_vocab, d, G, ldg, scale, drop, f32, dE, lde, accumulate, ws, stream);
+      return f32 ? TOC_GRAD(f16, float) : TOC_GRAD(f16, f16);
   }
+#undef TOC_GRAD
 }
 
 }  // extern "C"
