@@ -28,7 +28,7 @@ constexpr int kSmallKeys = 4;
 constexpr uint32_t kSmall = kSmallKeys * kSortBlock;
 constexpr uint32_t kFewTiles = 64;           // above, the tiles' counts are summed by scan_kernel
 constexpr int kSumBlock = 512;
-constexpr uint32_t kSpan = 16;               // entries of a span
+constexpr uint32_t kMinSpan = 8, kMaxSpan = 32;   // entries of a span
 constexpr int kAhead = 8;                    // entries whose rows' loads fly together
 constexpr int kJoinBlock = 256;
 constexpr int kZeroPer = 4;                  // chunks a thread of the zero workgroups writes
@@ -40,7 +40,7 @@ struct Plan {
   int bits, passes;       // digit bits of a pass
   bool small;
   uint32_t tiles;
-  size_t key[2], pos[2], count, total, slot, part, end;
+  size_t orig, key[2], pos[2], count, total, slot, part, end;
 };
 
 size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
@@ -62,10 +62,20 @@ int lanes_of(uint32_t chunks) {
   return best;
 }
 
+// Entries of a span: the more, the fewer parts of rows are put together, as long as the chip
+// has some 4,096 waves (us for 8, 16, 32: 131,072 x 1,024 bf16 161, 151, 148; 131,072 x 512 f16
+// of 300 numbers 80, 68, 58; 100,000 x 64 f32 35.9, 36.6, 43.8; 4,000 x 256 bf16 21.5, 25.2, 31.3).
+uint32_t span_of(int64_t n, uint32_t chunks) {
+  const int64_t lanes = lanes_of(chunks), slices = (chunks + lanes - 1) / lanes;
+  uint32_t span = kMaxSpan;
+  while (span > kMinSpan && n / span * lanes * slices < 4096 * 64) span /= 2;
+  return span;
+}
+
 // Entries of the sorted list that a workgroup of sum_kernel walks.
 template <typename T>
-uint32_t block_span(int32_t d) {
-  return (uint32_t)(kSumBlock / lanes_of(chunks_of<T>(d))) * kSpan;
+uint32_t block_span(int64_t n, int32_t d) {
+  return (uint32_t)(kSumBlock / lanes_of(chunks_of<T>(d))) * span_of(n, chunks_of<T>(d));
 }
 
 Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
@@ -76,7 +86,7 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   p.bits = (width + p.passes - 1) / p.passes;
   p.small = n <= (int64_t)kSmall;
   p.tiles = p.small ? 0 : (uint32_t)((n + kTile - 1) / kTile);
-  const int64_t least = std::min(block_span<float>(d), block_span<bf16>(d));
+  const int64_t least = std::min(block_span<float>(n, d), block_span<bf16>(n, d));
   const int64_t blocks = (n + least - 1) / least;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -84,6 +94,7 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
     at = align16(at + bytes);
     return here;
   };
+  p.orig = take(p.small ? 0 : (size_t)n * 4);
   for (int i = 0; i < 2; ++i) {
     // (a small sort keeps all passes but the last in LDS)
     p.key[i] = i == 0 || !p.small ? take((size_t)n * 4) : p.key[0];
@@ -97,47 +108,48 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   return p;
 }
 
+// A token number, or V for one outside the table.
 template <typename Id>
-__device__ inline uint32_t key_at(const Id *ids, uint32_t i, uint32_t n_vocab) {
+__device__ inline uint32_t key_of(const Id *ids, uint32_t i, uint32_t n_vocab) {
   const int64_t id = (int64_t)ids[i];
   return id >= 0 && id < (int64_t)n_vocab ? (uint32_t)id : n_vocab;
 }
-__device__ inline uint32_t key_at(const uint32_t *keys, uint32_t i, uint32_t) { return keys[i]; }
 
 // --- zero ----------------------------------------------------------------------
 
-// Chunks first .. first + count - 1 of dE, counted row by row.  ids NULL: all of them are
+// Chunks first .. first + count - 1 of dE, counted row by row.  keys NULL: all of them are
 // written.  Else those of rows whose number does not occur: count_kernel left in slot[v] some
 // token of number v if there is one, and whatever else a slot holds is no such token, since
 // the token's own number is looked up again (so the slots need no clearing).
-template <typename TO, typename Id>
+template <typename TO>
 struct ZeroArgs {
   TO *dE;
   int64_t lde;
   int d;
   Divisor chunks;
-  const uint32_t *slot;
-  const Id *ids;
-  uint32_t n, n_vocab;
+  const uint32_t *slot, *keys;
+  uint32_t n;
   int64_t row0;            // the row of chunk 0
   uint32_t first, count;
 };
 
-template <int kBlock, typename TO, typename Id>
-__device__ inline void zero_rows(const ZeroArgs<TO, Id> &z, uint32_t block) {
-  const Chunk zero = {{0u, 0u, 0u, 0u}};
+template <int kBlock, typename TO>
+__device__ inline void zero_rows(const ZeroArgs<TO> &z, uint32_t block) {
+  const Chunk zero = {0u, 0u, 0u, 0u};
   const uint32_t o0 = block * (uint32_t)(kBlock * kZeroPer) + threadIdx.x;
-  uint32_t row[kZeroPer], at[kZeroPer], t[kZeroPer];
+  uint32_t row[kZeroPer], at[kZeroPer], t[kZeroPer], key[kZeroPer];
 #pragma unroll
   for (int k = 0; k < kZeroPer; ++k) {
     const uint32_t o = o0 + (uint32_t)(k * kBlock);
     row[k] = divide(z.first + (o < z.count ? o : 0u), z.chunks, &at[k]);
-    t[k] = z.ids ? z.slot[z.row0 + row[k]] : kNone;
+    t[k] = z.keys ? z.slot[z.row0 + row[k]] : kNone;
   }
+#pragma unroll
+  for (int k = 0; k < kZeroPer; ++k) key[k] = t[k] < z.n ? z.keys[t[k]] : kNone;
 #pragma unroll
   for (int k = 0; k < kZeroPer; ++k) {
     if (o0 + (uint32_t)(k * kBlock) >= z.count) return;
-    if (t[k] < z.n && (int64_t)key_at(z.ids, t[k], z.n_vocab) == z.row0 + row[k]) continue;
+    if ((int64_t)key[k] == z.row0 + row[k]) continue;
     const int c = (int)at[k] * kCols<TO>;
     put(z.dE + (z.row0 + row[k]) * z.lde + c, z.d - c, zero);
   }
@@ -146,8 +158,8 @@ __device__ inline void zero_rows(const ZeroArgs<TO, Id> &z, uint32_t block) {
 template <int kBlock>
 uint32_t zero_blocks(uint32_t count) { return (count + kBlock * kZeroPer - 1) / (kBlock * kZeroPer); }
 
-template <typename TO, typename Id>
-__global__ __launch_bounds__(256) void zero_kernel(ZeroArgs<TO, Id> z) {
+template <typename TO>
+__global__ __launch_bounds__(256) void zero_kernel(ZeroArgs<TO> z) {
   zero_rows<256>(z, blockIdx.x);
 }
 
@@ -211,7 +223,7 @@ __global__ __launch_bounds__(kSortBlock) void small_kernel(const Id *__restrict_
                                                            uint32_t n_vocab, int bits, int passes,
                                                            uint32_t *__restrict__ key_out,
                                                            uint32_t *__restrict__ pos_out,
-                                                           ZeroArgs<TO, Id> z) {
+                                                           ZeroArgs<TO> z) {
   __shared__ uint16_t at[kSortWaves][kMaxDigits];
   __shared__ uint32_t base[kMaxDigits], sums[kSortWaves];
   __shared__ uint32_t keys[kSmall];
@@ -229,7 +241,7 @@ __global__ __launch_bounds__(kSortBlock) void small_kernel(const Id *__restrict_
   for (int k = 0; k < kSmallKeys; ++k) {
     i[k] = (wave * per + k) * 64 + lane;
     in[k] = (uint32_t)k < per && i[k] < n;
-    key[k] = in[k] ? key_at(ids, i[k], n_vocab) : 0u;
+    key[k] = in[k] ? key_of(ids, i[k], n_vocab) : 0u;
     pos[k] = i[k];
   }
   for (int pass = 0; pass < passes; ++pass) {
@@ -266,12 +278,13 @@ __global__ __launch_bounds__(kSortBlock) void small_kernel(const Id *__restrict_
   }
 }
 
-// The tile's count of each digit; in the first pass also a token of each number (slot, or
-// NULL when accumulating).
-template <typename Id>
+// The tile's count of each digit.  First pass (Id a token number): also the pairs' numbers
+// into orig, and a token of each number into slot (NULL when accumulating).
+template <typename Id, bool kFirst>
 __global__ __launch_bounds__(kSortBlock) void count_kernel(const Id *__restrict__ ids, uint32_t n,
                                                            uint32_t n_vocab, int shift, int bits,
                                                            uint32_t *__restrict__ count,
+                                                           uint32_t *__restrict__ orig,
                                                            uint32_t *__restrict__ slot) {
   __shared__ uint32_t c[kMaxDigits];
   const uint32_t digits = 1u << bits;
@@ -280,8 +293,11 @@ __global__ __launch_bounds__(kSortBlock) void count_kernel(const Id *__restrict_
 #pragma unroll
   for (int k = 0; k < kTileKeys; ++k) {
     const uint32_t i = blockIdx.x * kTile + k * kSortBlock + threadIdx.x;
-    key[k] = i < n ? key_at(ids, i, n_vocab) : kNone;
-    if (slot && key[k] < n_vocab) slot[key[k]] = i;
+    key[k] = i >= n ? kNone : kFirst ? key_of(ids, i, n_vocab) : (uint32_t)ids[i];
+    if (kFirst && i < n) {
+      orig[i] = key[k];
+      if (slot && key[k] < n_vocab) slot[key[k]] = i;
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -311,13 +327,13 @@ __global__ __launch_bounds__(256) void scan_kernel(uint32_t *__restrict__ count,
 
 // Workgroups 0 .. tiles-1 place a tile's pairs: a digit's pairs of the tile come after all
 // pairs of lower digits and the digit's of earlier tiles, waves and lanes.  total: NULL, or
-// scan_kernel's, and count then holds the counts before.  The other workgroups write zeros.
-template <typename TO, typename Id, typename Key, bool kFirst>
+// scan_kernel's, and count then holds the counts before; pos NULL: the pairs are in their
+// first order.  The other workgroups write zeros.
+template <typename TO>
 __global__ __launch_bounds__(kSortBlock) void scatter_kernel(
-    const Key *__restrict__ ids, const uint32_t *__restrict__ pos, uint32_t n, uint32_t n_vocab,
-    uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
+    const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, uint32_t n, uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
     const uint32_t *__restrict__ total, uint32_t *__restrict__ key_out, uint32_t *__restrict__ pos_out,
-    ZeroArgs<TO, Id> z) {
+    ZeroArgs<TO> z) {
   __shared__ uint16_t at[kSortWaves][kMaxDigits];
   __shared__ uint32_t base[kMaxDigits], sums[kSortWaves];
   __shared__ uint32_t before[kSortBlock], all[kSortBlock];
@@ -332,8 +348,8 @@ __global__ __launch_bounds__(kSortBlock) void scatter_kernel(
   for (int k = 0; k < kTileKeys; ++k) {
     const uint32_t i = blockIdx.x * kTile + (wave * kTileKeys + k) * 64 + lane;
     in[k] = i < n;
-    key[k] = in[k] ? key_at(ids, i, n_vocab) : 0u;
-    from[k] = kFirst || !in[k] ? i : pos[i];
+    key[k] = in[k] ? keys[i] : 0u;
+    from[k] = in[k] && pos ? pos[i] : i;
     digit[k] = key[k] >> shift & (digits - 1);
   }
   uint32_t b = 0, a = 0;
@@ -386,6 +402,7 @@ struct SumArgs {
   const uint32_t *key, *pos;
   uint32_t n, n_vocab, blocks;   // workgroups along the list
   int d, lanes, shift;           // lanes = 1 << shift
+  uint32_t span;                 // entries of a group of lanes
   const T *G;
   int64_t ldg;
   float scale;
@@ -407,93 +424,121 @@ __device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, in
   store(p, left, v);
 }
 
-// Workgroups 0 .. a.blocks-1 of a slice (blockIdx.y) of `lanes` chunks of the columns: group g
-// walks entries (blockIdx.x groups + g) kSpan onwards.  The others write zeros.
-template <typename T, typename TO, typename Id, bool kDrop>
+// Workgroups 0 .. a.blocks-1 of a slice (blockIdx.y) of kLanes chunks of the columns: group g
+// walks entries (blockIdx.x groups + g) span onwards.  The others write zeros.  A group's
+// lanes hold its entries' numbers and tokens between them, so that the rows' loads wait for
+// nothing but each other: kAhead of them are always under way.
+template <typename T, typename TO, int kLanes, bool kDrop>
 __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde,
-                                                        ZeroArgs<TO, Id> z) {
+                                                        ZeroArgs<TO> z) {
   constexpr int N = kCols<T>;
+  constexpr uint32_t kGroups = kSumBlock / kLanes;
+  constexpr int kHold = ((int)kMaxSpan + kLanes - 1) / kLanes;
   __shared__ float heads[kSumBlock][N];          // each group's part of a number from before
-  __shared__ uint8_t through[kSumBlock / 8];     // ... which goes on after the group
+  __shared__ uint8_t through[kGroups];           // ... which goes on after the group
   if (blockIdx.x >= a.blocks) {
     zero_rows<kSumBlock>(z, (blockIdx.x - a.blocks) * gridDim.y + blockIdx.y);
     return;
   }
-  const uint32_t groups = kSumBlock >> a.shift, group = threadIdx.x >> a.shift;
-  const int lane = threadIdx.x & (a.lanes - 1);
-  const int c = (int)(blockIdx.y * a.lanes + lane) * N, left = a.d - c;
-  const uint64_t first = ((uint64_t)blockIdx.x * groups + group) * kSpan;
-  const uint32_t e0 = (uint32_t)min(first, (uint64_t)a.n), e1 = min(a.n, e0 + kSpan);
+  uint32_t group = threadIdx.x / kLanes;
+  if (kLanes == 64) group = __builtin_amdgcn_readfirstlane(group);
+  const int lane = threadIdx.x % kLanes;
+  const int c = (int)(blockIdx.y * kLanes + lane) * N, left = a.d - c;
+  const Place<T, kLanes == 8> l = place<T, kLanes == 8>(c, a.d);
+  const uint32_t e0 = (uint32_t)min(((uint64_t)blockIdx.x * kGroups + group) * a.span, (uint64_t)a.n);
+  const uint32_t entries = min(a.n - e0, a.span);
+  uint32_t keys[kHold], tokens[kHold];
+#pragma unroll
+  for (int j = 0; j < kHold; ++j) {
+    const uint32_t e = lane + j * kLanes;
+    keys[j] = e < entries ? a.key[e0 + e] : kNone;
+    tokens[j] = e < entries ? a.pos[e0 + e] : 0u;
+  }
+  const uint32_t prev = e0 > 0 && entries ? a.key[e0 - 1] : kNone;
+  const uint32_t next = e0 + entries < a.n ? a.key[e0 + entries] : kNone;
+  // entry u's number or token, in all lanes of the group (all of them take part)
+  auto of = [&](const uint32_t(&held)[kHold], int u) -> uint32_t {
+    if constexpr (kLanes == 64) return __builtin_amdgcn_readlane(held[0], u);
+    else {
+      uint32_t x = held[0];
+#pragma unroll
+      for (int j = 1; j < kHold; ++j) x = u < j * kLanes ? x : held[j];
+      return __shfl(x, u % kLanes, kLanes);
+    }
+  };
+  Chunk in[kAhead];
+  uint32_t at[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    at[u] = of(tokens, u);
+    in[u] = fetch(a.G + (int64_t)at[u] * a.ldg, l);
+  }
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-  uint32_t cur = kNone;
-  bool from_before = false, goes_on = false;
-  if (e0 < e1) {
-    cur = a.key[e0];
-    from_before = e0 > 0 && a.key[e0 - 1] == cur;
-    for (uint32_t e = e0; e < e1; e += kAhead) {
-      uint32_t k[kAhead], p[kAhead];
-      Chunk in[kAhead];
+  uint32_t cur = of(keys, 0);
+  const uint32_t start = cur;
+  const bool begun = entries && prev == cur;     // the first number is from before
+  bool from_before = begun;
+#pragma unroll 1
+  for (int u0 = 0; u0 < (int)a.span; u0 += kAhead) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        k[u] = a.key[min(e + u, e1 - 1)];
-        p[u] = a.pos[min(e + u, e1 - 1)];
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) in[u] = fetch(a.G + (int64_t)p[u] * a.ldg + c, left);
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (e + u >= e1) break;
-        if (k[u] != cur) {
+    for (int j = 0; j < kAhead; ++j) {
+      const int u = u0 + j;
+      const uint32_t key = of(keys, u);
+      if (u < (int)entries) {
+        if (key != cur) {
           if (from_before) {
 #pragma unroll
             for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
           } else if (left > 0) {                 // (cur < V: a larger number sorts after it)
             write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
           }
-          cur = k[u];
+          cur = key;
           from_before = false;
 #pragma unroll
           for (int i = 0; i < N; ++i) acc[i] = 0.0f;
         }
+        Chunk x = settle(in[j], l);
         float v[N];
-        if (kDrop) drop<T>(in[u], (uint32_t)c, p[u], a.m);
-        widen<T>(in[u], v);
+        if (kDrop) drop<T>(x, (uint32_t)c, at[j], a.m);
+        widen<T>(x, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] += v[i];
       }
+      if (u0 + kAhead < (int)a.span) {
+        at[j] = of(tokens, u + kAhead);
+        in[j] = fetch(a.G + (int64_t)at[j] * a.ldg, l);
+      }
     }
-    goes_on = e1 < a.n && a.key[e1] == cur;
-    if (from_before) {
+  }
+  const bool goes_on = entries && next == cur;
+  if (from_before) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
-    } else if (!goes_on && cur < a.n_vocab && left > 0) {
-      write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
-    }
+    for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
+  } else if (entries && !goes_on && cur < a.n_vocab && left > 0) {
+    write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
   }
   if (lane == 0) through[group] = from_before && goes_on;
   __syncthreads();
-  if (left <= 0 || e0 >= e1) return;
+  if (left <= 0 || !entries) return;
   // A group whose last number begins in it and goes on adds the parts of the groups that
   // follow; group 0 does so for a number from before the workgroup.
-  const bool at_start = group == 0 && e0 > 0 && a.key[e0 - 1] == a.key[e0];
-  if (at_start) {
-    const uint32_t key = a.key[e0];
+  if (group == 0 && begun && start < a.n_vocab) {
     float v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = heads[threadIdx.x][i];
-    for (uint32_t g = 0; g + 1 < groups && through[g]; ++g)
+    for (uint32_t g = 0; g + 1 < kGroups && through[g]; ++g)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += heads[(g + 1) * a.lanes + lane][i];
-    if (key < a.n_vocab) store(a.part + (int64_t)blockIdx.x * 2 * a.d + c, left, v);
+      for (int i = 0; i < N; ++i) v[i] += heads[(g + 1) * kLanes + lane][i];
+    store(a.part + (int64_t)blockIdx.x * 2 * a.d + c, left, v);
   }
   if (goes_on && !from_before && cur < a.n_vocab) {
     uint32_t g = group + 1;
     bool open = true;                            // whether the number reaches group g
-    for (; g < groups && open; ++g) {
+    for (; g < kGroups && open; ++g) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) acc[i] += heads[g * a.lanes + lane][i];
+      for (int i = 0; i < N; ++i) acc[i] += heads[g * kLanes + lane][i];
       open = through[g];
     }
     if (open) store(a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d + c, left, acc);
@@ -553,26 +598,25 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t
 
 // dE's rows that a call has to write zeros to, handed out to its launches.  Rows go in slabs of
 // fewer than 2^31 chunks; all but the last slab get launches of their own.
-template <typename TO, typename Id>
+template <typename TO>
 struct Zeros {
-  ZeroArgs<TO, Id> z;
+  ZeroArgs<TO> z;
   uint32_t left = 0;
   hipStream_t s;
 
-  // present: whether slots tell the rows that occur
-  Zeros(TO *dE, int64_t lde, int64_t n_vocab, int32_t d, const uint32_t *slot, const Id *ids,
-        int64_t n, bool present, hipStream_t stream)
+  // keys: the tokens' numbers if the slots tell the rows that occur, or NULL
+  Zeros(TO *dE, int64_t lde, int64_t n_vocab, int32_t d, const uint32_t *slot, const uint32_t *keys,
+        int64_t n, hipStream_t stream)
       : s(stream) {
     const uint32_t chunks = chunks_of<TO>(d);
-    z = ZeroArgs<TO, Id>{dE, lde, d, divisor(chunks), slot, present ? ids : nullptr, (uint32_t)n,
-                         (uint32_t)n_vocab, 0, 0, 0};
+    z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, (uint32_t)n, 0, 0, 0};
     slab = ((int64_t)1 << 30) / chunks;
     rows = n_vocab;
     left = (uint32_t)(std::min(slab, rows) * chunks);
   }
   // The next `most` chunks at most.
-  ZeroArgs<TO, Id> take(uint32_t most) {
-    ZeroArgs<TO, Id> t = z;
+  ZeroArgs<TO> take(uint32_t most) {
+    ZeroArgs<TO> t = z;
     t.count = std::min(most, left);
     z.first += t.count;
     left -= t.count;
@@ -583,7 +627,7 @@ struct Zeros {
     int64_t r = slab;
     if (!keep) launch(take(left));
     for (; r < rows; r += slab) {
-      ZeroArgs<TO, Id> t = z;
+      ZeroArgs<TO> t = z;
       t.row0 = r;
       t.first = 0;
       t.count = (uint32_t)(std::min(slab, rows - r) * t.chunks.d);
@@ -593,8 +637,8 @@ struct Zeros {
 
  private:
   int64_t slab, rows;
-  void launch(const ZeroArgs<TO, Id> &t) {
-    if (t.count) hipLaunchKernelGGL((zero_kernel<TO, Id>), dim3(zero_blocks<256>(t.count)), dim3(256), 0, s, t);
+  void launch(const ZeroArgs<TO> &t) {
+    if (t.count) hipLaunchKernelGGL(zero_kernel<TO>, dim3(zero_blocks<256>(t.count)), dim3(256), 0, s, t);
   }
 };
 
@@ -604,32 +648,26 @@ constexpr uint32_t kBeside = 3 << 19;
 
 template <typename TO, typename Id>
 void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool slots, uint8_t *ws,
-                Zeros<TO, Id> &zeros, hipStream_t s) {
-  uint32_t *count = (uint32_t *)(ws + p.count);
+                Zeros<TO> &zeros, hipStream_t s) {
+  uint32_t *count = (uint32_t *)(ws + p.count), *orig = (uint32_t *)(ws + p.orig);
   uint32_t *total = p.tiles > kFewTiles ? (uint32_t *)(ws + p.total) : nullptr;
   uint32_t *slot = slots ? (uint32_t *)(ws + p.slot) : nullptr;
   for (int pass = 0; pass < p.passes; ++pass) {
-    const uint32_t *kin = (const uint32_t *)(ws + p.key[(pass + 1) % 2]);
-    const uint32_t *pin = (const uint32_t *)(ws + p.pos[(pass + 1) % 2]);
+    const uint32_t *kin = pass ? (const uint32_t *)(ws + p.key[(pass + 1) % 2]) : orig;
+    const uint32_t *pin = pass ? (const uint32_t *)(ws + p.pos[(pass + 1) % 2]) : nullptr;
     uint32_t *kout = (uint32_t *)(ws + p.key[pass % 2]), *pout = (uint32_t *)(ws + p.pos[pass % 2]);
     const int shift = pass * p.bits;
     if (pass == 0)
-      hipLaunchKernelGGL(count_kernel<Id>, dim3(p.tiles), dim3(kSortBlock), 0, s, ids, n, n_vocab, shift,
-                         p.bits, count, slot);
+      hipLaunchKernelGGL((count_kernel<Id, true>), dim3(p.tiles), dim3(kSortBlock), 0, s, ids, n, n_vocab,
+                         shift, p.bits, count, orig, slot);
     else
-      hipLaunchKernelGGL(count_kernel<uint32_t>, dim3(p.tiles), dim3(kSortBlock), 0, s, kin, n, n_vocab,
-                         shift, p.bits, count, (uint32_t *)nullptr);
+      hipLaunchKernelGGL((count_kernel<uint32_t, false>), dim3(p.tiles), dim3(kSortBlock), 0, s, kin, n,
+                         n_vocab, shift, p.bits, count, (uint32_t *)nullptr, (uint32_t *)nullptr);
     if (total)
       hipLaunchKernelGGL(scan_kernel, dim3(1u << p.bits), dim3(256), 0, s, count, p.tiles, p.bits, total);
-    const ZeroArgs<TO, Id> z = zeros.take(kBeside);
-    const dim3 grid(p.tiles + zero_blocks<kSortBlock>(z.count));
-    if (pass == 0)
-      hipLaunchKernelGGL((scatter_kernel<TO, Id, Id, true>), grid, dim3(kSortBlock), 0, s, ids,
-                         (const uint32_t *)nullptr, n, n_vocab, p.tiles, shift, p.bits, count, total, kout,
-                         pout, z);
-    else
-      hipLaunchKernelGGL((scatter_kernel<TO, Id, uint32_t, false>), grid, dim3(kSortBlock), 0, s, kin, pin,
-                         n, n_vocab, p.tiles, shift, p.bits, count, total, kout, pout, z);
+    const ZeroArgs<TO> z = zeros.take(kBeside);
+    hipLaunchKernelGGL(scatter_kernel<TO>, dim3(p.tiles + zero_blocks<kSortBlock>(z.count)), dim3(kSortBlock),
+                       0, s, kin, pin, n, p.tiles, shift, p.bits, count, total, kout, pout, z);
   }
 }
 
@@ -637,15 +675,15 @@ template <typename T, typename TO, typename Id>
 toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_t d, const T *G,
                 int64_t ldg, float scale, const toc_drop *drop, TO *dE, int64_t lde, bool accumulate,
                 uint8_t *ws, hipStream_t s) {
-  Zeros<TO, Id> zeros(dE, lde, accumulate ? 0 : n_vocab, d, (const uint32_t *)(ws + p.slot), ids, n,
-                      n > 0 && !p.small, s);
+  Zeros<TO> zeros(dE, lde, accumulate ? 0 : n_vocab, d, (const uint32_t *)(ws + p.slot),
+                  n > 0 && !p.small ? (const uint32_t *)(ws + p.orig) : nullptr, n, s);
   if (n == 0) {
     zeros.rest(false);
     return launched("zero_kernel");
   }
   if (p.small) {
     zeros.rest(true);
-    const ZeroArgs<TO, Id> z = zeros.take(zeros.left);
+    const ZeroArgs<TO> z = zeros.take(zeros.left);
     hipLaunchKernelGGL((small_kernel<TO, Id>), dim3(1 + zero_blocks<kSortBlock>(z.count)), dim3(kSortBlock), 0,
                        s, ids, (uint32_t)n, (uint32_t)n_vocab, p.bits, p.passes,
                        (uint32_t *)(ws + p.key[0]), (uint32_t *)(ws + p.pos[0]), z);
@@ -655,18 +693,23 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
   }
   const Mask m = mask_of(drop);
   const int last = p.small ? 0 : (p.passes - 1) % 2;
-  const uint32_t span = block_span<T>(d);
+  const uint32_t span = block_span<T>(n, d);
   const int lanes = lanes_of(chunks_of<T>(d));
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
                (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), d, lanes,
-               __builtin_ctz(lanes), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
+               __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
   const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
-  const ZeroArgs<TO, Id> z = zeros.take(zeros.left);
+  const ZeroArgs<TO> z = zeros.take(zeros.left);
   const dim3 grid(a.blocks + (zero_blocks<kSumBlock>(z.count) + slices - 1) / slices, slices);
-  if (m.on)
-    hipLaunchKernelGGL((sum_kernel<T, TO, Id, true>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);
-  else
-    hipLaunchKernelGGL((sum_kernel<T, TO, Id, false>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);
+#define TOC_SUM(L)                                                                                      \
+  if (lanes == L) {                                                                                      \
+    if (m.on)                                                                                            \
+      hipLaunchKernelGGL((sum_kernel<T, TO, L, true>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);      \
+    else                                                                                                 \
+      hipLaunchKernelGGL((sum_kernel<T, TO, L, false>), grid, dim3(kSumBlock), 0, s, a, dE, lde, z);     \
+  }
+  TOC_SUM(8) TOC_SUM(16) TOC_SUM(32) TOC_SUM(64)
+#undef TOC_SUM
   if (a.blocks > 1)
     hipLaunchKernelGGL((join_kernel<T, TO>), dim3(a.blocks - 1, slices), dim3(kJoinBlock), 0, s, a, span, dE,
                        lde);

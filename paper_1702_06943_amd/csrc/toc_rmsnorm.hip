@@ -112,6 +112,9 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
   const int lane = threadIdx.x % kLanes;
   float w[kPer][N];
   load_w(a.w, a.d, lane, kLanes, w);
+  Place<T, kLanes == 8> l[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) l[k] = place<T, kLanes == 8>(N * (lane + k * kLanes), a.d);
   // (kLanes >= 64: all lanes of a wave, so all waves of a workgroup, share a row)
   for (uint32_t row = blockIdx.x * kGroups + threadIdx.x / kLanes; row < a.n; row += gridDim.x * kGroups) {
     float h[kPer][N];
@@ -120,18 +123,17 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
     Chunk in[kPer], rin[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const int c = N * (lane + k * kLanes);
-      in[k] = fetch(x + c, a.d - c);
+      in[k] = fetch(x, l[k]);
     }
     if (a.R) {
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const int c = N * (lane + k * kLanes);
-        rin[k] = fetch(res + c, a.d - c);
+        rin[k] = fetch(res, l[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
+      in[k] = settle(in[k], l[k]);
       if (kDrop) drop<T>(in[k], (uint32_t)(N * (lane + k * kLanes)), row, a.m);
       widen<T>(in[k], h[k]);
     }
@@ -139,6 +141,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
         float v[N];
+        rin[k] = settle(rin[k], l[k]);
         widen<T>(rin[k], v);
 #pragma unroll
         for (int i = 0; i < N; ++i) h[k][i] = kDrop ? fmaf(h[k][i], a.m.keep, v[i]) : h[k][i] + v[i];
@@ -222,6 +225,9 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
   int turn = 0;
   float w[kPer][N], dw[kPer][N];
   load_w(a.w, a.d, lane, kLanes, w);
+  Place<T, kLanes == 8> l[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) l[k] = place<T, kLanes == 8>(N * (lane + k * kLanes), a.d);
 #pragma unroll
   for (int k = 0; k < kPer; ++k)
 #pragma unroll
@@ -232,19 +238,19 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     Chunk hin[kPer], gin[kPer], rin[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const int c = N * (lane + k * kLanes);
-      hin[k] = fetch(a.H + (int64_t)row * a.ldh + c, a.d - c);
-      gin[k] = fetch(a.dY + (int64_t)row * a.lddy + c, a.d - c);
+      hin[k] = fetch(a.H + (int64_t)row * a.ldh, l[k]);
+      gin[k] = fetch(a.dY + (int64_t)row * a.lddy, l[k]);
     }
     if (a.dR) {
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const int c = N * (lane + k * kLanes);
-        rin[k] = fetch(a.dR + (int64_t)row * a.lddr + c, a.d - c);
+        rin[k] = fetch(a.dR + (int64_t)row * a.lddr, l[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
+      hin[k] = settle(hin[k], l[k]);
+      gin[k] = settle(gin[k], l[k]);
       widen<T>(hin[k], h[k]);
       widen<T>(gin[k], g[k]);
     }
@@ -271,6 +277,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
       if (c >= a.d) continue;
       if (a.dR) {
         float v[N];
+        rin[k] = settle(rin[k], l[k]);
         widen<T>(rin[k], v);
 #pragma unroll
         for (int i = 0; i < N; ++i) h[k][i] += v[i];

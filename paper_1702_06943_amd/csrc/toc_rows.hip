@@ -34,8 +34,10 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(const Id *__restrict__ ids
                                                       Mask m, uint32_t row0, uint32_t total,
                                                       int d, Divisor chunks, T *out, int64_t ldo) {
   constexpr int P = kPer<Id>;
+  constexpr bool same = std::is_same<Id, Same>::value;
   const uint32_t o0 = blockIdx.x * (uint32_t)(kBlock * P) + threadIdx.x;
   uint32_t row[P], at[P];
+  Place<T, true> l[P];
   int64_t from[P];
   Chunk in[P];
 #pragma unroll
@@ -46,14 +48,17 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(const Id *__restrict__ ids
   }
 #pragma unroll
   for (int k = 0; k < P; ++k) {
-    const int c = (int)at[k] * kCols<T>;
-    in[k] = fetch(src + (from[k] >= 0 ? from[k] : 0) * lds + c, from[k] >= 0 ? d - c : 0);
+    // (a row of zeros: nothing is read but some row of the table, or none of an empty one)
+    l[k] = place<T, true>(from[k] >= 0 ? (int)at[k] * kCols<T> : d, d);
+    if (same || n_vocab > 0) in[k] = fetch(src + (from[k] >= 0 ? from[k] : 0) * lds, l[k]);
+    else in[k] = Chunk{0u, 0u, 0u, 0u};
   }
 #pragma unroll
   for (int k = 0; k < P; ++k) {
     if (o0 + (uint32_t)(k * kBlock) >= total) continue;
     const int c = (int)at[k] * kCols<T>;
     float v[kCols<T>];
+    in[k] = settle(in[k], l[k]);
     if (kDrop) drop<T>(in[k], (uint32_t)c, row0 + row[k], m);
     widen<T>(in[k], v);
 #pragma unroll

@@ -127,48 +127,65 @@ inline uint32_t chunks_of(int32_t d) {
 
 // Rows start wherever the caller's strides put them, so a chunk is aligned to its elements
 // only; the hardware takes 16-byte loads and stores at such addresses.
-struct Chunk {
-  uint32_t w[4];
-};
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) PackedChunk {
-  Chunk c;
-};
-typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t Words2 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
+typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
 
-// Columns 0..left-1 (at most a chunk's) as they are stored, the others 0.  Nothing here uses
-// what is loaded, so that the loads of several chunks can fly together.
-template <typename T>
-__device__ inline Chunk fetch(const T *p, int left) {
-  Chunk c;
-  if (left >= kCols<T>) {
-    c = ((const PackedChunk<T> *)p)->c;
-  } else {
+// Where a lane reads its chunk of a row of d columns, from column c on: the last chunk of a
+// row is read as the row's last 16 bytes and shifted down, so that all lanes' loads are one
+// instruction without a branch.  Rows shorter than a chunk are read by the element; kTiny
+// says whether there can be such.
+template <typename T, bool kTiny>
+struct Place {
+  int at, shift;      // first column read; columns to shift down by, kCols: nothing is left
+  int tiny;           // 0, or the row's columns
+};
+template <typename T, bool kTiny>
+__device__ inline Place<T, kTiny> place(int c, int d) {
+  if (kTiny && d < kCols<T>) return Place<T, kTiny>{0, c < d ? 0 : kCols<T>, d};
+  const int shift = min(max(c + kCols<T> - d, 0), kCols<T>);
+  return Place<T, kTiny>{shift < kCols<T> ? c - shift : 0, shift, 0};
+}
+
+// The chunk as it lies in memory.  Nothing here uses what is loaded, so that the loads of
+// several chunks can fly together; settle() comes before its use.
+template <typename T, bool kTiny>
+__device__ inline Chunk fetch(const T *row, const Place<T, kTiny> &l) {
+  if (!kTiny || !l.tiny) return *(const Unaligned *)(row + l.at);
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c.w[i] = 0u;
-#pragma unroll
-    for (int i = 0; i < kCols<T> - 1; ++i) {
-      if (i >= left) continue;
-      if (sizeof(T) == 4) c.w[i] = ((const uint32_t *)p)[i];
-      else c.w[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
-    }
+  for (int i = 0; i < kCols<T> - 1; ++i) {
+    if constexpr (sizeof(T) == 4) w[i] = i < l.tiny ? ((const uint32_t *)row)[i] : 0u;
+    else w[i / 2] |= (i < l.tiny ? (uint32_t)((const uint16_t *)row)[i] : 0u) << (16 * (i % 2));
+  }
+  return Chunk{w[0], w[1], w[2], w[3]};
+}
+
+// The lane's own columns first, 0 in those past the row's end.
+template <typename T, bool kTiny>
+__device__ inline Chunk settle(Chunk c, const Place<T, kTiny> &l) {
+  if (l.shift) {
+    const int bits = l.shift * 8 * (int)sizeof(T);
+    if (bits & 64) c = Chunk{c[2], c[3], 0u, 0u};
+    if (bits & 32) c = Chunk{c[1], c[2], c[3], 0u};
+    if (sizeof(T) == 2 && (bits & 16))
+      c = Chunk{c[0] >> 16 | c[1] << 16, c[1] >> 16 | c[2] << 16, c[2] >> 16 | c[3] << 16, c[3] >> 16};
+    if (bits & 128) c = Chunk{0u, 0u, 0u, 0u};
   }
   return c;
 }
 
 template <typename T>
-__device__ inline void widen(const Chunk &c, float (&v)[kCols<T>]) {
+__device__ inline void widen(Chunk c, float (&v)[kCols<T>]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 4) {
-      v[i] = __uint_as_float(c.w[i]);
+      v[i] = __uint_as_float(c[i]);
     } else if constexpr (std::is_same<T, bf16>::value) {
-      v[2 * i] = __uint_as_float(c.w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(c.w[i] & 0xffff0000u);
+      v[2 * i] = __uint_as_float(c[i] << 16);
+      v[2 * i + 1] = __uint_as_float(c[i] & 0xffff0000u);
     } else {
-      v[2 * i] = (float)__builtin_bit_cast(T, (uint16_t)c.w[i]);
-      v[2 * i + 1] = (float)__builtin_bit_cast(T, (uint16_t)(c.w[i] >> 16));
+      v[2 * i] = (float)__builtin_bit_cast(T, (uint16_t)c[i]);
+      v[2 * i + 1] = (float)__builtin_bit_cast(T, (uint16_t)(c[i] >> 16));
     }
   }
 }
@@ -183,7 +200,12 @@ __device__ inline void load(const T *p, int left, float (&v)[N]) {
 #pragma unroll
   for (int j = 0; j < N; j += kCols<T>) {
     float x[kCols<T>];
-    widen<T>(fetch(p + j, left - j), x);
+    if (left - j >= kCols<T>) {
+      widen<T>(*(const Unaligned *)(p + j), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCols<T>; ++i) x[i] = i < left - j ? (float)p[j + i] : 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < kCols<T>; ++i) v[j + i] = x[i];
   }
@@ -196,35 +218,38 @@ __device__ inline Chunk narrow(const float *v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 4) {
-      c.w[i] = __float_as_uint(v[i]);
+      c[i] = __float_as_uint(v[i]);
     } else {
       typedef T TwoT __attribute__((ext_vector_type(2)));
       const Two x = {v[2 * i], v[2 * i + 1]};
-      c.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, TwoT));
+      c[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, TwoT));
     }
   }
   return c;
 }
 
-template <typename T>
-__device__ inline void put(T *p, int left, const Chunk &c) {
+template <typename T, bool kStream = true>
+__device__ inline void put(T *p, int left, Chunk c) {
   if (left >= kCols<T>) {
-    const Words4 x = {c.w[0], c.w[1], c.w[2], c.w[3]};
-    __builtin_nontemporal_store(x, (Words4 *)p);
+    if (kStream) __builtin_nontemporal_store((Unaligned)c, (Unaligned *)p);
+    else *(Unaligned *)p = c;
   } else {
 #pragma unroll
     for (int i = 0; i < kCols<T> - 1; ++i) {
       if (i >= left) continue;
-      if (sizeof(T) == 4) ((uint32_t *)p)[i] = c.w[i];
-      else ((uint16_t *)p)[i] = (uint16_t)(c.w[i / 2] >> (16 * (i % 2)));
+      if (sizeof(T) == 4) ((uint32_t *)p)[i] = c[i];
+      else ((uint16_t *)p)[i] = (uint16_t)(c[i / 2] >> (16 * (i % 2)));
     }
   }
 }
 
+// A lane's N columns in more than one chunk lie 32 bytes from its neighbour's: those stores
+// have to meet in the cache (non-temporal, a gradient of 131,072 distinct bf16 rows of 1,024
+// into binary32 took 479 us, TODO with these).
 template <typename T, int N>
 __device__ inline void store(T *p, int left, const float (&v)[N]) {
 #pragma unroll
-  for (int j = 0; j < N; j += kCols<T>) put(p + j, left - j, narrow<T>(v + j));
+  for (int j = 0; j < N; j += kCols<T>) put<T, N == kCols<T>>(p + j, left - j, narrow<T>(v + j));
 }
 
 struct E4m3 {
@@ -287,10 +312,10 @@ __device__ inline void drop(Chunk &x, uint32_t c, uint32_t row, const Mask &m) {
   if constexpr (sizeof(T) == 4) {
     const bool high = c & 4u;
     const uint32_t lo = high ? u[2] : u[0], hi = high ? u[3] : u[1];
-    x.w[0] = (lo & 0xffffu) > m.last ? x.w[0] : 0u;
-    x.w[1] = (lo >> 16) > m.last ? x.w[1] : 0u;
-    x.w[2] = (hi & 0xffffu) > m.last ? x.w[2] : 0u;
-    x.w[3] = (hi >> 16) > m.last ? x.w[3] : 0u;
+    x[0] = (lo & 0xffffu) > m.last ? x[0] : 0u;
+    x[1] = (lo >> 16) > m.last ? x[1] : 0u;
+    x[2] = (hi & 0xffffu) > m.last ? x[2] : 0u;
+    x[3] = (hi >> 16) > m.last ? x[3] : 0u;
   } else {
     typedef int16_t Two __attribute__((ext_vector_type(2)));
     const Two limit = __builtin_bit_cast(Two, m.limit);
@@ -298,7 +323,7 @@ __device__ inline void drop(Chunk &x, uint32_t c, uint32_t row, const Mask &m) {
     for (int i = 0; i < 4; ++i) {
       const Two word = __builtin_bit_cast(Two, u[i] ^ 0x80008000u);
       const Two kept = __builtin_elementwise_sub_sat(limit, word) >> 15;
-      x.w[i] &= __builtin_bit_cast(uint32_t, kept);
+      x[i] &= __builtin_bit_cast(uint32_t, kept);
     }
   }
 }
