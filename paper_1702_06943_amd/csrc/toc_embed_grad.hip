@@ -31,7 +31,8 @@ constexpr int kSumBlock = 512;
 constexpr uint32_t kMinSpan = 8, kMaxSpan = 32;   // entries of a span
 constexpr int kAhead = 8;                    // entries whose rows' loads fly together
 constexpr int kJoinBlock = 256;
-constexpr int kZeroPer = 4;                  // chunks a thread of the zero workgroups writes
+constexpr uint32_t kZeroRows = 256;          // most rows of dE that a workgroup looks up at a time
+constexpr uint32_t kZeroChunks = 4096;       // ... of about so many chunks
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr int32_t kMaxGradCols = 1 << 20;
 
@@ -117,10 +118,10 @@ __device__ inline uint32_t key_of(const Id *ids, uint32_t i, uint32_t n_vocab) {
 
 // --- zero ----------------------------------------------------------------------
 
-// Chunks first .. first + count - 1 of dE, counted row by row.  keys NULL: all of them are
-// written.  Else those of rows whose number does not occur: count_kernel left in slot[v] some
-// token of number v if there is one, and whatever else a slot holds is no such token, since
-// the token's own number is looked up again (so the slots need no clearing).
+// Rows row0 .. row0 + rows - 1 of dE, `per` of them at a time by a workgroup.  keys NULL: all
+// of them are written.  Else those whose number does not occur: count_kernel left in slot[v]
+// some token of number v if there is one, and whatever else a slot holds is no such token,
+// since the token's own number is looked up again (so the slots need no clearing).
 template <typename TO>
 struct ZeroArgs {
   TO *dE;
@@ -129,34 +130,34 @@ struct ZeroArgs {
   Divisor chunks;
   const uint32_t *slot, *keys;
   uint32_t n;
-  int64_t row0;            // the row of chunk 0
-  uint32_t first, count;
+  int64_t row0, rows;
+  uint32_t per, blocks;
 };
 
 template <int kBlock, typename TO>
 __device__ inline void zero_rows(const ZeroArgs<TO> &z, uint32_t block) {
+  __shared__ uint32_t absent[kZeroRows], n_absent;
   const Chunk zero = {0u, 0u, 0u, 0u};
-  const uint32_t o0 = block * (uint32_t)(kBlock * kZeroPer) + threadIdx.x;
-  uint32_t row[kZeroPer], at[kZeroPer], t[kZeroPer], key[kZeroPer];
-#pragma unroll
-  for (int k = 0; k < kZeroPer; ++k) {
-    const uint32_t o = o0 + (uint32_t)(k * kBlock);
-    row[k] = divide(z.first + (o < z.count ? o : 0u), z.chunks, &at[k]);
-    t[k] = z.keys ? z.slot[z.row0 + row[k]] : kNone;
-  }
-#pragma unroll
-  for (int k = 0; k < kZeroPer; ++k) key[k] = t[k] < z.n ? z.keys[t[k]] : kNone;
-#pragma unroll
-  for (int k = 0; k < kZeroPer; ++k) {
-    if (o0 + (uint32_t)(k * kBlock) >= z.count) return;
-    if ((int64_t)key[k] == z.row0 + row[k]) continue;
-    const int c = (int)at[k] * kCols<TO>;
-    put(z.dE + (z.row0 + row[k]) * z.lde + c, z.d - c, zero);
+  for (int64_t r0 = (int64_t)block * z.per; r0 < z.rows; r0 += (int64_t)z.blocks * z.per) {
+    if (threadIdx.x == 0) n_absent = 0u;
+    __syncthreads();
+    if (threadIdx.x < z.per && r0 + threadIdx.x < z.rows) {
+      const int64_t row = z.row0 + r0 + threadIdx.x;
+      const uint32_t t = z.keys ? z.slot[row] : kNone;
+      // (their order in the list does not matter)
+      if (!(t < z.n && (int64_t)z.keys[t] == row)) absent[atomicAdd(&n_absent, 1u)] = threadIdx.x;
+    }
+    __syncthreads();
+    const uint32_t total = n_absent * z.chunks.d;
+    for (uint32_t o = threadIdx.x; o < total; o += kBlock) {
+      uint32_t at;
+      const uint32_t i = divide(o, z.chunks, &at);
+      const int c = (int)at * kCols<TO>;
+      put(z.dE + (z.row0 + r0 + absent[i]) * z.lde + c, z.d - c, zero);
+    }
+    __syncthreads();
   }
 }
-
-template <int kBlock>
-uint32_t zero_blocks(uint32_t count) { return (count + kBlock * kZeroPer - 1) / (kBlock * kZeroPer); }
 
 template <typename TO>
 __global__ __launch_bounds__(256) void zero_kernel(ZeroArgs<TO> z) {
@@ -596,55 +597,35 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t
 
 // --- launches -----------------------------------------------------------------------
 
-// dE's rows that a call has to write zeros to, handed out to its launches.  Rows go in slabs of
-// fewer than 2^31 chunks; all but the last slab get launches of their own.
+// dE's rows that a call has to write zeros to, handed out to its launches.
 template <typename TO>
 struct Zeros {
   ZeroArgs<TO> z;
-  uint32_t left = 0;
-  hipStream_t s;
+  int64_t left;
 
   // keys: the tokens' numbers if the slots tell the rows that occur, or NULL
   Zeros(TO *dE, int64_t lde, int64_t n_vocab, int32_t d, const uint32_t *slot, const uint32_t *keys,
-        int64_t n, hipStream_t stream)
-      : s(stream) {
+        int64_t n)
+      : left(n_vocab) {
     const uint32_t chunks = chunks_of<TO>(d);
-    z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, (uint32_t)n, 0, 0, 0};
-    slab = ((int64_t)1 << 30) / chunks;
-    rows = n_vocab;
-    left = (uint32_t)(std::min(slab, rows) * chunks);
+    z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, (uint32_t)n, 0, 0,
+                     std::max(1u, std::min(kZeroRows, kZeroChunks / chunks)), 0};
   }
-  // The next `most` chunks at most.
-  ZeroArgs<TO> take(uint32_t most) {
+  // Rows for the next `most` chunks, about, and workgroups for them.
+  ZeroArgs<TO> take(int64_t most) {
     ZeroArgs<TO> t = z;
-    t.count = std::min(most, left);
-    z.first += t.count;
-    left -= t.count;
+    t.rows = std::min(left, most / t.chunks.d + 1);
+    t.blocks = (uint32_t)std::min<int64_t>((t.rows + t.per - 1) / t.per, 1 << 17);
+    z.row0 += t.rows;
+    left -= t.rows;
     return t;
   }
-  // Launches of their own for what is left, but for the first slab's when keep is set.
-  void rest(bool keep) {
-    int64_t r = slab;
-    if (!keep) launch(take(left));
-    for (; r < rows; r += slab) {
-      ZeroArgs<TO> t = z;
-      t.row0 = r;
-      t.first = 0;
-      t.count = (uint32_t)(std::min(slab, rows - r) * t.chunks.d);
-      launch(t);
-    }
-  }
-
- private:
-  int64_t slab, rows;
-  void launch(const ZeroArgs<TO> &t) {
-    if (t.count) hipLaunchKernelGGL(zero_kernel<TO>, dim3(zero_blocks<256>(t.count)), dim3(256), 0, s, t);
-  }
+  ZeroArgs<TO> rest() { return take(left * z.chunks.d); }
 };
 
 // What a sort launch writes beside its own work (24 MB): it takes some 4 us, in which the
 // chip writes that much.
-constexpr uint32_t kBeside = 3 << 19;
+constexpr int64_t kBeside = 3 << 19;
 
 template <typename TO, typename Id>
 void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool slots, uint8_t *ws,
@@ -666,7 +647,7 @@ void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool
     if (total)
       hipLaunchKernelGGL(scan_kernel, dim3(1u << p.bits), dim3(256), 0, s, count, p.tiles, p.bits, total);
     const ZeroArgs<TO> z = zeros.take(kBeside);
-    hipLaunchKernelGGL(scatter_kernel<TO>, dim3(p.tiles + zero_blocks<kSortBlock>(z.count)), dim3(kSortBlock),
+    hipLaunchKernelGGL(scatter_kernel<TO>, dim3(p.tiles + z.blocks), dim3(kSortBlock),
                        0, s, kin, pin, n, p.tiles, shift, p.bits, count, total, kout, pout, z);
   }
 }
@@ -676,20 +657,19 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
                 int64_t ldg, float scale, const toc_drop *drop, TO *dE, int64_t lde, bool accumulate,
                 uint8_t *ws, hipStream_t s) {
   Zeros<TO> zeros(dE, lde, accumulate ? 0 : n_vocab, d, (const uint32_t *)(ws + p.slot),
-                  n > 0 && !p.small ? (const uint32_t *)(ws + p.orig) : nullptr, n, s);
+                  n > 0 && !p.small ? (const uint32_t *)(ws + p.orig) : nullptr, n);
   if (n == 0) {
-    zeros.rest(false);
+    const ZeroArgs<TO> z = zeros.rest();
+    if (z.blocks) hipLaunchKernelGGL(zero_kernel<TO>, dim3(z.blocks), dim3(256), 0, s, z);
     return launched("zero_kernel");
   }
   if (p.small) {
-    zeros.rest(true);
-    const ZeroArgs<TO> z = zeros.take(zeros.left);
-    hipLaunchKernelGGL((small_kernel<TO, Id>), dim3(1 + zero_blocks<kSortBlock>(z.count)), dim3(kSortBlock), 0,
-                       s, ids, (uint32_t)n, (uint32_t)n_vocab, p.bits, p.passes,
-                       (uint32_t *)(ws + p.key[0]), (uint32_t *)(ws + p.pos[0]), z);
+    const ZeroArgs<TO> z = zeros.rest();
+    hipLaunchKernelGGL((small_kernel<TO, Id>), dim3(1 + z.blocks), dim3(kSortBlock), 0, s, ids, (uint32_t)n,
+                       (uint32_t)n_vocab, p.bits, p.passes, (uint32_t *)(ws + p.key[0]),
+                       (uint32_t *)(ws + p.pos[0]), z);
   } else {
     sort_tiles(p, (uint32_t)n, ids, (uint32_t)n_vocab, !accumulate, ws, zeros, s);
-    zeros.rest(true);
   }
   const Mask m = mask_of(drop);
   const int last = p.small ? 0 : (p.passes - 1) % 2;
@@ -699,8 +679,8 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
                (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), d, lanes,
                __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
   const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
-  const ZeroArgs<TO> z = zeros.take(zeros.left);
-  const dim3 grid(a.blocks + (zero_blocks<kSumBlock>(z.count) + slices - 1) / slices, slices);
+  const ZeroArgs<TO> z = zeros.rest();
+  const dim3 grid(a.blocks + (z.blocks + slices - 1) / slices, slices);
 #define TOC_SUM(L)                                                                                      \
   if (lanes == L) {                                                                                      \
     if (m.on)                                                                                            \
