@@ -402,6 +402,7 @@ template <typename T>
 struct SumArgs {
   const uint32_t *key, *pos;
   uint32_t n, n_vocab, blocks;   // workgroups along the list
+  Divisor slices;                // and along the columns
   int d, lanes, shift;           // lanes = 1 << shift
   uint32_t span;                 // entries of a group of lanes
   const T *G;
@@ -425,8 +426,9 @@ __device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, in
   store(p, left, v);
 }
 
-// Workgroups 0 .. a.blocks-1 of a slice (blockIdx.y) of kLanes chunks of the columns: group g
-// walks entries (blockIdx.x groups + g) span onwards.  The others write zeros.  A group's
+// Workgroup b of the first a.blocks slices: slice b mod slices of kLanes chunks of the columns
+// (neighbours read and write the same rows), entries of the list (b / slices groups + g) span
+// onwards for group g.  The other workgroups write zeros.  A group's
 // lanes hold its entries' numbers and tokens between them, so that the rows' loads wait for
 // nothing but each other: kAhead of them are always under way.
 template <typename T, typename TO, int kLanes, bool kDrop>
@@ -437,16 +439,18 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
   constexpr int kHold = ((int)kMaxSpan + kLanes - 1) / kLanes;
   __shared__ float heads[kSumBlock][N];          // each group's part of a number from before
   __shared__ uint8_t through[kGroups];           // ... which goes on after the group
-  if (blockIdx.x >= a.blocks) {
-    zero_rows<kSumBlock>(z, (blockIdx.x - a.blocks) * gridDim.y + blockIdx.y);
+  uint32_t slice;
+  const uint32_t block = divide(blockIdx.x, a.slices, &slice);
+  if (block >= a.blocks) {
+    zero_rows<kSumBlock>(z, blockIdx.x - a.blocks * a.slices.d);
     return;
   }
   uint32_t group = threadIdx.x / kLanes;
   if (kLanes == 64) group = __builtin_amdgcn_readfirstlane(group);
   const int lane = threadIdx.x % kLanes;
-  const int c = (int)(blockIdx.y * kLanes + lane) * N, left = a.d - c;
+  const int c = (int)(slice * kLanes + lane) * N, left = a.d - c;
   const Place<T, kLanes == 8> l = place<T, kLanes == 8>(c, a.d);
-  const uint32_t e0 = (uint32_t)min(((uint64_t)blockIdx.x * kGroups + group) * a.span, (uint64_t)a.n);
+  const uint32_t e0 = (uint32_t)min(((uint64_t)block * kGroups + group) * a.span, (uint64_t)a.n);
   const uint32_t entries = min(a.n - e0, a.span);
   uint32_t keys[kHold], tokens[kHold];
 #pragma unroll
@@ -481,38 +485,42 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
   const uint32_t start = cur;
   const bool begun = entries && prev == cur;     // the first number is from before
   bool from_before = begun;
+  auto step = [&](int u, int j) {
+    const uint32_t key = of(keys, u);
+    if (u >= (int)entries) return;
+    if (key != cur) {
+      if (from_before) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
+      } else if (left > 0) {                     // (cur < V: a larger number sorts after it)
+        write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+      }
+      cur = key;
+      from_before = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+    }
+    Chunk x = settle(in[j], l);
+    float v[N];
+    if (kDrop) drop<T>(x, (uint32_t)c, at[j], a.m);
+    widen<T>(x, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] += v[i];
+  };
+  // (the loads under way are the same on every path through the loop, so that a step waits
+  // for its own and not for all)
+  int u0 = 0;
 #pragma unroll 1
-  for (int u0 = 0; u0 < (int)a.span; u0 += kAhead) {
+  for (; u0 + kAhead < (int)a.span; u0 += kAhead) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int u = u0 + j;
-      const uint32_t key = of(keys, u);
-      if (u < (int)entries) {
-        if (key != cur) {
-          if (from_before) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
-          } else if (left > 0) {                 // (cur < V: a larger number sorts after it)
-            write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
-          }
-          cur = key;
-          from_before = false;
-#pragma unroll
-          for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-        }
-        Chunk x = settle(in[j], l);
-        float v[N];
-        if (kDrop) drop<T>(x, (uint32_t)c, at[j], a.m);
-        widen<T>(x, v);
-#pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] += v[i];
-      }
-      if (u0 + kAhead < (int)a.span) {
-        at[j] = of(tokens, u + kAhead);
-        in[j] = fetch(a.G + (int64_t)at[j] * a.ldg, l);
-      }
+      step(u0 + j, j);
+      at[j] = of(tokens, u0 + j + kAhead);
+      in[j] = fetch(a.G + (int64_t)at[j] * a.ldg, l);
     }
   }
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) step(u0 + j, j);
   const bool goes_on = entries && next == cur;
   if (from_before) {
 #pragma unroll
@@ -532,7 +540,7 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
     for (uint32_t g = 0; g + 1 < kGroups && through[g]; ++g)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += heads[(g + 1) * kLanes + lane][i];
-    store(a.part + (int64_t)blockIdx.x * 2 * a.d + c, left, v);
+    store(a.part + (int64_t)block * 2 * a.d + c, left, v);
   }
   if (goes_on && !from_before && cur < a.n_vocab) {
     uint32_t g = group + 1;
@@ -542,26 +550,27 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
       for (int i = 0; i < N; ++i) acc[i] += heads[g * kLanes + lane][i];
       open = through[g];
     }
-    if (open) store(a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d + c, left, acc);
+    if (open) store(a.part + ((int64_t)block * 2 + 1) * a.d + c, left, acc);
     else write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
   }
 }
 
-// The row of a number that begins in workgroup blockIdx.x's entries and goes on after them: its
-// part there, then those of the workgroups that follow, split over this one's groups of lanes.
+// The row of a number that begins in a workgroup's entries and goes on after them: its part there, then those of the workgroups that follow, split over this one's groups of lanes.
 template <typename T, typename TO>
 __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t span,
                                                           TO *__restrict__ dE, int64_t lde) {
   constexpr int N = kCols<T>;
   __shared__ float sums[kJoinBlock][N];
-  const uint32_t e0 = blockIdx.x * span, e1 = e0 + span;          // (the last one has no later)
+  uint32_t slice;
+  const uint32_t block = divide(blockIdx.x, a.slices, &slice);
+  const uint32_t e0 = block * span, e1 = e0 + span;          // (the last one has no later)
   const uint32_t key = a.key[e1 - 1], next = a.key[e1], head = a.key[e0];
   const uint32_t prev = e0 > 0 ? a.key[e0 - 1] : kNone;
   if (key >= a.n_vocab || next != key || (head == key && prev == key)) return;
   // one part in each later workgroup up to the first whose last entry is another number
   uint32_t parts = 0;
   for (bool more = true; more;) {
-    const uint32_t b = blockIdx.x + 1 + parts + threadIdx.x % 64;
+    const uint32_t b = block + 1 + parts + threadIdx.x % 64;
     const uint64_t end = ((uint64_t)b + 1) * span;
     const bool full = b < a.blocks && end < a.n && a.key[end - 1] == key && a.key[end] == key;
     const uint64_t stop = ~__ballot(full);
@@ -569,18 +578,18 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t
     parts += more ? 64 : (uint32_t)__builtin_ctzll(stop) + 1;
   }
   const uint32_t groups = kJoinBlock >> a.shift, group = threadIdx.x >> a.shift;
-  const int c = (int)(blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * N, left = a.d - c;
+  const int c = (int)(slice * a.lanes + (threadIdx.x & (a.lanes - 1))) * N, left = a.d - c;
   const uint32_t per = (parts + groups - 1) / groups;
   float acc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.0f;
   if (left > 0) {
-    if (group == 0) load((const float *)a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d + c, left, acc);
+    if (group == 0) load((const float *)a.part + ((int64_t)block * 2 + 1) * a.d + c, left, acc);
     const uint32_t q1 = min(parts, (group + 1) * per);
 #pragma unroll 4
     for (uint32_t q = group * per; q < q1; ++q) {
       float v[N];
-      load((const float *)a.part + ((int64_t)(blockIdx.x + 1 + q) * 2) * a.d + c, left, v);
+      load((const float *)a.part + ((int64_t)(block + 1 + q) * 2) * a.d + c, left, v);
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] += v[i];
     }
@@ -623,13 +632,15 @@ struct Zeros {
   ZeroArgs<TO> rest() { return take(left * z.chunks.d); }
 };
 
-// What a sort launch writes beside its own work (24 MB): it takes some 4 us, in which the
-// chip writes that much.
-constexpr int64_t kBeside = 3 << 19;
+// Chunks that a sort launch writes beside its own work, which takes some 5 us and little of the
+// chip: 24 MB, or 48 MB where the sums read more than 64 MB and would be held up by what is
+// left to them (us with 0, 24, 48 MB: 18,750 x 300 f32 42.8, 37.2, 40.0; 65,536 x 1,024 bf16
+// 80.4, 75.4, 71.0; 131,072 x 1,024 144.5, 136.2, 134.0).
+int64_t beside(int64_t read_bytes) { return (read_bytes > 64 << 20 ? 2 : 1) * ((int64_t)3 << 19); }
 
 template <typename TO, typename Id>
 void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool slots, uint8_t *ws,
-                Zeros<TO> &zeros, hipStream_t s) {
+                Zeros<TO> &zeros, int64_t zero_chunks, hipStream_t s) {
   uint32_t *count = (uint32_t *)(ws + p.count), *orig = (uint32_t *)(ws + p.orig);
   uint32_t *total = p.tiles > kFewTiles ? (uint32_t *)(ws + p.total) : nullptr;
   uint32_t *slot = slots ? (uint32_t *)(ws + p.slot) : nullptr;
@@ -646,7 +657,7 @@ void sort_tiles(const Plan &p, uint32_t n, const Id *ids, uint32_t n_vocab, bool
                          n_vocab, shift, p.bits, count, (uint32_t *)nullptr, (uint32_t *)nullptr);
     if (total)
       hipLaunchKernelGGL(scan_kernel, dim3(1u << p.bits), dim3(256), 0, s, count, p.tiles, p.bits, total);
-    const ZeroArgs<TO> z = zeros.take(kBeside);
+    const ZeroArgs<TO> z = zeros.take(zero_chunks);
     hipLaunchKernelGGL(scatter_kernel<TO>, dim3(p.tiles + z.blocks), dim3(kSortBlock),
                        0, s, kin, pin, n, p.tiles, shift, p.bits, count, total, kout, pout, z);
   }
@@ -669,18 +680,19 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
                        (uint32_t)n_vocab, p.bits, p.passes, (uint32_t *)(ws + p.key[0]),
                        (uint32_t *)(ws + p.pos[0]), z);
   } else {
-    sort_tiles(p, (uint32_t)n, ids, (uint32_t)n_vocab, !accumulate, ws, zeros, s);
+    sort_tiles(p, (uint32_t)n, ids, (uint32_t)n_vocab, !accumulate, ws, zeros,
+               beside(n * d * (int64_t)sizeof(T)), s);
   }
   const Mask m = mask_of(drop);
   const int last = p.small ? 0 : (p.passes - 1) % 2;
   const uint32_t span = block_span<T>(n, d);
   const int lanes = lanes_of(chunks_of<T>(d));
+  const uint32_t slices = (chunks_of<T>(d) + lanes - 1) / lanes;
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
-               (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), d, lanes,
+               (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), divisor(slices), d, lanes,
                __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
-  const unsigned slices = (unsigned)((chunks_of<T>(d) + a.lanes - 1) / a.lanes);
   const ZeroArgs<TO> z = zeros.rest();
-  const dim3 grid(a.blocks + (z.blocks + slices - 1) / slices, slices);
+  const dim3 grid(a.blocks * slices + z.blocks);
 #define TOC_SUM(L)                                                                                      \
   if (lanes == L) {                                                                                      \
     if (m.on)                                                                                            \
@@ -691,7 +703,7 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
   TOC_SUM(8) TOC_SUM(16) TOC_SUM(32) TOC_SUM(64)
 #undef TOC_SUM
   if (a.blocks > 1)
-    hipLaunchKernelGGL((join_kernel<T, TO>), dim3(a.blocks - 1, slices), dim3(kJoinBlock), 0, s, a, span, dE,
+    hipLaunchKernelGGL((join_kernel<T, TO>), dim3((a.blocks - 1) * slices), dim3(kJoinBlock), 0, s, a, span, dE,
                        lde);
   return launched("embed gradient kernels");
 }
