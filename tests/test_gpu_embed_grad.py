@@ -214,3 +214,64 @@ def test_binding_refusals():
     with pytest.raises(T.TocError) as e:
         T.toc_embed_grad(ids, G, dE, ws[:-16])
     assert e.value.status == T.TOC_ESIZE
+
+
+def gpu_check(ids, V, G, dE, scale=1.0, accumulated=None):
+    """dE against a float64 sum on the GPU (64-bit atomics: its own error is far below)."""
+    ok = (ids >= 0) & (ids < V)
+    at = torch.where(ok, ids, 0).long()
+    terms = torch.where(ok[:, None], G.double(), 0.0) * scale
+    want = torch.zeros(dE.shape, dtype=torch.float64, device=DEV).index_add_(0, at, terms)
+    S = torch.zeros(dE.shape, dtype=torch.float64, device=DEV).index_add_(0, at, terms.abs())
+    count = torch.zeros(V, dtype=torch.float64, device=DEV).index_add_(0, at, ok.double())
+    kind = {v: k for k, v in TYPES.items()}[dE.dtype]
+    tol = (count[:, None] + 6) * U * S + UNIT[kind] * want.abs() + LEAST[kind]
+    assert bool(((dE.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("n,V,d,out", [
+    (150001, 70000, 16, "f32"),      # more tiles than are summed without a scan
+    (150001, 300000, 8, "f32"),      # three passes
+    (70001, 60000, 512, "f32"),      # zeros beside both passes and the sums
+    (70001, 500, 520, "bf16"),       # every row occurs, two slices, frequent numbers
+    (4097, 100, 2000, "bf16"),       # the fewest tokens of the tiled sort
+    (4096, 5000, 48, "f32"),         # the most of the small one
+])
+def test_large_calls(n, V, d, out):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n + V)
+    law = torch.cumsum(torch.arange(1, V + 1, device=DEV, dtype=torch.float64) ** -1.1, 0)
+    ids = torch.searchsorted(law, torch.rand(n, generator=g, device=DEV, dtype=torch.float64) * law[-1])
+    ids = torch.where(torch.rand(n, generator=g, device=DEV) < 0.05, -1, ids)
+    G = torch.randn((n, d), generator=g, device=DEV).to(torch.bfloat16)
+    dE = blank(V, d, out)
+    run(ids, G, dE, 0.5)
+    gpu_check(ids, V, G, dE, 0.5)
+    again = blank(V, d, out)
+    run(ids.int(), G, again, 0.5)
+    assert torch.equal(dE, again)
+
+
+def test_more_rows_than_one_launch_looks_up():
+    """40 million table rows: the workgroups that write zeros take several runs of rows each."""
+    V, d = 40_000_000, 3
+    ids = on([0, 5, V - 1, 12_345_678, 5])
+    for n in (5, 5000):
+        more = torch.cat([ids, torch.full((n - 5,), -1, dtype=ids.dtype, device=DEV)])
+        dE = torch.full((V, d), 9.0, device=DEV)
+        run(more, torch.ones((n, d), device=DEV), dE, dirty=False)
+        assert float(dE.sum()) == 15.0
+        assert torch.equal(dE[ids], torch.tensor([1.0, 2, 1, 1, 2], device=DEV)[:, None].expand(5, d))
+
+
+def test_another_stream():
+    rng = np.random.default_rng(9)
+    ids, G = on(rng.integers(0, 900, 6000)), rows(rng, 6000, 72, "f32")[0]
+    want, dE = blank(900, 72, "f32"), blank(900, 72, "f32")
+    run(ids, G, want)
+    ws = torch.empty(T.toc_embed_grad_workspace_size(6000, 900, 72), dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    T.toc_embed_grad(ids, G, dE, ws, stream=side)
+    side.synchronize()
+    assert torch.equal(dE, want)

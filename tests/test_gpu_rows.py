@@ -173,3 +173,18 @@ def test_binding_refusals():
         with pytest.raises(T.TocError) as e:
             T.toc_dropout(E, E, drop)
         assert e.value.status == T.TOC_EINVAL
+
+
+def test_more_chunks_than_one_launch():
+    """17 million rows of 512 bfloat16 numbers, 2^30 chunks and more: the rows of later launches
+    have their own rows' masks."""
+    n, d, drop = (1 << 24) + 1001, 512, (0.5, 0x1234567, 3)
+    X = torch.ones((n, d), dtype=torch.bfloat16, device=DEV)
+    T.toc_dropout(X, X, T.Drop(*drop))
+    for row in (0, 1, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, n - 1):
+        q = np.arange(d // 8, dtype=np.uint64)
+        fill = [np.full(d // 8, v, np.uint64) for v in (row, drop[2] & 0xFFFFFFFF, drop[2] >> 32)]
+        words = R.philox4x32((q, *fill), (drop[1] & 0xFFFFFFFF, drop[1] >> 32))
+        kept = np.stack([words[j // 2] >> np.uint64(16 * (j % 2)) & np.uint64(0xFFFF) for j in range(8)], 1)
+        want = np.where(kept.reshape(-1) >= R.drop_below(drop[0]), 2.0, 0.0)
+        assert np.array_equal(host(X[row]), want), row
