@@ -2,8 +2,9 @@
 //   dE[v, :] (+)= scale * sum of drop(G)[t, :] over the tokens t with ids[t] = v
 // the left product G^T.A (Theorem 2) of tuples that hold one pair each, in a fixed order:
 //   sort   (number, token) pairs stably by number, 9 bits or fewer a pass; numbers outside
-//          the table sort last, as number V.  Up to 4,096 pairs in one workgroup's LDS, else
-//          in tiles: each tile's count of every digit, then each tile places its pairs
+//          the table sort last, as number V.  Up to 128 pairs by every workgroup of the sums
+//          for itself (one launch in all), up to 4,096 in one workgroup's LDS, else in tiles:
+//          each tile's count of every digit, then each tile places its pairs
 //   sum    the sorted list cut into spans of equal length, so that a frequent number costs
 //          no more than others: a group of lanes walks a span, its chunk of dE's row in
 //          registers, and writes a row when its number ends.  A number that crosses spans
@@ -30,6 +31,9 @@ constexpr uint32_t kFewTiles = 64;           // above, the tiles' counts are sum
 constexpr int kSumBlock = 512;
 constexpr uint32_t kMinSpan = 8, kMaxSpan = 32;   // entries of a span
 constexpr int kAhead = 8;                    // entries whose rows' loads fly together
+// Pairs that each workgroup of the sums sorts itself (us in one launch and with a sort before:
+// 20 x 100 bf16 7, 13; 75 x 333 f16 9, 13.5; 128 x 1,024 bf16 14.1, 16.5; 256 x 1,024 24.3, 16.9).
+constexpr uint32_t kTiny = 128;
 constexpr int kJoinBlock = 256;
 constexpr uint32_t kZeroRows = 256;          // most rows of dE that a workgroup looks up at a time
 constexpr uint32_t kZeroChunks = 4096;       // ... of about so many chunks
@@ -39,7 +43,7 @@ constexpr int32_t kMaxGradCols = 1 << 20;
 // The sort's shape, and where the workspace's parts lie (bytes).
 struct Plan {
   int bits, passes;       // digit bits of a pass
-  bool small;
+  bool tiny, small;
   uint32_t tiles;
   size_t orig, key[2], pos[2], count, total, slot, part, end;
 };
@@ -66,7 +70,12 @@ int lanes_of(uint32_t chunks) {
 // Entries of a span: the more, the fewer parts of rows are put together, as long as the chip
 // has some 4,096 waves (us for 8, 16, 32: 131,072 x 1,024 bf16 161, 151, 148; 131,072 x 512 f16
 // of 300 numbers 80, 68, 58; 100,000 x 64 f32 35.9, 36.6, 43.8; 4,000 x 256 bf16 21.5, 25.2, 31.3).
+// Up to kTiny pairs: so many that one workgroup walks them all.
 uint32_t span_of(int64_t n, uint32_t chunks) {
+  if (n <= (int64_t)kTiny) {
+    const uint32_t groups = (uint32_t)(kSumBlock / lanes_of(chunks));
+    return std::max<uint32_t>(kMinSpan, ((uint32_t)n + groups * kMinSpan - 1) / (groups * kMinSpan) * kMinSpan);
+  }
   const int64_t lanes = lanes_of(chunks), slices = (chunks + lanes - 1) / lanes;
   uint32_t span = kMaxSpan;
   while (span > kMinSpan && n / span * lanes * slices < 4096 * 64) span /= 2;
@@ -85,8 +94,9 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   while (width < 32 && ((int64_t)1 << width) <= n_vocab) ++width;
   p.passes = (width + kMaxBits - 1) / kMaxBits;
   p.bits = (width + p.passes - 1) / p.passes;
-  p.small = n <= (int64_t)kSmall;
-  p.tiles = p.small ? 0 : (uint32_t)((n + kTile - 1) / kTile);
+  p.tiny = n <= (int64_t)kTiny;
+  p.small = !p.tiny && n <= (int64_t)kSmall;
+  p.tiles = p.tiny || p.small ? 0 : (uint32_t)((n + kTile - 1) / kTile);
   const int64_t least = std::min(block_span<float>(n, d), block_span<bf16>(n, d));
   const int64_t blocks = (n + least - 1) / least;
   size_t at = 0;
@@ -95,15 +105,17 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
     at = align16(at + bytes);
     return here;
   };
-  p.orig = take(p.small ? 0 : (size_t)n * 4);
+  // (tiny sorts keep nothing here; their calls ask for it all the same, by one rule for all)
+  const bool one = p.tiny || p.small;
+  p.orig = take(one ? 0 : (size_t)n * 4);
   for (int i = 0; i < 2; ++i) {
     // (a small sort keeps all passes but the last in LDS)
-    p.key[i] = i == 0 || !p.small ? take((size_t)n * 4) : p.key[0];
-    p.pos[i] = i == 0 || !p.small ? take((size_t)n * 4) : p.pos[0];
+    p.key[i] = i == 0 || !one ? take((size_t)n * 4) : p.key[0];
+    p.pos[i] = i == 0 || !one ? take((size_t)n * 4) : p.pos[0];
   }
   p.count = take(((size_t)p.tiles << p.bits) * 4);
   p.total = take(p.tiles > kFewTiles ? (size_t)4 << p.bits : 0);
-  p.slot = take(p.small ? 0 : (size_t)n_vocab * 4);
+  p.slot = take(one ? 0 : (size_t)n_vocab * 4);
   p.part = take(blocks > 1 ? (size_t)blocks * 2 * (size_t)d * 4 : 0);
   p.end = at;
   return p;
@@ -116,12 +128,24 @@ __device__ inline uint32_t key_of(const Id *ids, uint32_t i, uint32_t n_vocab) {
   return id >= 0 && id < (int64_t)n_vocab ? (uint32_t)id : n_vocab;
 }
 
+// The token numbers of a call as they are, for the workgroups that sort up to kTiny of them;
+// ids NULL in other calls.
+struct TinyIds {
+  const void *ids;
+  int bits;
+  uint32_t n_vocab;
+};
+__device__ inline uint32_t key_of(const TinyIds &t, uint32_t i) {
+  return t.bits == 32 ? key_of((const int32_t *)t.ids, i, t.n_vocab) : key_of((const int64_t *)t.ids, i, t.n_vocab);
+}
+
 // --- zero ----------------------------------------------------------------------
 
 // Rows row0 .. row0 + rows - 1 of dE, `per` of them at a time by a workgroup.  keys NULL: all
 // of them are written.  Else those whose number does not occur: count_kernel left in slot[v]
 // some token of number v if there is one, and whatever else a slot holds is no such token,
-// since the token's own number is looked up again (so the slots need no clearing).
+// since the token's own number is looked up again (so the slots need no clearing).  Of at most
+// kTiny tokens (tiny.ids) every workgroup looks at all.
 template <typename TO>
 struct ZeroArgs {
   TO *dE;
@@ -129,6 +153,7 @@ struct ZeroArgs {
   int d;
   Divisor chunks;
   const uint32_t *slot, *keys;
+  TinyIds tiny;
   uint32_t n;
   int64_t row0, rows;
   uint32_t per, blocks;
@@ -137,15 +162,25 @@ struct ZeroArgs {
 template <int kBlock, typename TO>
 __device__ inline void zero_rows(const ZeroArgs<TO> &z, uint32_t block) {
   __shared__ uint32_t absent[kZeroRows], n_absent;
+  __shared__ uint8_t occurs[kZeroRows];
   const Chunk zero = {0u, 0u, 0u, 0u};
   for (int64_t r0 = (int64_t)block * z.per; r0 < z.rows; r0 += (int64_t)z.blocks * z.per) {
     if (threadIdx.x == 0) n_absent = 0u;
+    if (threadIdx.x < kZeroRows) occurs[threadIdx.x] = 0;
     __syncthreads();
+    if (z.tiny.ids) {
+      if (threadIdx.x < z.n) {
+        const int64_t r = (int64_t)key_of(z.tiny, threadIdx.x) - (z.row0 + r0);
+        if (r >= 0 && r < (int64_t)z.per) occurs[r] = 1;
+      }
+      __syncthreads();
+    }
     if (threadIdx.x < z.per && r0 + threadIdx.x < z.rows) {
       const int64_t row = z.row0 + r0 + threadIdx.x;
       const uint32_t t = z.keys ? z.slot[row] : kNone;
       // (their order in the list does not matter)
-      if (!(t < z.n && (int64_t)z.keys[t] == row)) absent[atomicAdd(&n_absent, 1u)] = threadIdx.x;
+      if (!occurs[threadIdx.x] && !(t < z.n && (int64_t)z.keys[t] == row))
+        absent[atomicAdd(&n_absent, 1u)] = threadIdx.x;
     }
     __syncthreads();
     const uint32_t total = n_absent * z.chunks.d;
@@ -400,7 +435,8 @@ __global__ __launch_bounds__(kSortBlock) void scatter_kernel(
 
 template <typename T>
 struct SumArgs {
-  const uint32_t *key, *pos;
+  const uint32_t *key, *pos;     // the sorted list; not there where tiny.ids is
+  TinyIds tiny;
   uint32_t n, n_vocab, blocks;   // workgroups along the list
   Divisor slices;                // and along the columns
   int d, lanes, shift;           // lanes = 1 << shift
@@ -430,7 +466,8 @@ __device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, in
 // (neighbours read and write the same rows), entries of the list (b / slices groups + g) span
 // onwards for group g.  The other workgroups write zeros.  A group's
 // lanes hold its entries' numbers and tokens between them, so that the rows' loads wait for
-// nothing but each other: kAhead of them are always under way.
+// nothing but each other: kAhead of them are always under way.  Up to kTiny tokens are ranked
+// here, each against all the others, in every workgroup.
 template <typename T, typename TO, int kLanes, bool kDrop>
 __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__restrict__ dE, int64_t lde,
                                                         ZeroArgs<TO> z) {
@@ -445,6 +482,27 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
     zero_rows<kSumBlock>(z, blockIdx.x - a.blocks * a.slices.d);
     return;
   }
+  __shared__ __attribute__((aligned(16))) uint32_t tiny_in[kTiny];
+  __shared__ uint32_t tiny_key[kTiny], tiny_pos[kTiny];
+  const bool tiny = a.tiny.ids != nullptr;
+  if (tiny) {
+    const uint32_t t = threadIdx.x;
+    const uint32_t key = t < a.n ? key_of(a.tiny, t) : kNone;
+    if (t < kTiny) tiny_in[t] = key;
+    __syncthreads();
+    if (t < a.n) {
+      uint32_t rank = 0;                         // (entries past n are above all numbers)
+      for (uint32_t j = 0; j < a.n; j += 4) {
+        const Chunk other = *(const Chunk *)&tiny_in[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rank += other[i] < key || (other[i] == key && j + i < t) ? 1u : 0u;
+      }
+      tiny_key[rank] = key;
+      tiny_pos[rank] = t;
+    }
+    __syncthreads();
+  }
+  auto key_at = [&](uint32_t e) { return tiny ? tiny_key[e] : a.key[e]; };
   uint32_t group = threadIdx.x / kLanes;
   if (kLanes == 64) group = __builtin_amdgcn_readfirstlane(group);
   const int lane = threadIdx.x % kLanes;
@@ -456,11 +514,11 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
 #pragma unroll
   for (int j = 0; j < kHold; ++j) {
     const uint32_t e = lane + j * kLanes;
-    keys[j] = e < entries ? a.key[e0 + e] : kNone;
-    tokens[j] = e < entries ? a.pos[e0 + e] : 0u;
+    keys[j] = e < entries ? key_at(e0 + e) : kNone;
+    tokens[j] = e >= entries ? 0u : tiny ? tiny_pos[e0 + e] : a.pos[e0 + e];
   }
-  const uint32_t prev = e0 > 0 && entries ? a.key[e0 - 1] : kNone;
-  const uint32_t next = e0 + entries < a.n ? a.key[e0 + entries] : kNone;
+  const uint32_t prev = e0 > 0 && entries ? key_at(e0 - 1) : kNone;
+  const uint32_t next = e0 + entries < a.n ? key_at(e0 + entries) : kNone;
   // entry u's number or token, in all lanes of the group (all of them take part)
   auto of = [&](const uint32_t(&held)[kHold], int u) -> uint32_t {
     if constexpr (kLanes == 64) return __builtin_amdgcn_readlane(held[0], u);
@@ -614,10 +672,10 @@ struct Zeros {
 
   // keys: the tokens' numbers if the slots tell the rows that occur, or NULL
   Zeros(TO *dE, int64_t lde, int64_t n_vocab, int32_t d, const uint32_t *slot, const uint32_t *keys,
-        int64_t n)
+        const TinyIds &tiny, int64_t n)
       : left(n_vocab) {
     const uint32_t chunks = chunks_of<TO>(d);
-    z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, (uint32_t)n, 0, 0,
+    z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, tiny, (uint32_t)n, 0, 0,
                      std::max(1u, std::min(kZeroRows, kZeroChunks / chunks)), 0};
   }
   // Rows for the next `most` chunks, about, and workgroups for them.
@@ -667,8 +725,10 @@ template <typename T, typename TO, typename Id>
 toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_t d, const T *G,
                 int64_t ldg, float scale, const toc_drop *drop, TO *dE, int64_t lde, bool accumulate,
                 uint8_t *ws, hipStream_t s) {
-  Zeros<TO> zeros(dE, lde, accumulate ? 0 : n_vocab, d, (const uint32_t *)(ws + p.slot),
-                  n > 0 && !p.small ? (const uint32_t *)(ws + p.orig) : nullptr, n);
+  const TinyIds tiny{p.tiny && n > 0 ? ids : nullptr, 8 * (int)sizeof(Id), (uint32_t)n_vocab};
+  const bool tiled = !p.tiny && !p.small;
+  Zeros<TO> zeros(dE, lde, accumulate ? 0 : n_vocab, d, tiled ? (const uint32_t *)(ws + p.slot) : nullptr,
+                  tiled ? (const uint32_t *)(ws + p.orig) : nullptr, tiny, n);
   if (n == 0) {
     const ZeroArgs<TO> z = zeros.rest();
     if (z.blocks) hipLaunchKernelGGL(zero_kernel<TO>, dim3(z.blocks), dim3(256), 0, s, z);
@@ -679,16 +739,16 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
     hipLaunchKernelGGL((small_kernel<TO, Id>), dim3(1 + z.blocks), dim3(kSortBlock), 0, s, ids, (uint32_t)n,
                        (uint32_t)n_vocab, p.bits, p.passes, (uint32_t *)(ws + p.key[0]),
                        (uint32_t *)(ws + p.pos[0]), z);
-  } else {
+  } else if (tiled) {
     sort_tiles(p, (uint32_t)n, ids, (uint32_t)n_vocab, !accumulate, ws, zeros,
                beside(n * d * (int64_t)sizeof(T)), s);
   }
   const Mask m = mask_of(drop);
-  const int last = p.small ? 0 : (p.passes - 1) % 2;
+  const int last = p.small || p.tiny ? 0 : (p.passes - 1) % 2;
   const uint32_t span = block_span<T>(n, d);
   const int lanes = lanes_of(chunks_of<T>(d));
   const uint32_t slices = (chunks_of<T>(d) + lanes - 1) / lanes;
-  SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), (uint32_t)n,
+  SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), tiny, (uint32_t)n,
                (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), divisor(slices), d, lanes,
                __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
   const ZeroArgs<TO> z = zeros.rest();
