@@ -651,8 +651,8 @@ toc_status toc_mlp_epoch(const toc_dev *dev, int64_t b0, int64_t n_batches, int3
  * Everything is computed and summed in binary32 and rounded once, to nearest even,
  * where an output is stored; the squares of |h| above about 1e19 overflow.  Sums run
  * in an order that depends on the sizes alone, so equal calls give equal bits.
- * Limits (TOC_EUNSUPPORTED): n and n_vocab below 2^31, d at most 16384 for the norm and
- * 2^20 for the table's gradient.
+ * Limits (TOC_EUNSUPPORTED): n and n_vocab below 2^31, d at most 2^28, 16384 for the norm
+ * and 2^20 for the table's gradient.
  * An output may be the very matrix (pointer, stride and type) of one of the call's
  * inputs except G and E; outputs overlap nothing else.
  * ------------------------------------------------------------------------- */

@@ -157,6 +157,7 @@ struct ZeroArgs {
   uint32_t n;
   int64_t row0, rows;
   uint32_t per, blocks;
+  bool stream;
 };
 
 template <int kBlock, typename TO>
@@ -188,7 +189,7 @@ __device__ inline void zero_rows(const ZeroArgs<TO> &z, uint32_t block) {
       uint32_t at;
       const uint32_t i = divide(o, z.chunks, &at);
       const int c = (int)at * kCols<TO>;
-      put(z.dE + (z.row0 + r0 + absent[i]) * z.lde + c, z.d - c, zero);
+      put(z.dE + (z.row0 + r0 + absent[i]) * z.lde + c, z.d - c, zero, z.stream);
     }
     __syncthreads();
   }
@@ -447,10 +448,12 @@ struct SumArgs {
   Mask m;
   float *part;                   // two rows a workgroup: its first number's, its last number's
   int accumulate;
+  bool stream;                   // dE's rows go past the caches
 };
 
 template <typename TO, int N>
-__device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, int accumulate) {
+__device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, int accumulate,
+                                 bool stream) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] *= scale;
   if (accumulate) {
@@ -459,7 +462,7 @@ __device__ inline void write_row(TO *p, int left, float (&v)[N], float scale, in
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += old[i];
   }
-  store(p, left, v);
+  store(p, left, v, stream);
 }
 
 // Workgroup b of the first a.blocks slices: slice b mod slices of kLanes chunks of the columns
@@ -551,7 +554,7 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
 #pragma unroll
         for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
       } else if (left > 0) {                     // (cur < V: a larger number sorts after it)
-        write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+        write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate, a.stream);
       }
       cur = key;
       from_before = false;
@@ -584,7 +587,7 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
 #pragma unroll
     for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = acc[i];
   } else if (entries && !goes_on && cur < a.n_vocab && left > 0) {
-    write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+    write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate, a.stream);
   }
   if (lane == 0) through[group] = from_before && goes_on;
   __syncthreads();
@@ -598,7 +601,7 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
     for (uint32_t g = 0; g + 1 < kGroups && through[g]; ++g)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += heads[(g + 1) * kLanes + lane][i];
-    store(a.part + (int64_t)block * 2 * a.d + c, left, v);
+    store(a.part + (int64_t)block * 2 * a.d + c, left, v, false);
   }
   if (goes_on && !from_before && cur < a.n_vocab) {
     uint32_t g = group + 1;
@@ -608,8 +611,8 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
       for (int i = 0; i < N; ++i) acc[i] += heads[g * kLanes + lane][i];
       open = through[g];
     }
-    if (open) store(a.part + ((int64_t)block * 2 + 1) * a.d + c, left, acc);
-    else write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate);
+    if (open) store(a.part + ((int64_t)block * 2 + 1) * a.d + c, left, acc, false);
+    else write_row(dE + (int64_t)cur * lde + c, left, acc, a.scale, a.accumulate, a.stream);
   }
 }
 
@@ -659,7 +662,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t
   for (uint32_t g = 1; g < groups; ++g)
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] += sums[g * a.lanes + threadIdx.x][i];
-  write_row(dE + (int64_t)key * lde + c, left, acc, a.scale, a.accumulate);
+  write_row(dE + (int64_t)key * lde + c, left, acc, a.scale, a.accumulate, a.stream);
 }
 
 // --- launches -----------------------------------------------------------------------
@@ -676,7 +679,8 @@ struct Zeros {
       : left(n_vocab) {
     const uint32_t chunks = chunks_of<TO>(d);
     z = ZeroArgs<TO>{dE, lde, d, divisor(chunks), slot, keys, tiny, (uint32_t)n, 0, 0,
-                     std::max(1u, std::min(kZeroRows, kZeroChunks / chunks)), 0};
+                     std::max(1u, std::min(kZeroRows, kZeroChunks / chunks)), 0,
+                     stream_out(n_vocab, d, sizeof(TO))};
   }
   // Rows for the next `most` chunks, about, and workgroups for them.
   ZeroArgs<TO> take(int64_t most) {
@@ -750,7 +754,8 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
   const uint32_t slices = (chunks_of<T>(d) + lanes - 1) / lanes;
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), tiny, (uint32_t)n,
                (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), divisor(slices), d, lanes,
-               __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate};
+               __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate,
+               stream_out(accumulate ? std::min(n, n_vocab) : n_vocab, d, sizeof(TO))};
   const ZeroArgs<TO> z = zeros.rest();
   const dim3 grid(a.blocks * slices + z.blocks);
 #define TOC_SUM(L)                                                                                      \

@@ -88,6 +88,7 @@ struct NormArgs {
   int64_t ldh;
   int64_t ldy;
   float *y_scale;
+  bool stream;
 };
 
 template <int kPer, int N>
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
     for (int k = 0; k < kPer; ++k) {
       const int c = N * (lane + k * kLanes);
       if (c >= a.d) continue;
-      if (a.H) store(a.H + (int64_t)row * a.ldh + c, a.d - c, h[k]);
+      if (a.H) store(a.H + (int64_t)row * a.ldh + c, a.d - c, h[k], a.stream);
       float y[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
           y[i] = y[i] > kE4m3Max ? kE4m3Max : y[i] < -kE4m3Max ? -kE4m3Max : y[i];
         }
       }
-      store(Yp + (int64_t)row * a.ldy + c, a.d - c, y);
+      store(Yp + (int64_t)row * a.ldy + c, a.d - c, y, a.stream);
     }
   }
 }
@@ -212,6 +213,7 @@ struct GradArgs {
   T *dX;               // or NULL
   int64_t lddx;
   float *part;         // NULL, or one row of d per workgroup: its part of dw
+  bool stream;
 };
 
 template <typename T, int kLanes, int kPer, bool kDrop>
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
 #pragma unroll
         for (int i = 0; i < N; ++i) h[k][i] += dr[k][i];
       }
-      if (a.dH) store(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k]);
+      if (a.dH) store(a.dH + (int64_t)row * a.lddh + c, a.d - c, h[k], a.stream);
       if (a.dX) {
         if (kDrop) {
 #pragma unroll
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
         }
         Chunk x = narrow<T>(h[k]);
         if (kDrop) drop<T>(x, (uint32_t)c, row, a.m);
-        put(a.dX + (int64_t)row * a.lddx + c, a.d - c, x);
+        put(a.dX + (int64_t)row * a.lddx + c, a.d - c, x, a.stream);
       }
     }
   }
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int c = N * (lane + k * kLanes);
-      if (c < a.d) store(to + c, a.d - c, dw[k]);
+      if (c < a.d) store(to + c, a.d - c, dw[k], false);
     }
     return;
   }
@@ -436,7 +438,7 @@ toc_status norm_typed(int64_t n, int32_t d, const void *X, int64_t ldx, const vo
                       const toc_drop *drop, const float *w, float eps, void *H, int64_t ldh, void *Y,
                       int64_t ldy, bool eight, float *y_scale, void *stream) {
   const NormArgs<T> a{(uint32_t)n, d, (const T *)X, ldx, (const T *)R, ldr, mask_of(drop), w, eps,
-                      1.0f / (float)d, (T *)H, ldh, ldy, y_scale};
+                      1.0f / (float)d, (T *)H, ldh, ldy, y_scale, stream_out(n, d, sizeof(T))};
   if (eight) return norm(a, (E4m3 *)Y, (hipStream_t)stream);
   return norm(a, (T *)Y, (hipStream_t)stream);
 }
@@ -446,7 +448,8 @@ toc_status grad_typed(int64_t n, int32_t d, const void *H, int64_t ldh, const fl
                       const void *dY, int64_t lddy, const void *dR, int64_t lddr, const toc_drop *drop,
                       void *dH, int64_t lddh, void *dX, int64_t lddx, float *part, void *stream) {
   const GradArgs<T> a{(uint32_t)n, d, (const T *)H, ldh, w, eps, 1.0f / (float)d, (const T *)dY, lddy,
-                      (const T *)dR, lddr, mask_of(drop), (T *)dH, lddh, (T *)dX, lddx, part};
+                      (const T *)dR, lddr, mask_of(drop), (T *)dH, lddh, (T *)dX, lddx, part,
+                      stream_out(n, d, sizeof(T))};
   return norm_grad(a, (hipStream_t)stream);
 }
 

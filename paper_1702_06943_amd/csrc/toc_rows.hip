@@ -32,7 +32,8 @@ template <typename T, typename Id, bool kDrop>
 __global__ __launch_bounds__(kBlock) void rows_kernel(const Id *__restrict__ ids, int64_t n_vocab,
                                                       const T *src, int64_t lds, float scale,
                                                       Mask m, uint32_t row0, uint32_t total,
-                                                      int d, Divisor chunks, T *out, int64_t ldo) {
+                                                      int d, Divisor chunks, T *out, int64_t ldo,
+                                                      bool stream) {
   constexpr int P = kPer<Id>;
   constexpr bool same = std::is_same<Id, Same>::value;
   const uint32_t o0 = blockIdx.x * (uint32_t)(kBlock * P) + threadIdx.x;
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(const Id *__restrict__ ids
     widen<T>(in[k], v);
 #pragma unroll
     for (int i = 0; i < kCols<T>; ++i) v[i] *= scale;
-    store(out + (int64_t)row[k] * ldo + c, d - c, v);
+    store(out + (int64_t)row[k] * ldo + c, d - c, v, stream);
   }
 }
 
@@ -74,6 +75,7 @@ toc_status map_rows(int64_t n, int32_t d, const Id *ids, int64_t n_vocab, const 
   const Mask m = mask_of(drop);
   scale *= m.keep;
   const uint32_t chunks = chunks_of<T>(d);
+  const bool stream = stream_out(n, d, sizeof(T));
   const int64_t most = ((int64_t)1 << 30) / chunks;
   constexpr bool same = std::is_same<Id, Same>::value;
   for (int64_t r = 0; r < n; r += most) {
@@ -85,10 +87,10 @@ toc_status map_rows(int64_t n, int32_t d, const Id *ids, int64_t n_vocab, const 
     T *y = out + r * ldo;
     if (m.on)
       hipLaunchKernelGGL((rows_kernel<T, Id, true>), grid, dim3(kBlock), 0, s, i, n_vocab, x, lds, scale,
-                         m, (uint32_t)r, total, d, divisor(chunks), y, ldo);
+                         m, (uint32_t)r, total, d, divisor(chunks), y, ldo, stream);
     else
       hipLaunchKernelGGL((rows_kernel<T, Id, false>), grid, dim3(kBlock), 0, s, i, n_vocab, x, lds, scale,
-                         m, (uint32_t)r, total, d, divisor(chunks), y, ldo);
+                         m, (uint32_t)r, total, d, divisor(chunks), y, ldo, stream);
   }
   return launched("rows_kernel");
 }

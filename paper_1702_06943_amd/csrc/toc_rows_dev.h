@@ -75,6 +75,7 @@ inline toc_status check_sizes(int64_t n, int32_t d, int32_t type) {
   if (n < 0 || d < 1) return fail(TOC_EINVAL, "%lld rows of %d columns", (long long)n, d);
   if (!type_ok(type)) return fail(TOC_EINVAL, "unknown element type %d", type);
   if (n > kMaxRows) return fail(TOC_EUNSUPPORTED, "more than 2^31-1 rows");
+  if (d > 1 << 28) return fail(TOC_EUNSUPPORTED, "rows of more than 2^28 columns");
   return TOC_OK;
 }
 
@@ -91,6 +92,13 @@ inline toc_status launched(const char *what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TOC_OK : fail(TOC_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
+
+// Whether a call's output is written past the caches: from 8 MB on it is larger than what the
+// next call would find there, and the rows still to be read get their room (us, non-temporal
+// and not: lookup of 32,768 x 1,024 f32 27.5, 49.0; norm of 60,000 x 300 f32 53, 67; lookup, two
+// norms and two matrix products of 256, 1,024, 4,096, 16,384 rows of 1,024 bf16 31.6, 27.0;
+// 35.9, 32.5; 48.8, 49.5; 118.7, 118.8).
+inline bool stream_out(int64_t n, int64_t d, int64_t size) { return n * d * size >= (int64_t)8 << 20; }
 
 // Division of o < 2^31 by a divisor known on the host: floor(2^32 / divisor) times o, high
 // word, is the quotient or one less.
@@ -191,10 +199,7 @@ __device__ inline void widen(Chunk c, float (&v)[kCols<T>]) {
 }
 
 // N numbers (N: 4 or 8), columns 0..left-1 of them (the others read as 0, and are not
-// written): as binary32, a chunk at a time; as T, to nearest even, a NaN staying one.  Stores are non-temporal: outputs are
-// written once and far larger than the caches, which the rows still to be read get instead
-// (lookup of 32,768 x 1,024 f32 27.5 us against 49.0, norm of 60,000 x 300 f32 53 against 67,
-// dropout of 65,536 x 2,048 bf16 86 against 89).
+// written): as binary32, a chunk at a time; as T, to nearest even, a NaN staying one.
 template <typename T, int N>
 __device__ inline void load(const T *p, int left, float (&v)[N]) {
 #pragma unroll
@@ -228,11 +233,18 @@ __device__ inline Chunk narrow(const float *v) {
   return c;
 }
 
-template <typename T, bool kStream = true>
-__device__ inline void put(T *p, int left, Chunk c) {
+// stream: non-temporal, as stream_out() has it.  (The empty statements keep the compiler from
+// making one ordinary store of the two.)
+template <typename T>
+__device__ inline void put(T *p, int left, Chunk c, bool stream) {
   if (left >= kCols<T>) {
-    if (kStream) __builtin_nontemporal_store((Unaligned)c, (Unaligned *)p);
-    else *(Unaligned *)p = c;
+    if (stream) {
+      __builtin_nontemporal_store((Unaligned)c, (Unaligned *)p);
+    } else {
+      asm volatile("");
+      *(Unaligned *)p = c;
+      asm volatile("");
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kCols<T> - 1; ++i) {
@@ -247,9 +259,9 @@ __device__ inline void put(T *p, int left, Chunk c) {
 // have to meet in the cache (non-temporal, a gradient of 131,072 distinct bf16 rows of 1,024
 // into binary32 took 479 us, 316 with these).
 template <typename T, int N>
-__device__ inline void store(T *p, int left, const float (&v)[N]) {
+__device__ inline void store(T *p, int left, const float (&v)[N], bool stream) {
 #pragma unroll
-  for (int j = 0; j < N; j += kCols<T>) put<T, N == kCols<T>>(p + j, left - j, narrow<T>(v + j));
+  for (int j = 0; j < N; j += kCols<T>) put(p + j, left - j, narrow<T>(v + j), stream && N == kCols<T>);
 }
 
 struct E4m3 {
@@ -258,7 +270,7 @@ struct E4m3 {
 
 // N numbers of magnitude at most 448 as e4m3 numbers, rounded to nearest even.
 template <int N>
-__device__ inline void store(E4m3 *p, int left, const float (&v)[N]) {
+__device__ inline void store(E4m3 *p, int left, const float (&v)[N], bool) {
   uint32_t w[N / 4];
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {

@@ -54,6 +54,8 @@ def test_shared_refusals(name, fn, order, good):
     assert call(fn, order, good, type=7) == T.TOC_EINVAL
     assert call(fn, order, good, type=T.TOC_E4M3) == T.TOC_EINVAL
     assert call(fn, order, good, n=1 << 31) == T.TOC_EUNSUPPORTED
+    wide = {k: (1 << 28) + 1 for k in order if k == "d" or k.startswith("ld")}
+    assert call(fn, order, good, **wide) == T.TOC_EUNSUPPORTED
     for p in (-0.1, 1.5, NAN, INF):
         d = T.Drop(p, 1, 2)
         assert call(fn, order, good, drop=C.addressof(d)) == T.TOC_EINVAL
@@ -76,6 +78,8 @@ def test_token_refusals(fn, order, good):
     assert call(fn, order, good, n_vocab=1 << 31) == T.TOC_EUNSUPPORTED
     for s in (NAN, INF):
         assert call(fn, order, good, scale=s) == T.TOC_EINVAL
+    d = T.Drop(0.9, 1, 2)                                         # keeps with a factor of 10
+    assert call(fn, order, good, scale=1e38, drop=C.addressof(d)) == T.TOC_EINVAL
     assert call(fn, order, good, n=0, ids=None, n_vocab=0, E=None, dE=None, G=None, out=None,
                 ws=None, ws_bytes=0) == 0                         # nothing to do
 
