@@ -695,7 +695,8 @@ toc_status toc_embed_grad_workspace_size(int64_t n, int64_t n_vocab, int32_t d, 
  * alone: with dE = E and scale times -lr that is the table's step of mini-batch
  * gradient descent.
  *   G  n x d of `type`: the gradient of out    dE  n_vocab x d of de_type: type or TOC_F32
- *   ws device, toc_embed_grad_workspace_size bytes, 16-byte aligned, scratch
+ *   ws device, toc_embed_grad_workspace_size bytes, 16-byte aligned, scratch that no other
+ *      call may use while this one runs
  * Errors as toc_embed; TOC_ESIZE for a small workspace. */
 toc_status toc_embed_grad(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab, int32_t d,
                           int32_t type, const void *G, int64_t ldg, float scale, const toc_drop *drop,
@@ -730,7 +731,8 @@ toc_status toc_rmsnorm_grad_workspace_size(int64_t n, int32_t d, size_t *bytes);
  *   dX = drop(dH)                      the gradient of X
  *   dw[j] (+)= sum over rows of dY_j h_j r    (added to dw if accumulate != 0)
  * dH, dX and dw: outputs, each may be NULL.  ws: device, 4-byte aligned,
- * toc_rmsnorm_grad_workspace_size bytes (with dw NULL: not read).  Errors as toc_rmsnorm;
+ * toc_rmsnorm_grad_workspace_size bytes that no other call may use while this one runs
+ * (with dw NULL: not used).  Errors as toc_rmsnorm;
  * TOC_ESIZE for a small workspace. */
 toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, int64_t ldh,
                             const float *w, float eps, const void *dY, int64_t lddy, const void *dR,

@@ -21,7 +21,7 @@ ASAN_DIR = os.path.join(B.BUILD, "asan")
 ASAN_LIB = os.path.join(ASAN_DIR, "libtoc.so")
 SAN = ["-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined"]
 TESTS = ["tests/test_encode_abi.py", "tests/test_layout.py", "tests/test_phys.py",
-         "tests/test_ingest_host.py"]
+         "tests/test_ingest_host.py", "tests/test_rows_abi.py"]
 
 
 def runtime():
