@@ -141,7 +141,8 @@ struct TinyIds {
   uint32_t n_vocab;
 };
 __device__ inline uint32_t key_of(const TinyIds &t, uint32_t i) {
-  return t.bits == 32 ? key_of((const int32_t *)t.ids, i, t.n_vocab) : key_of((const int64_t *)t.ids, i, t.n_vocab);
+  return t.bits == 32 ? key_of((const int32_t *)t.ids, i, t.n_vocab)
+                      : key_of((const int64_t *)t.ids, i, t.n_vocab);
 }
 
 // --- zero ----------------------------------------------------------------------
@@ -373,7 +374,8 @@ __global__ __launch_bounds__(256) void scan_kernel(uint32_t *__restrict__ count,
 // first order.  The other workgroups write zeros.
 template <typename TO>
 __global__ __launch_bounds__(kSortBlock) void scatter_kernel(
-    const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, uint32_t n, uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
+    const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, uint32_t n,
+    uint32_t tiles, int shift, int bits, const uint32_t *__restrict__ count,
     const uint32_t *__restrict__ total, uint32_t *__restrict__ key_out, uint32_t *__restrict__ pos_out,
     ZeroArgs<TO> z) {
   __shared__ uint16_t at[kSortWaves][kMaxDigits];
@@ -621,7 +623,8 @@ __global__ __launch_bounds__(kSumBlock) void sum_kernel(SumArgs<T> a, TO *__rest
   }
 }
 
-// The row of a number that begins in a workgroup's entries and goes on after them: its part there, then those of the workgroups that follow, split over this one's groups of lanes.
+// The row of a number that begins in a workgroup's entries and goes on after them: its part
+// there, then those of the workgroups that follow, split over this one's groups of lanes.
 template <typename T, typename TO>
 __global__ __launch_bounds__(kJoinBlock) void join_kernel(SumArgs<T> a, uint32_t span,
                                                           TO *__restrict__ dE, int64_t lde) {
@@ -759,7 +762,8 @@ toc_status grad(const Plan &p, int64_t n, const Id *ids, int64_t n_vocab, int32_
   const uint32_t slices = (chunks_of<T>(d) + lanes - 1) / lanes;
   SumArgs<T> a{(const uint32_t *)(ws + p.key[last]), (const uint32_t *)(ws + p.pos[last]), tiny, (uint32_t)n,
                (uint32_t)n_vocab, (uint32_t)((n + span - 1) / span), divisor(slices), d, lanes,
-               __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m, (float *)(ws + p.part), accumulate,
+               __builtin_ctz(lanes), span_of(n, chunks_of<T>(d)), G, ldg, scale * m.keep, m,
+               (float *)(ws + p.part), accumulate,
                stream_out(accumulate ? std::min(n, n_vocab) : n_vocab, d, sizeof(TO))};
   const ZeroArgs<TO> z = zeros.rest();
   const dim3 grid(a.blocks * slices + z.blocks);
@@ -831,7 +835,8 @@ toc_status toc_embed_grad(int64_t n, const void *ids, int32_t id_bits, int64_t n
   if ((st = check_scale(scale, drop))) return st;
   const Plan p = plan_of(n, n_vocab, d);
   if (n > 0 && !ws) return fail(TOC_EINVAL, "workspace is NULL");
-  if (n > 0 && ws_bytes < p.end) return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, p.end);
+  if (n > 0 && ws_bytes < p.end)
+    return fail(TOC_ESIZE, "workspace of %zu bytes below the %zu needed", ws_bytes, p.end);
   if ((uintptr_t)ws % 16) return fail(TOC_EINVAL, "workspace is not 16-byte aligned");
   if (n_vocab == 0) return TOC_OK;
   const bool f32 = de_type == TOC_F32;

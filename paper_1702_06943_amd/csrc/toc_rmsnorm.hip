@@ -392,7 +392,9 @@ int64_t blocks_for(int64_t n, Shape sh, int64_t most) {
   return std::max<int64_t>(1, std::min((n + groups - 1) / groups, most));
 }
 int64_t norm_blocks(int64_t n, Shape sh) { return blocks_for(n, sh, sh.lanes > 256 ? 1024 : 1 << 22); }
-int64_t grad_blocks(int64_t n, Shape sh) { return blocks_for(n, sh, sh.lanes > 256 ? 256 : sh.lanes < 64 ? 1024 : 512); }
+int64_t grad_blocks(int64_t n, Shape sh) {
+  return blocks_for(n, sh, sh.lanes > 256 ? 256 : sh.lanes < 64 ? 1024 : 512);
+}
 
 template <typename T, typename Y>
 toc_status norm(const NormArgs<T> &a, Y *y, hipStream_t s) {

@@ -54,8 +54,10 @@ inline Mask mask_of(const toc_drop *drop) {
 inline toc_status check_rows(const char *name, const void *p, int64_t n, int32_t d, int64_t ld,
                              int size) {
   if (n > 0 && !p) return fail(TOC_EINVAL, "%s is NULL", name);
-  if (ld < d) return fail(TOC_EINVAL, "row stride %lld of %s below %d columns", (long long)ld, name, d);
-  if ((uintptr_t)p % (uintptr_t)size) return fail(TOC_EINVAL, "%s is not aligned to its %d-byte elements", name, size);
+  if (ld < d)
+    return fail(TOC_EINVAL, "row stride %lld of %s below %d columns", (long long)ld, name, d);
+  if ((uintptr_t)p % (uintptr_t)size)
+    return fail(TOC_EINVAL, "%s is not aligned to its %d-byte elements", name, size);
   return TOC_OK;
 }
 
@@ -67,7 +69,8 @@ inline toc_status check_drop(const toc_drop *drop) {
 
 // The scale and the kept elements' factor are one product.
 inline toc_status check_scale(float scale, const toc_drop *drop) {
-  if (!std::isfinite(scale * mask_of(drop).keep)) return fail(TOC_EINVAL, "scale, times the mask's factor, not finite");
+  if (!std::isfinite(scale * mask_of(drop).keep))
+    return fail(TOC_EINVAL, "scale, times the mask's factor, not finite");
   return TOC_OK;
 }
 
@@ -80,7 +83,8 @@ inline toc_status check_sizes(int64_t n, int32_t d, int32_t type) {
 }
 
 inline toc_status check_ids(int64_t n, const void *ids, int32_t id_bits, int64_t n_vocab) {
-  if (id_bits != 32 && id_bits != 64) return fail(TOC_EINVAL, "token numbers have 32 or 64 bits, not %d", id_bits);
+  if (id_bits != 32 && id_bits != 64)
+    return fail(TOC_EINVAL, "token numbers have 32 or 64 bits, not %d", id_bits);
   if (n > 0 && !ids) return fail(TOC_EINVAL, "ids is NULL");
   if ((uintptr_t)ids % (uintptr_t)(id_bits / 8)) return fail(TOC_EINVAL, "ids is not aligned to its elements");
   if (n_vocab < 0) return fail(TOC_EINVAL, "%lld table rows", (long long)n_vocab);
