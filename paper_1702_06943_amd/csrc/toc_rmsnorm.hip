@@ -282,14 +282,17 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     sum = group_sum2<kLanes>(sum, part[turn]);
     turn ^= 1;
     const float r = inv_rms(sum.x, a.inv_d, a.eps);
-    const float c3 = r * r * r * (sum.y * a.inv_d);
+    // dh = r g - (h r) (r mean(g h) r), whose factors stay in range where dh does: r^3 is 0 in
+    // binary32 for |h| above 1e15, and infinite in a row of zeros for eps below 1e-26
+    const float along = r * (sum.y * a.inv_d) * r;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int c = N * (lane + k * kLanes);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        dw[k][i] = fmaf(g[k][i] * r, h[k][i], dw[k][i]);
-        h[k][i] = fmaf(g[k][i] * w[k][i], r, -h[k][i] * c3);
+        const float x = h[k][i] * r;
+        dw[k][i] = fmaf(g[k][i], x, dw[k][i]);
+        h[k][i] = fmaf(g[k][i] * w[k][i], r, -x * along);
       }
       if (c >= a.d) continue;
       if (a.dR) {
