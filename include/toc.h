@@ -649,7 +649,9 @@ toc_status toc_mlp_epoch(const toc_dev *dev, int64_t b0, int64_t n_batches, int3
  * ld >= d elements, aligned to their elements only.  `type` is that of all of a
  * call's matrices unless it says otherwise; w, dw and the scales are binary32.
  * Everything is computed and summed in binary32 and rounded once, to nearest even,
- * where an output is stored; the squares of |h| above about 1e19 overflow.  Sums run
+ * where an output is stored.  The norm's mean(h^2) is infinite, so y is 0, in a row with
+ * some |h| above 1.8e19; it is off by up to 1e-41 beside its rounding, so an eps below
+ * 1e-33 is not held in full.  Sums run
  * in an order that depends on the sizes alone, so equal calls give equal bits.
  * Limits (TOC_EUNSUPPORTED): n and n_vocab below 2^31, d at most 2^28, 16384 for the norm
  * and 2^20 for the table's gradient.

@@ -74,8 +74,20 @@ __device__ inline float group_max(float x, float *lds) {
   return x;
 }
 
-__device__ inline float inv_rms(float sum, float inv_d, float eps) {
-  return 1.0f / sqrtf(fmaf(sum, inv_d, eps));
+// A row's mean of d numbers is back times the sum of `by` times each of them.  by is a power of
+// two and by d at most 1, so that the sum of d squares (or products) of binary32 numbers
+// overflows no earlier than one of them, and has the bits it would have without by.
+struct Mean {
+  float by, back;
+};
+inline Mean mean_of(int32_t d) {
+  float by = 1.0f;
+  while (by * (float)d > 1.0f) by *= 0.5f;
+  return Mean{by, 1.0f / (float)d / by};
+}
+
+__device__ inline float inv_rms(float sum, Mean mean, float eps) {
+  return 1.0f / sqrtf(fmaf(sum, mean.back, eps));
 }
 
 template <typename T>
@@ -88,7 +100,8 @@ struct NormArgs {
   int64_t ldr;
   Mask m;
   const float *w;      // or NULL: ones
-  float eps, inv_d;
+  float eps;
+  Mean mean;
   T *H;                // or NULL
   int64_t ldh;
   int64_t ldy;
@@ -162,7 +175,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum = fmaf(h[k][i], h[k][i], sum);
+      for (int i = 0; i < N; ++i) sum = fmaf(h[k][i] * a.mean.by, h[k][i], sum);
       if (k8) {
 #pragma unroll
         for (int i = 0; i < N; ++i) most = max_nan(fabsf(h[k][i] * w[k][i]), most);
@@ -171,7 +184,7 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_kernel(NormA
     // (the row before may still be reading the other reduction's words, never these: a
     // barrier of that other reduction, or of this one, lies between)
     sum = group_sum<kLanes>(sum, part[0]);
-    const float r = inv_rms(sum, a.inv_d, a.eps);
+    const float r = inv_rms(sum, a.mean, a.eps);
     float s = 1.0f;
     if (k8) {
       most = group_max<kLanes>(most, part[1]) * r;
@@ -208,7 +221,8 @@ struct GradArgs {
   const T *H;
   int64_t ldh;
   const float *w;      // or NULL: ones
-  float eps, inv_d;
+  float eps;
+  Mean mean;
   const T *dY;
   int64_t lddy;
   const T *dR;         // or NULL
@@ -275,16 +289,17 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void norm_grad_kernel(
     for (int k = 0; k < kPer; ++k)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        sum.x = fmaf(h[k][i], h[k][i], sum.x);
-        sum.y = fmaf(g[k][i] * w[k][i], h[k][i], sum.y);
+        const float x = h[k][i] * a.mean.by;
+        sum.x = fmaf(x, h[k][i], sum.x);
+        sum.y = fmaf(g[k][i] * w[k][i], x, sum.y);
       }
     // (two rows' words: the row before this one's may still be read)
     sum = group_sum2<kLanes>(sum, part[turn]);
     turn ^= 1;
-    const float r = inv_rms(sum.x, a.inv_d, a.eps);
+    const float r = inv_rms(sum.x, a.mean, a.eps);
     // dh = r g - (h r) (r mean(g h) r), whose factors stay in range where dh does: r^3 is 0 in
     // binary32 for |h| above 1e15, and infinite in a row of zeros for eps below 1e-26
-    const float along = r * (sum.y * a.inv_d) * r;
+    const float along = r * (sum.y * a.mean.back) * r;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int c = N * (lane + k * kLanes);
@@ -453,7 +468,7 @@ toc_status norm_typed(int64_t n, int32_t d, const void *X, int64_t ldx, const vo
                       const toc_drop *drop, const float *w, float eps, void *H, int64_t ldh, void *Y,
                       int64_t ldy, bool eight, float *y_scale, void *stream) {
   const NormArgs<T> a{(uint32_t)n, d, (const T *)X, ldx, (const T *)R, ldr, mask_of(drop), w, eps,
-                      1.0f / (float)d, (T *)H, ldh, ldy, y_scale, stream_out(n, d, sizeof(T))};
+                      mean_of(d), (T *)H, ldh, ldy, y_scale, stream_out(n, d, sizeof(T))};
   if (eight) return norm(a, (E4m3 *)Y, (hipStream_t)stream);
   return norm(a, (T *)Y, (hipStream_t)stream);
 }
@@ -462,7 +477,7 @@ template <typename T>
 toc_status grad_typed(int64_t n, int32_t d, const void *H, int64_t ldh, const float *w, float eps,
                       const void *dY, int64_t lddy, const void *dR, int64_t lddr, const toc_drop *drop,
                       void *dH, int64_t lddh, void *dX, int64_t lddx, float *part, void *stream) {
-  const GradArgs<T> a{(uint32_t)n, d, (const T *)H, ldh, w, eps, 1.0f / (float)d, (const T *)dY, lddy,
+  const GradArgs<T> a{(uint32_t)n, d, (const T *)H, ldh, w, eps, mean_of(d), (const T *)dY, lddy,
                       (const T *)dR, lddr, mask_of(drop), (T *)dH, lddh, (T *)dX, lddx, part,
                       stream_out(n, d, sizeof(T))};
   return norm_grad(a, (hipStream_t)stream);
