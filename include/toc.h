@@ -688,7 +688,8 @@ toc_status toc_embed(int64_t n, const void *ids, int32_t id_bits, int64_t n_voca
                      int32_t type, const void *E, int64_t lde, float scale, const toc_drop *drop,
                      void *out, int64_t ldo, void *stream);
 
-/* Workspace bytes of toc_embed_grad for n tokens. */
+/* Workspace bytes of toc_embed_grad for n tokens, or fewer, of n_vocab rows of d columns: the
+ * size does not fall as n grows. */
 toc_status toc_embed_grad_workspace_size(int64_t n, int64_t n_vocab, int32_t d, size_t *bytes);
 
 /* The lookup's gradient for the table: dE[v, :] = scale * sum of drop(G)[t, :] over the

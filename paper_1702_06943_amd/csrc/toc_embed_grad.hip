@@ -72,6 +72,7 @@ int lanes_of(uint32_t chunks) {
   return best;
 }
 
+constexpr int64_t kSumLanes = 4096 * 64;
 // Entries of a span: the more, the fewer parts of rows are put together, as long as the chip
 // has some 4,096 waves (us for 8, 16, 32: 131,072 x 1,024 bf16 161, 151, 148; 131,072 x 512 f16
 // of 300 numbers 80, 68, 58; 100,000 x 64 f32 35.9, 36.6, 43.8; 4,000 x 256 bf16 21.5, 25.2, 31.3).
@@ -83,7 +84,7 @@ uint32_t span_of(int64_t n, uint32_t chunks) {
   }
   const int64_t lanes = lanes_of(chunks), slices = (chunks + lanes - 1) / lanes;
   uint32_t span = kMaxSpan;
-  while (span > kMinSpan && n / span * lanes * slices < 4096 * 64) span /= 2;
+  while (span > kMinSpan && n / span * lanes * slices < kSumLanes) span /= 2;
   return span;
 }
 
@@ -91,6 +92,22 @@ uint32_t span_of(int64_t n, uint32_t chunks) {
 template <typename T>
 uint32_t block_span(int64_t n, int32_t d) {
   return (uint32_t)(kSumBlock / lanes_of(chunks_of<T>(d))) * span_of(n, chunks_of<T>(d));
+}
+
+// The most workgroups along the list that a call of at most n tokens has.  They halve where the
+// span doubles, so the last count of tokens before each doubling is looked at too: a workspace is
+// enough for smaller calls.
+template <typename T>
+int64_t most_blocks(int64_t n, int32_t d) {
+  auto blocks = [d](int64_t m) {
+    const int64_t span = block_span<T>(m, d);
+    return (m + span - 1) / span;
+  };
+  const int64_t chunks = chunks_of<T>(d), lanes = lanes_of(chunks), wide = (chunks + lanes - 1) / lanes * lanes;
+  int64_t most = blocks(n);
+  for (int64_t next = 2 * kMinSpan; next <= kMaxSpan; next *= 2)
+    most = std::max(most, blocks(std::min(n, next * ((kSumLanes + wide - 1) / wide) - 1)));
+  return most;
 }
 
 Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
@@ -102,8 +119,7 @@ Plan plan_of(int64_t n, int64_t n_vocab, int32_t d) {
   p.tiny = n <= (int64_t)kTiny;
   p.small = !p.tiny && n <= (int64_t)kSmall;
   p.tiles = p.tiny || p.small ? 0 : (uint32_t)((n + kTile - 1) / kTile);
-  const int64_t least = std::min(block_span<float>(n, d), block_span<bf16>(n, d));
-  const int64_t blocks = (n + least - 1) / least;
+  const int64_t blocks = std::max(most_blocks<float>(n, d), most_blocks<bf16>(n, d));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
