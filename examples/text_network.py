@@ -2,7 +2,8 @@
 
 The mini-batches (the sparse-text workload: 250 texts, 47,236 possible tokens) are
 encoded, uploaded and kept compressed; a step decodes its batch on the GPU, and the column
-numbers that come out are its tokens.  Per token t of text i:
+numbers that come out are its tokens (the values beside them are not used).  Per token t of
+text i:
 
     x_t = drop(sqrt(d) E[token])          toc_embed
     y_t = norm(x_t)                       toc_rmsnorm

@@ -644,15 +644,18 @@ toc_status toc_mlp_epoch(const toc_dev *dev, int64_t b0, int64_t n_batches, int3
  * matrix products: the lookup of the rows in a table (the right product of tuples
  * that hold one pair each, Theorem 1) and the table's gradient (the left product,
  * Theorem 2), dropout, and the root-mean-square norm with the residual's addition.
+ * Each of those pairs has the call's one `scale` as its value: the values that a
+ * mini-batch's own pairs carry take no part.
  *
  * Matrices of rows are caller-owned device memory, row-major with a stride of
  * ld >= d elements, aligned to their elements only.  `type` is that of all of a
  * call's matrices unless it says otherwise; w, dw and the scales are binary32.
  * Everything is computed and summed in binary32 and rounded once, to nearest even,
- * where an output is stored.  The norm's mean(h^2) is infinite, so y is 0, in a row with
- * some |h| above 1.8e19; it is off by up to 1e-41 beside its rounding, so an eps below
- * 1e-33 is not held in full.  Sums run
- * in an order that depends on the sizes alone, so equal calls give equal bits.
+ * where an output is stored.  The norm holds for |h| up to 1.8e19, where squares overflow
+ * (y is then 0), its gradient for |dY w h| up to 3e38 too; mean(h^2) is off by up to
+ * 1e-41 beside its rounding, so an eps below 1e-33 is not held in full.  The order of
+ * sums depends on the sizes alone, for the table's gradient on the token numbers too:
+ * equal calls give equal bits.
  * Limits (TOC_EUNSUPPORTED): n and n_vocab below 2^31, d at most 2^28, 16384 for the norm
  * and 2^20 for the table's gradient.
  * An output may be the very matrix (pointer, stride and type) of one of the call's

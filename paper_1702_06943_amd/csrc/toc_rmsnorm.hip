@@ -10,7 +10,7 @@
 //   norm_kernel       bound by memory: 32,768 x 2,048 bf16 with dropout and residual 92 us, 5.8
 //                     TB/s; 18,749 x 1,001 f16 rows of a wider matrix into e4m3 25 us, 5.2 TB/s
 //   norm_grad_kernel  bound by memory, four or five streams at once: 32,768 x 2,048 bf16 with
-//                     dropout 125 us, 5.4 TB/s
+//                     dropout 121 us, 5.6 TB/s with dw's parts (the call 127 us, 5.3 without)
 //   norm_join_kernel  dw from the workgroups' rows, some 5 us of a call
 #include "toc_rows_dev.h"
 
@@ -380,7 +380,9 @@ __global__ __launch_bounds__(kJoinCols * kJoinParts) void norm_join_kernel(
 
 // Lanes to a row and chunks to a lane (us: 32,768 x 2,048 bf16 forward by 256 x 1 92, 64 x 4 102;
 // 18,749 x 1,001 f16 by 64 x 2 28, 256 x 1 36; 8,192 x 8,192 bf16 with dropout by 512 x 2 88,
-// 1,024 x 1 119, backward 135 and 128).
+// 1,024 x 1 119, backward 135 and 128).  The widest binary32 rows hold 16 numbers of each stream
+// a lane, and spill on the way back: 2,000 x 16,384 forward 88, 6.0 TB/s, backward with dropout
+// 170, 3.9 TB/s.
 struct Shape {
   int lanes, per;
 };
@@ -405,6 +407,7 @@ Shape shape_of(uint32_t chunks, bool grad) {
 // Backward all walk, since each workgroup leaves a row of dw's parts, 512 of them (us for 1,024,
 // 768, 512: 32,768 x 2,048 bf16 with dropout 132, 127, 127; 8,192 x 4,096 bf16 63.5, 58.5, 55.5;
 // 18,750 x 300 f32 21.4, 21.9, 21.8), short rows 1,024 (100,000 x 64 bf16 15.3, 16.1, 15.9).
+// (Few long rows pay for their parts: 1,000 x 4,096 bf16 without dropout 16.0 us, 6.9 without dw.)
 int64_t blocks_for(int64_t n, Shape sh, int64_t most) {
   const int64_t groups = sh.lanes > 256 ? 1 : 256 / sh.lanes;
   return std::max<int64_t>(1, std::min((n + groups - 1) / groups, most));
