@@ -746,6 +746,85 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
                             int64_t lddx, float *dw, int32_t accumulate, void *ws, size_t ws_bytes,
                             void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Rows of logits: the end of a network over tokens.  Z is n x d of `type`, a row per
+ * token and a column per token number of the vocabulary; with s = scale (1 /
+ * temperature, positive), row by row
+ *   p_j = exp(s z_j) / sum_i exp(s z_i)
+ * formed from the differences to the row's largest logit, so that s z itself is never
+ * formed.  A column at minus infinity is masked: its p is 0.  The conventions are those of
+ * the rows above; vectors of n are contiguous binary32, token numbers id_bits (32 or 64)
+ * signed bits, and one outside 0 .. d-1 (say -1, to pad) is no token.
+ *   A row of nothing but minus infinity: p = 0, log p and lse minus infinity, entropy 0, its
+ *     gradient 0.
+ *   A row with a NaN or +infinity: what depends on its sum is NaN.
+ * Sums are binary32, their order depends on n, d and `type` alone: equal calls give equal bits.
+ * dZ may be Z; outputs overlap nothing else.
+ * Limits (TOC_EUNSUPPORTED): n below 2^31, d at most 2^28, 64 alternatives, 256 saved logits.
+ * ------------------------------------------------------------------------- */
+
+/* Workspace bytes of the four calls below for n rows, or fewer, of d columns and k
+ * alternatives, or fewer (0: toc_logprob without, and the other three): the size does not
+ * fall as n or k grows.  It may be 0. */
+toc_status toc_logits_workspace_size(int64_t n, int32_t d, int32_t k, size_t *bytes);
+
+/* Of each row, what is asked for (each output may be NULL):
+ *   logp[i]     = log p of token ids[i]; 0 where that is no token (ids: NULL without logp)
+ *   lse[i]      = log sum_j exp(s z_ij)
+ *   entropy[i]  = - sum_j p_j log p_j
+ *   top_ids[i, 0..k-1], top_logp[i, 0..k-1] (n x k, contiguous, top_ids of id_bits): the k
+ *               columns with the largest logits, the largest first, of equal ones the lowest
+ *               column first, and their log p; -1 and minus infinity past the last column above
+ *               minus infinity.  A NaN is no alternative.  k = 0: none
+ *   ws   device, toc_logits_workspace_size bytes, 16-byte aligned, that no other call may use
+ *        while this one runs
+ * Asynchronous on stream.  TOC_EINVAL for NULL or misaligned pointers, strides below d, unknown
+ * types or widths, a scale that is not positive or not finite once multiplied by log2(e), logp
+ * without ids; TOC_ESIZE for a small workspace. */
+toc_status toc_logprob(int64_t n, int32_t d, int32_t type, const void *Z, int64_t ldz, float scale,
+                       const void *ids, int32_t id_bits, float *logp, float *lse, float *entropy,
+                       int32_t k, void *top_ids, float *top_logp, void *ws, size_t ws_bytes,
+                       void *stream);
+
+/* The gradient for the logits of a loss whose gradients for logp, lse and entropy are dlogp,
+ * dlse and dentropy (n each; NULL: zeros):
+ *   dZ_ij = s (dlogp_i ([j = ids_i] - p_j) + dlse_i p_j - dentropy_i p_j (log p_j + entropy_i))
+ * dlogp counts only where ids[i] is a token.  A row whose three numbers are 0 has the gradient 0,
+ * whatever it holds.  The alternatives have no gradient.
+ *   logp, lse, entropy   as in toc_logprob, or NULL: a training step whose dlogp is known before
+ *                        (a mean's share, say) needs no call of toc_logprob
+ *   dZ   n x d of `type`; it may be Z
+ * Errors as toc_logprob; dlogp needs ids. */
+toc_status toc_logprob_grad(int64_t n, int32_t d, int32_t type, const void *Z, int64_t ldz, float scale,
+                            const void *ids, int32_t id_bits, const float *dlogp, const float *dlse,
+                            const float *dentropy, float *logp, float *lse, float *entropy, void *dZ,
+                            int64_t lddz, void *ws, size_t ws_bytes, void *stream);
+
+/* How far each row is from a teacher's, of which the k logits top_z[i, a] at the columns
+ * top_ids[i, a] were saved (toc_logprob's alternatives, say):
+ *   loss[i] = sum_a q_a (log q_a - log p_{top_ids[i, a]})
+ *   q_a = exp(top_scale top_z_a) / the sum of that over the row's entries    (top_lse NULL)
+ *   q_a = exp(top_scale top_z_a - top_lse[i])      (the rest of the teacher's row left out)
+ *   top_ids   n x k, row stride ldi; an entry that is no token takes no part, equal ones all count
+ *   top_z     n x k of top_type (`type` or TOC_F32), row stride ldt; top_scale positive and finite
+ * An entry with q = 0 adds nothing; q > 0 at a masked column makes the loss infinite.  A row without
+ * entries has loss 0.  Errors as toc_logprob. */
+toc_status toc_distill(int64_t n, int32_t d, int32_t type, const void *Z, int64_t ldz, float scale,
+                       int32_t k, const void *top_ids, int32_t id_bits, int64_t ldi, int32_t top_type,
+                       const void *top_z, int64_t ldt, float top_scale, const float *top_lse, float *loss,
+                       void *ws, size_t ws_bytes, void *stream);
+
+/* The gradient for the logits of a loss whose gradient for toc_distill's is dloss (n):
+ *   dZ_ij = s dloss_i (p_j sum_a q_a - sum of q_a over the entries with top_ids[i, a] = j)
+ * A row with dloss 0, or without entries, has the gradient 0, whatever it holds.
+ *   loss   as in toc_distill, or NULL    dZ   n x d of `type`; it may be Z
+ * Errors as toc_distill. */
+toc_status toc_distill_grad(int64_t n, int32_t d, int32_t type, const void *Z, int64_t ldz, float scale,
+                            int32_t k, const void *top_ids, int32_t id_bits, int64_t ldi, int32_t top_type,
+                            const void *top_z, int64_t ldt, float top_scale, const float *top_lse,
+                            const float *dloss, float *loss, void *dZ, int64_t lddz, void *ws,
+                            size_t ws_bytes, void *stream);
+
 /* Message for the last non-OK status returned on this thread. */
 const char *toc_last_error(void);
 

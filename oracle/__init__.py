@@ -67,9 +67,13 @@ Parity status of each function (what pins it, see ``tests/test_oracle.py``):
   rows.e4m3_values
                  pinned: the format's largest, smallest normal and smallest
                  numbers, symmetry, increasing order
+  logits.logprob, logits.logprob_grad, logits.distill, logits.distill_grad
+                 pinned (tests/test_logits_oracle.py): uniform and two-column rows in
+                 closed form, masked rows, central finite differences of the gradients
 """
 
 from . import rows_oracle as rows  # noqa: F401
+from . import logits_oracle as logits  # noqa: F401
 
 from .toc_oracle import (  # noqa: F401
     TocInputError,

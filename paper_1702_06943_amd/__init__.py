@@ -6,8 +6,10 @@ it on the GPU; run
 mini-batch gradient descent steps of linear models and of a feed-forward neural
 network on the compressed batches;
 encode many mini-batches at once on the GPU.  For networks over the tokens of decoded
-mini-batches: embedding lookup and its gradient, dropout, and the residual
-root-mean-square norm and its gradient.
+mini-batches: embedding lookup and its gradient, dropout, the residual
+root-mean-square norm and its gradient; and at their end, log probabilities of given
+tokens with entropy and most probable tokens, distillation from a teacher's saved
+logits, and the gradients of both.
 
 The functions are those of include/toc.h, called through ctypes; see binding.py.
 """
@@ -35,5 +37,6 @@ from .binding import (  # noqa: F401
     TOC_F32, TOC_BF16, TOC_F16, TOC_E4M3, Drop,
     toc_embed, toc_embed_grad_workspace_size, toc_embed_grad, toc_dropout,
     toc_rmsnorm, toc_rmsnorm_grad_workspace_size, toc_rmsnorm_grad,
+    toc_logits_workspace_size, toc_logprob, toc_logprob_grad, toc_distill, toc_distill_grad,
     TOC_INGEST_CHANGED, toc_ingest_workspace_size, toc_ingest_plan, toc_ingest_build,
 )

@@ -153,6 +153,14 @@ def lib():
         "toc_rmsnorm_grad_workspace_size": [I64, I32, P],
         "toc_rmsnorm_grad": [I64, I32, I32, P, I64, P, C.c_float, P, I64, P, I64, P, P, I64, P,
                              I64, P, I32, P, SZ, P],
+        "toc_logits_workspace_size": [I64, I32, I32, P],
+        "toc_logprob": [I64, I32, I32, P, I64, C.c_float, P, I32, P, P, P, I32, P, P, P, SZ, P],
+        "toc_logprob_grad": [I64, I32, I32, P, I64, C.c_float, P, I32, P, P, P, P, P, P, P, I64,
+                             P, SZ, P],
+        "toc_distill": [I64, I32, I32, P, I64, C.c_float, I32, P, I32, I64, I32, P, I64, C.c_float,
+                        P, P, P, SZ, P],
+        "toc_distill_grad": [I64, I32, I32, P, I64, C.c_float, I32, P, I32, I64, I32, P, I64,
+                             C.c_float, P, P, P, P, I64, P, SZ, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -819,3 +827,126 @@ def toc_rmsnorm_grad(H, dY, dH, ws, w=None, eps=1e-5, dR=None, dX=None, dw=None,
     _check(lib().toc_rmsnorm_grad(n, d, kind, hp, ldh, _row_vec(w, "w", d, dev), eps, gp, ldg, rp, ldr,
                                   _row_drop(drop), dhp, lddh, dxp, lddx, _row_vec(dw, "dw", d, dev),
                                   1 if accumulate else 0, wp, wn, _row_stream(stream, dev)))
+
+
+# --- rows of logits --------------------------------------------------------------
+
+
+def toc_logits_workspace_size(n, d, k=0):
+    """For the four calls below; k: toc_logprob's alternatives."""
+    b = C.c_size_t()
+    _check(lib().toc_logits_workspace_size(int(n), int(d), int(k), C.byref(b)))
+    return b.value
+
+
+def _row_given(ids, n, dev):
+    """(pointer, bits) of the rows' token numbers; without any, 64 bits."""
+    if ids is None:
+        return None, 64
+    m, p, bits = _row_ids(ids, dev)
+    if m != n:
+        raise TocError(TOC_EINVAL, f"ids must hold one number for each of {n} rows, not {m}")
+    return p, bits
+
+
+def toc_logprob(Z, ids=None, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None,
+                scale=1.0, ws=None, stream=None):
+    """Of each row of Z (n x d device tensor: float32, bfloat16, float16), p the softmax of
+    scale * Z, what is asked for: logp[i] = log p of ids[i] (device int32 or int64 vector of n;
+    one outside 0 .. d-1: 0), lse[i] = log sum exp(scale * Z[i]), entropy[i], and the k most
+    probable columns with their log p (top_ids: n x k of ids' type, top_logp: n x k; of equal
+    logits the lowest column; -1 and -inf past the last column above -inf).  Outputs: contiguous
+    device tensors, float32 unless said, or None; ws: device tensor of
+    toc_logits_workspace_size(n, d, k) bytes, None if that is 0."""
+    dev = _row_device()
+    n, d = _row_shape(Z, "Z")
+    zp, ldz, kind = _row_mat(Z, "Z", n, d, dev, _ROWS)
+    ip, bits = _row_given(ids, n, dev)
+    k, tp, lp = 0, None, None
+    if top_ids is not None or top_logp is not None:
+        if top_ids is None or top_logp is None:
+            raise TocError(TOC_EINVAL, "top_ids and top_logp come together")
+        k = _row_shape(top_ids, "top_ids")[1]
+        tbits = {_torch.int32: 32, _torch.int64: 64}.get(top_ids.dtype)
+        if tbits is None or (ids is not None and tbits != bits):
+            raise TocError(TOC_EINVAL, "top_ids must be int32 or int64, as ids are")
+        bits = tbits
+        for t, name, dtype in ((top_ids, "top_ids", top_ids.dtype),
+                               (top_logp, "top_logp", _torch.float32)):
+            if (t.get_device() != dev or t.dtype != dtype or t.shape != (n, k)
+                    or not t.is_contiguous()):
+                raise TocError(TOC_EINVAL, f"{name} must be a contiguous {n} x {k} tensor of "
+                                           f"{dtype} on the current CUDA device")
+        tp, lp = top_ids.data_ptr() or None, top_logp.data_ptr() or None
+    wp, wn = _row_ws(ws, dev)
+    _check(lib().toc_logprob(n, d, kind, zp, ldz, scale, ip, bits, _row_vec(logp, "logp", n, dev),
+                             _row_vec(lse, "lse", n, dev), _row_vec(entropy, "entropy", n, dev), k,
+                             tp, lp, wp, wn, _row_stream(stream, dev)))
+
+
+def toc_logprob_grad(Z, dZ, ids=None, dlogp=None, dlse=None, dentropy=None, logp=None, lse=None,
+                     entropy=None, scale=1.0, ws=None, stream=None):
+    """dZ (n x d of Z's type; it may be Z): the gradient for Z of a loss whose gradients for
+    toc_logprob's logp, lse and entropy are dlogp, dlse and dentropy (device float32 vectors of
+    n, or None: zeros).  logp, lse, entropy: outputs as in toc_logprob, or None.  ws: as there."""
+    dev = _row_device()
+    n, d = _row_shape(Z, "Z")
+    zp, ldz, kind = _row_mat(Z, "Z", n, d, dev, _ROWS)
+    gp, ldg, _ = _row_mat(dZ, "dZ", n, d, dev, (kind,))
+    ip, bits = _row_given(ids, n, dev)
+    wp, wn = _row_ws(ws, dev)
+    _check(lib().toc_logprob_grad(n, d, kind, zp, ldz, scale, ip, bits,
+                                  _row_vec(dlogp, "dlogp", n, dev), _row_vec(dlse, "dlse", n, dev),
+                                  _row_vec(dentropy, "dentropy", n, dev),
+                                  _row_vec(logp, "logp", n, dev), _row_vec(lse, "lse", n, dev),
+                                  _row_vec(entropy, "entropy", n, dev), gp, ldg, wp, wn,
+                                  _row_stream(stream, dev)))
+
+
+def _row_saved(top_ids, top_z, n, dev, kind):
+    """A teacher's saved logits: k, (pointer, bits, stride) of their columns and (type, pointer,
+    stride) of their values."""
+    k = _row_shape(top_ids, "top_ids")[1]
+    bits = {_torch.int32: 32, _torch.int64: 64}.get(top_ids.dtype)
+    if bits is None or top_ids.get_device() != dev or top_ids.shape[0] != n:
+        raise TocError(TOC_EINVAL, f"top_ids must be int32 or int64, {n} rows on the current CUDA "
+                                   "device")
+    ldi, cs = top_ids.stride()
+    if (cs != 1 and k > 1) or (ldi < k and n > 1):
+        raise TocError(TOC_EINVAL, "top_ids must have unit column stride and rows apart")
+    tp, ldt, tkind = _row_mat(top_z, "top_z", n, k, dev, (kind, TOC_F32))
+    return k, top_ids.data_ptr() or None, bits, max(ldi, k), tkind, tp, ldt
+
+
+def toc_distill(Z, top_ids, top_z, loss, scale=1.0, top_scale=1.0, top_lse=None, ws=None,
+                stream=None):
+    """loss[i] = sum_a q_a (log q_a - log p[top_ids[i, a]]), p the softmax of scale * Z[i], q that
+    of the teacher's saved logits top_scale * top_z[i] (n x k of Z's type or float32; top_ids: n x k
+    of int32 or int64, one outside 0 .. d-1 takes no part), or exp(top_scale * top_z[i] -
+    top_lse[i]) with top_lse.  loss, top_lse: device float32 vectors of n; ws: device tensor of
+    toc_logits_workspace_size(n, d) bytes, None if that is 0."""
+    dev = _row_device()
+    n, d = _row_shape(Z, "Z")
+    zp, ldz, kind = _row_mat(Z, "Z", n, d, dev, _ROWS)
+    k, ip, bits, ldi, tkind, tp, ldt = _row_saved(top_ids, top_z, n, dev, kind)
+    wp, wn = _row_ws(ws, dev)
+    _check(lib().toc_distill(n, d, kind, zp, ldz, scale, k, ip, bits, ldi, tkind, tp, ldt, top_scale,
+                             _row_vec(top_lse, "top_lse", n, dev), _row_vec(loss, "loss", n, dev),
+                             wp, wn, _row_stream(stream, dev)))
+
+
+def toc_distill_grad(Z, dZ, top_ids, top_z, dloss, loss=None, scale=1.0, top_scale=1.0,
+                     top_lse=None, ws=None, stream=None):
+    """dZ (n x d of Z's type; it may be Z): the gradient for Z of a loss whose gradient for
+    toc_distill's is dloss (device float32 vector of n).  loss: output as there, or None; the
+    other arguments as there."""
+    dev = _row_device()
+    n, d = _row_shape(Z, "Z")
+    zp, ldz, kind = _row_mat(Z, "Z", n, d, dev, _ROWS)
+    gp, ldg, _ = _row_mat(dZ, "dZ", n, d, dev, (kind,))
+    k, ip, bits, ldi, tkind, tp, ldt = _row_saved(top_ids, top_z, n, dev, kind)
+    wp, wn = _row_ws(ws, dev)
+    _check(lib().toc_distill_grad(n, d, kind, zp, ldz, scale, k, ip, bits, ldi, tkind, tp, ldt,
+                                  top_scale, _row_vec(top_lse, "top_lse", n, dev),
+                                  _row_vec(dloss, "dloss", n, dev), _row_vec(loss, "loss", n, dev),
+                                  gp, ldg, wp, wn, _row_stream(stream, dev)))
