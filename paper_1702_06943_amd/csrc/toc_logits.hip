@@ -10,31 +10,6 @@ namespace {
 
 constexpr int kEntropy = 1, kTop = 2, kTeach = 4;   // what a kernel is asked for
 
-// The sums of a lane's chunks: the row's chunks are dealt out to the group's lanes in turn.
-template <typename T, int kLanes, bool kT>
-__device__ inline Sums lane_sums(const T *row, int d, int lane, float c) {
-  constexpr int N = kCols<T>;
-  Sums a{kNone, 0.0f, 0.0f};
-  for (int at = N * lane; at < d; at += N * kLanes) {
-    const Place<T, true> l = place<T, true>(at, d);
-    float v[N];
-    widen_row<T>(settle(fetch(row, l), l), at, d, v);
-    float m = a.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-    const float base = from(m);
-    a = moved<kT>(a, base, c);
-    a.m = m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float y = (v[i] - base) * c, e = two_to(y);
-      a.s += e;
-      if (kT) a.t = fmaf(e, fmaxf(y, kFar), a.t);
-    }
-  }
-  return a;
-}
-
 // Logits in the order that the alternatives have them: the larger first, of equal ones the
 // lower column.  A key is never 0 for a column above minus infinity; a NaN has none.
 __device__ inline uint64_t key_of(float z, int column) {
@@ -55,74 +30,198 @@ __device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const E
   a.top_logp[at] = key ? log_p(key_logit(key), e, scale) : kNone;
 }
 
-// The alternatives by k searches of the row for the largest key below the last.
-template <typename T, int kLanes>
-__device__ inline void top_rounds(const Rows<T> &a, const Score &o, uint32_t row, int lane, const End &e,
-                                  uint64_t *lds) {
+// Keys of columns that may be among a row's alternatives; at first the lanes' own.
+template <int kLanes>
+constexpr int kCand = kLanes > 64 ? 1024 : 512;
+
+template <int kLanes, bool kOn>
+struct TopLds {
+  uint64_t keys[kOn ? kCand<kLanes> : 1];
+  uint64_t best[kLanes / 64];
+  uint16_t who[kOn ? kLanes : 1];      // lanes that may hold some
+  uint32_t lanes, count;
+};
+
+// The numbers of chunk q < end of a row.
+template <typename T>
+__device__ inline void chunk_numbers(const T *z, int q, int end, int d, float (&v)[kCols<T>]) {
+  Batch<T, 64, 1> b;
+  b.load(z, q, end, d, 0);
+  b.numbers(0, v);
+}
+
+__device__ inline uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
+
+// The alternatives by k searches for the largest key below the last.
+template <typename T, int kLanes, typename Put>
+__device__ inline void top_searches(const T *z, int d, int q0, int end, int k, int lane, uint64_t *best_lds, Put put) {
   constexpr int N = kCols<T>;
-  const T *z = a.Z + (int64_t)row * a.ldz;
   uint64_t last = ~(uint64_t)0;
-  for (int r = 0; r < o.k; ++r) {
+  for (int r = 0; r < k; ++r) {
     uint64_t best = 0;
     if (last) {
-      for (int at = N * lane; at < a.d; at += N * kLanes) {
-        const Place<T, true> l = place<T, true>(at, a.d);
+      for (int q = q0 + lane; q < end; q += kLanes) {
         float v[N];
-        widen_row<T>(settle(fetch(z, l), l), at, a.d, v);
+        chunk_numbers(z, q, end, d, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const uint64_t key = key_of(v[i], at + i);
-          if (key < last && key > best) best = key;
+          const uint64_t key = key_of(v[i], N * q + i);
+          if (key < last) best = larger(key, best);
         }
       }
     }
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) {
-      const uint64_t other = __shfl_xor((unsigned long long)best, x, 64);
-      best = other > best ? other : best;
-    }
+    for (int x = 32; x > 0; x >>= 1) best = larger(best, __shfl_xor((unsigned long long)best, x, 64));
     if (kLanes > 64) {
       __syncthreads();
-      if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = best;
+      if (threadIdx.x % 64 == 0) best_lds[threadIdx.x / 64] = best;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kLanes / 64; ++i) best = lds[i] > best ? lds[i] : best;
+      for (int i = 0; i < kLanes / 64; ++i) best = larger(best, best_lds[i]);
     }
-    if (lane == 0) put_top(o, (int64_t)row * o.k + r, best, e, a.scale);
+    if (lane == 0) put(r, best);
     last = best;
   }
 }
 
-template <typename T, int kLanes, int kWhat>
-__global__ __launch_bounds__(kBlock) void score_kernel(Rows<T> a, Score o, Teacher t) {
-  __shared__ Sums sums[kLanes / 64];
-  __shared__ float teach_lds[kLanes / 64 * 4];
-  __shared__ uint64_t keys[kLanes / 64];
-  const int lane = threadIdx.x;
-  for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-    const T *z = a.Z + (int64_t)row * a.ldz;
-    __syncthreads();
-    if (kWhat & kTeach) {
-      const Taught<kLanes> x = teach<T, kLanes>(t, row, z, a.d, lane, teach_lds);
-      const End e = end_of(group_sums<kLanes, false>(lane_sums<T, kLanes, false>(z, a.d, lane, a.c), a.c, sums));
-      const float loss = taught_loss<kLanes>(x, e, a.scale, teach_lds + 3 * (kLanes / 64));
-      if (lane == 0) t.loss[row] = loss;
+// A lower bound, and no key lies between it and the k-th largest of a wave's 64 keys: by bits from
+// the highest on, of the logits first.  1 if fewer than k keys are not 0.
+__device__ inline uint64_t kth_largest(uint64_t key, int k) {
+  if (__popcll(__ballot(key != 0)) < k) return 1;
+  const uint32_t high = (uint32_t)(key >> 32), low = (uint32_t)key;
+  uint32_t t = 0;
+  int count = 64;
+  for (uint32_t bit = 1u << 31; bit && count != k; bit >>= 1) {
+    const int n = __popcll(__ballot(high >= (t | bit)));
+    if (n < k) continue;
+    t |= bit;
+    count = n;
+  }
+  uint32_t u = 0;
+  if (count != k) {
+    // more than k at or above t, fewer than k above it: the lowest columns among those at t
+    const int more = k - (int)__popcll(__ballot(high > t));
+    for (uint32_t bit = 1u << 31; bit; bit >>= 1)
+      if ((int)__popcll(__ballot(high == t && low >= (u | bit))) >= more) u |= bit;
+  }
+  const uint64_t bound = (uint64_t)t << 32 | u;
+  uint64_t least = key >= bound ? key : ~(uint64_t)0;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) {
+    const uint64_t other = __shfl_xor((unsigned long long)least, x, 64);
+    least = other < least ? other : least;
+  }
+  return least;
+}
+
+// The k largest keys of a group's chunks q0 .. end - 1, put(r, key) for the r-th of them (0: there
+// is none).  The sums' pass over the row leaves each lane's largest logit and its chunk.  Of lanes i,
+// i + 64, ... the largest such keys are 64 keys of different columns, so the k-th largest of them is
+// a lower bound of the k-th largest of all, and lanes whose own largest logit is below it have none
+// of those: the chunks of the other lanes, some k, are dealt out to the group and read again, and
+// the keys from the bound on, little more than k, are left in LDS, where each counts those above
+// it.  (A lane's chunk stands for its last column: the key is then at most the column's own.)
+// Where more than kCand are left, which takes most of the largest logits in the columns of a few
+// lanes, k searches follow.
+template <typename T, int kLanes, typename Put>
+__device__ inline void top_of(const T *z, int d, int q0, int end, int k, int lane, float m, int most,
+                              TopLds<kLanes, true> &lds, Put put) {
+  constexpr int N = kCols<T>;
+  lds.keys[lane] = key_of(m, min(most + N, d) - 1);
+  if (lane == 0) lds.lanes = lds.count = 0;
+  group_sync<kLanes>();
+  uint64_t key = lds.keys[lane % 64];
+#pragma unroll
+  for (int w = 1; w < kLanes / 64; ++w) key = larger(key, lds.keys[w * 64 + lane % 64]);
+  const uint64_t bound = kth_largest(key, k);
+  if (key_of(m, 0) >= bound) lds.who[atomicAdd(&lds.lanes, 1u)] = (uint16_t)lane;
+  group_sync<kLanes>();
+  const uint32_t lanes = lds.lanes, deals = (uint32_t)(end - q0 + kLanes - 1) / kLanes;
+  for (uint32_t i = lane; i < lanes * deals; i += kLanes) {
+    const int q = q0 + (int)lds.who[i % lanes] + (int)(i / lanes) * kLanes;
+    if (q >= end) continue;
+    float v[N];
+    chunk_numbers(z, q, end, d, v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint64_t key = key_of(v[j], N * q + j);
+      if (key < bound) continue;
+      const uint32_t at = atomicAdd(&lds.count, 1u);
+      if (at < (uint32_t)kCand<kLanes>) lds.keys[at] = key;
+    }
+  }
+  group_sync<kLanes>();
+  const int count = (int)lds.count;
+  if (count > kCand<kLanes>) {
+    top_searches<T, kLanes>(z, d, q0, end, k, lane, lds.best, put);
+    return;
+  }
+  for (int i = lane; i < max(count, k); i += kLanes) {
+    if (i >= count) {
+      put(i, (uint64_t)0);
       continue;
     }
-    constexpr bool kT = kWhat & kEntropy;
-    const End e = end_of(group_sums<kLanes, kT>(lane_sums<T, kLanes, kT>(z, a.d, lane, a.c), a.c, sums));
-    if (lane == 0) {
-      const int id = token(o.ids, row, a.d);
-      score_row(o, row, id, id < 0 ? 0.0f : (float)z[id], e, a.scale);
+    const uint64_t mine = lds.keys[i];
+    int above = 0;
+    for (int j = 0; j < count; ++j) above += lds.keys[j] > mine;
+    if (above < k) put(above, mine);
+  }
+}
+
+// kLanes lanes to a row, kPer chunks of a lane asked for at once.
+template <typename T, int kLanes, int kPer, int kWhat>
+__global__ __launch_bounds__(kLanes > kBlock ? kLanes : kBlock) void score_kernel(Rows<T> a, Score o, Teacher t) {
+  constexpr int kGroups = (kLanes > kBlock ? kLanes : kBlock) / kLanes;
+  constexpr bool kT = kWhat & kEntropy;
+  __shared__ Sums sums_lds[kGroups][kLanes / 64];
+  __shared__ float teach_lds[kGroups][kWhat & kTeach ? kLanes / 64 * 4 : 1];
+  __shared__ TopLds<kLanes, (kWhat & kTop) != 0> top_lds[kGroups];
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  for (uint32_t row = blockIdx.x * kGroups + group; row < a.n; row += gridDim.x * kGroups) {
+    const T *z = a.Z + (int64_t)row * a.ldz;
+    group_sync<kLanes>();      // the row before is done with LDS
+    Taught<kLanes> x;
+    int id = -1;
+    float zt = 0.0f;
+    if (kWhat & kTeach) {
+      x = teach<T, kLanes>(t, row, z, a.d, lane, teach_lds[group]);
+    } else {
+      id = token(o.ids, row, a.d);
+      if (id >= 0) zt = (float)z[id];
     }
-    if (kWhat & kTop) top_rounds<T, kLanes>(a, o, row, lane, e, keys);
+    Sums s{kNone, 0.0f, 0.0f};
+    int most = 0;
+    Batch<T, kLanes, kPer> b;
+    for (int q = 0; q < a.chunks; q += kLanes * kPer) {
+      b.load(z, q, a.chunks, a.d, lane);
+      add_batch<kT>(b, a.c, s, most);
+    }
+    const float m = s.m;
+    const End e = end_of(group_sums<kLanes, kT>(s, a.c, sums_lds[group]));
+    if (kWhat & kTeach) {
+      const float loss = taught_loss<kLanes>(x, e, a.scale, teach_lds[group] + 3 * (kLanes / 64));
+      if (lane == 0) t.loss[row] = loss;
+    } else if (lane == 0) {
+      score_row(o, row, id, zt, e, a.scale);
+    }
+    if constexpr ((kWhat & kTop) != 0)
+      top_of<T, kLanes>(z, a.d, 0, a.chunks, o.k, lane, m, most, top_lds[group], [&](int r, uint64_t key) {
+        put_top(o, (int64_t)row * o.k + r, key, e, a.scale);
+      });
   }
 }
 
 template <typename T, int kWhat>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_t s) {
-  const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 20));
-  hipLaunchKernelGGL((score_kernel<T, kBlock, kWhat>), grid, dim3(kBlock), 0, s, a, o, t);
+#define TOC_SCORE(L, K)                                                                          \
+  hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>),                                             \
+                     dim3((unsigned)std::min<int64_t>((a.n + std::max(kBlock / L, 1) - 1) / std::max(kBlock / L, 1), \
+                                                      1 << 20)), \
+                     dim3(std::max(kBlock, L)), 0, s, a, o, t)
+  if (a.chunks <= 256) TOC_SCORE(64, 4);
+  else if (a.n >= 512 || a.chunks <= 1024) TOC_SCORE(256, 4);
+  else TOC_SCORE(1024, 4);
+#undef TOC_SCORE
   return launched("score_kernel");
 }
 
@@ -131,11 +230,6 @@ toc_status score(const Rows<T> &a, const Score &o, hipStream_t s) {
   const Teacher t{};
   if (o.k) return o.entropy ? launch<T, kTop | kEntropy>(a, o, t, s) : launch<T, kTop>(a, o, t, s);
   return o.entropy ? launch<T, kEntropy>(a, o, t, s) : launch<T, 0>(a, o, t, s);
-}
-
-template <typename T>
-Rows<T> rows_of(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale) {
-  return Rows<T>{(uint32_t)n, d, (const T *)Z, ldz, scale, scale * kLog2e};
 }
 
 }  // namespace

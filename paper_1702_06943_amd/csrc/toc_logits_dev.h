@@ -70,13 +70,89 @@ __device__ inline Sums group_sums(Sums a, float c, Sums *lds) {
   return all;
 }
 
-// The numbers of a chunk that starts at column at of a row of d: minus infinity past its end.
-template <typename T>
-__device__ inline void widen_row(Chunk x, int at, int d, float (&v)[kCols<T>]) {
-  widen<T>(x, v);
-  if (at + kCols<T> > d) {
+// What a group's lanes wrote to LDS is there for all of them.
+template <int kLanes>
+__device__ inline void group_sync() {
+  if (kLanes > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// --- a row's columns -------------------------------------------------------------
+
+// Up to kPer chunks of a lane of a group, of the chunks q .. end - 1 of a row of d columns: lane i
+// holds chunks q + i, q + i + kLanes and so on, as they lie in memory.  All loads are asked for
+// before any is used.
+template <typename T, int kLanes, int kPer>
+struct Batch {
+  static constexpr int N = kCols<T>;
+  Chunk in[kPer];
+  int q, end, d, lane;
+
+  // Whether any lane has a chunk k, and whether all have whole ones (the same in all lanes).
+  __device__ inline bool any(int k) const { return q + k * kLanes < end; }
+  __device__ inline bool whole(int k) const { return q + (k + 1) * kLanes <= min(end, d / N); }
+  __device__ inline int column(int k) const { return N * (q + k * kLanes + lane); }
+
+  __device__ inline void load(const T *row, int q_, int end_, int d_, int lane_) {
+    q = q_;
+    end = end_;
+    d = d_;
+    lane = lane_;
 #pragma unroll
-    for (int i = 0; i < kCols<T>; ++i) v[i] = at + i < d ? v[i] : kNone;
+    for (int k = 0; k < kPer; ++k) {
+      if (!any(k)) continue;
+      if (whole(k)) in[k] = *(const Unaligned *)(row + column(k));
+      else in[k] = fetch(row, place<T, true>(column(k), d));
+    }
+  }
+  // The numbers of chunk k: minus infinity past the row's end, and in a chunk past `end`.
+  __device__ inline void numbers(int k, float (&v)[N]) const {
+    if (whole(k)) {
+      widen<T>(in[k], v);
+      return;
+    }
+    const int at = column(k), stop = min(d, N * end);
+    widen<T>(settle(in[k], place<T, true>(at, d)), v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = at + i < stop ? v[i] : kNone;
+  }
+};
+
+// A lane's sums with its batch's numbers added; most: the first column of the first chunk that
+// holds its largest logit.
+template <bool kT, typename T, int kLanes, int kPer>
+__device__ inline void add_batch(const Batch<T, kLanes, kPer> &b, float c, Sums &a, int &most) {
+  constexpr int N = kCols<T>;
+  float m = a.m;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (!b.any(k)) continue;
+    float v[N];
+    b.numbers(k, v);
+    float x = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) x = fmaxf(x, v[i]);
+    if (x > m) most = b.column(k);
+    m = fmaxf(m, x);
+  }
+  const float base = from(m);
+  a = moved<kT>(a, base, c);
+  a.m = m;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (!b.any(k)) continue;
+    float v[N];
+    b.numbers(k, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = (v[i] - base) * c, e = two_to(y);
+      a.s += e;
+      if (kT) a.t = fmaf(e, fmaxf(y, kFar), a.t);
+    }
   }
 }
 
@@ -123,7 +199,12 @@ struct Rows {
   const T *Z;
   int64_t ldz;
   float scale, c;      // c = scale log2(e)
+  int chunks;          // of a row
 };
+template <typename T>
+Rows<T> rows_of(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale) {
+  return Rows<T>{(uint32_t)n, d, (const T *)Z, ldz, scale, scale * kLog2e, (int)chunks_of<T>(d)};
+}
 
 // Log probabilities: what is asked for, each but ids may be NULL.
 struct Score {

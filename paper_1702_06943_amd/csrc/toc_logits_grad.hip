@@ -50,22 +50,11 @@ __global__ __launch_bounds__(kBlock) void grad_kernel(Rows<T> a, Score o, Teache
       if (g.dentropy) ge = g.dentropy[row];
     }
     Sums s{kNone, 0.0f, 0.0f};
-    for (int at = N * lane; at < a.d; at += N * kLanes) {
-      const Place<T, true> l = place<T, true>(at, a.d);
-      float v[N];
-      widen_row<T>(settle(fetch(z, l), l), at, a.d, v);
-      float m = s.m;
-#pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-      const float base = from(m);
-      s = moved<kEntropy>(s, base, a.c);
-      s.m = m;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float y = (v[i] - base) * a.c, e = two_to(y);
-        s.s += e;
-        if (kEntropy) s.t = fmaf(e, fmaxf(y, kFar), s.t);
-      }
+    int most = 0;
+    Batch<T, kLanes, 4> b;
+    for (int q = 0; q < a.chunks; q += kLanes * 4) {
+      b.load(z, q, a.chunks, a.d, lane);
+      add_batch<kEntropy>(b, a.c, s, most);
     }
     s = group_sums<kLanes, kEntropy>(s, a.c, sums);
     const End e = end_of(s);
@@ -84,19 +73,24 @@ __global__ __launch_bounds__(kBlock) void grad_kernel(Rows<T> a, Score o, Teache
     k.a = a.scale * (gs - gl + ge * e.t_s) / s.s;
     k.b = -a.scale * ge * kLn2 / s.s;
     const float base = from(e.m);
-    for (int at = N * lane; at < a.d; at += N * kLanes) {
-      const Place<T, true> l = place<T, true>(at, a.d);
-      float v[N];
-      widen_row<T>(settle(fetch(z, l), l), at, a.d, v);
+    for (int q = 0; q < a.chunks; q += kLanes * 4) {
+      b.load(z, q, a.chunks, a.d, lane);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float y = (v[i] - base) * a.c;
-        const float p = two_to(y);
-        y = fmaxf(y, kFar);
-        v[i] = k.none ? 0.0f : p * (kEntropy ? fmaf(k.b, y, k.a) : k.a);
-        if (!kTeach && at + i == id && !k.none) v[i] = fmaf(a.scale, gl, v[i]);
+      for (int j = 0; j < 4; ++j) {
+        if (!b.any(j)) continue;
+        float v[N];
+        b.numbers(j, v);
+        const int at = b.column(j);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          float y = (v[i] - base) * a.c;
+          const float p = two_to(y);
+          y = fmaxf(y, kFar);
+          v[i] = k.none ? 0.0f : p * (kEntropy ? fmaf(k.b, y, k.a) : k.a);
+          if (!kTeach && at + i == id && !k.none) v[i] = fmaf(a.scale, gl, v[i]);
+        }
+        if (at < a.d) store(dz + at, a.d - at, v, false);
       }
-      store(dz + at, a.d - at, v, false);
     }
     if (kTeach) {
       // the columns with entries, written again: an entry's column by its first one, with the sum of
@@ -142,7 +136,7 @@ template <typename T, bool kTeach>
 toc_status grad(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale, const Score &o,
                 const Teacher &t, void *dZ, int64_t lddz, const float *dlogp, const float *dlse,
                 const float *dentropy, const float *dloss, void *stream) {
-  const Rows<T> a{(uint32_t)n, d, (const T *)Z, ldz, scale, scale * kLog2e};
+  const Rows<T> a = rows_of<T>(n, d, Z, ldz, scale);
   const Grad<T> g{(T *)dZ, lddz, dlogp, dlse, dentropy, dloss};
   return launch<T, kTeach>(a, o, t, g, (hipStream_t)stream);
 }
