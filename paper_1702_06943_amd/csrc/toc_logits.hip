@@ -45,9 +45,7 @@ struct TopLds {
 // The numbers of chunk q < end of a row.
 template <typename T>
 __device__ inline void chunk_numbers(const T *z, int q, int end, int d, float (&v)[kCols<T>]) {
-  Batch<T, 64, 1> b;
-  b.load(z, q, end, d, 0);
-  b.numbers(0, v);
+  widen<T>(edge_chunk(z, kCols<T> * q, min(d, kCols<T> * end), d), v);
 }
 
 __device__ inline uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
@@ -170,54 +168,53 @@ __device__ inline void top_of(const T *z, int d, int q0, int end, int k, int lan
 
 // kLanes lanes to a row, kPer chunks of a lane asked for at once.
 template <typename T, int kLanes, int kPer, int kWhat>
-__global__ __launch_bounds__(kLanes > kBlock ? kLanes : kBlock) void score_kernel(Rows<T> a, Score o, Teacher t) {
-  constexpr int kGroups = (kLanes > kBlock ? kLanes : kBlock) / kLanes;
+__global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Score o, Teacher t) {
+  constexpr int kGroups = kThreads<kLanes> / kLanes;
   constexpr bool kT = kWhat & kEntropy;
   __shared__ Sums sums_lds[kGroups][kLanes / 64];
-  __shared__ float teach_lds[kGroups][kWhat & kTeach ? kLanes / 64 * 4 : 1];
   __shared__ TopLds<kLanes, (kWhat & kTop) != 0> top_lds[kGroups];
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  for (uint32_t row = blockIdx.x * kGroups + group; row < a.n; row += gridDim.x * kGroups) {
-    const T *z = a.Z + (int64_t)row * a.ldz;
-    group_sync<kLanes>();      // the row before is done with LDS
-    Taught<kLanes> x;
-    int id = -1;
-    float zt = 0.0f;
+  const int lane = lane_of<kLanes>(), group = group_of<kLanes>();
+  const int64_t row = row_of<kLanes>();
+  if (row >= a.n) return;
+  const T *z = a.Z + row * a.ldz;
+  const bool first = lane < 64;          // the wave that has the row's few numbers
+  Taught x;
+  if ((kWhat & kTeach) && first) x.ask(t, row, a.d, lane);
+  const int id = kWhat & kTeach ? -1 : scalar_token(o.ids, row, a.d);
+  Batch<T, kLanes, kPer> b;
+  b.load(z, 0, a.chunks, a.d, lane);
+  float zt = 0.0f;
+  if ((kWhat & kTeach) && first) x.gather(t, z);
+  if (id >= 0) zt = (float)z[id];
+  Sums s{kNone, 0.0f, 0.0f};
+  int most = 0;
+  add_batch<kT>(b, a.c, s, most);
+  while (b.next < a.chunks) {
+    b.load(z, b.next, a.chunks, a.d, lane);
+    add_batch<kT>(b, a.c, s, most);
+  }
+  const float m = s.m;
+  const End e = end_of(group_sums<kLanes, kT>(s, a.c, sums_lds[group]));
+  if (first) {
     if (kWhat & kTeach) {
-      x = teach<T, kLanes>(t, row, z, a.d, lane, teach_lds[group]);
-    } else {
-      id = token(o.ids, row, a.d);
-      if (id >= 0) zt = (float)z[id];
-    }
-    Sums s{kNone, 0.0f, 0.0f};
-    int most = 0;
-    Batch<T, kLanes, kPer> b;
-    for (int q = 0; q < a.chunks; q += kLanes * kPer) {
-      b.load(z, q, a.chunks, a.d, lane);
-      add_batch<kT>(b, a.c, s, most);
-    }
-    const float m = s.m;
-    const End e = end_of(group_sums<kLanes, kT>(s, a.c, sums_lds[group]));
-    if (kWhat & kTeach) {
-      const float loss = taught_loss<kLanes>(x, e, a.scale, teach_lds[group] + 3 * (kLanes / 64));
+      x.learn(t, row);
+      const float loss = x.loss(e, a.scale);
       if (lane == 0) t.loss[row] = loss;
     } else if (lane == 0) {
       score_row(o, row, id, zt, e, a.scale);
     }
-    if constexpr ((kWhat & kTop) != 0)
-      top_of<T, kLanes>(z, a.d, 0, a.chunks, o.k, lane, m, most, top_lds[group], [&](int r, uint64_t key) {
-        put_top(o, (int64_t)row * o.k + r, key, e, a.scale);
-      });
   }
+  if constexpr ((kWhat & kTop) != 0)
+    top_of<T, kLanes>(z, a.d, 0, a.chunks, o.k, lane, m, most, top_lds[group], [&](int r, uint64_t key) {
+      put_top(o, row * o.k + r, key, e, a.scale);
+    });
 }
 
 template <typename T, int kWhat>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_t s) {
 #define TOC_SCORE(L, K)                                                                          \
   hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>),                                             \
-                     dim3((unsigned)std::min<int64_t>((a.n + std::max(kBlock / L, 1) - 1) / std::max(kBlock / L, 1), \
-                                                      1 << 20)), \
-                     dim3(std::max(kBlock, L)), 0, s, a, o, t)
+                     grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t)
   if (a.chunks <= 256) TOC_SCORE(64, 4);
   else if (a.n >= 512 || a.chunks <= 1024) TOC_SCORE(256, 4);
   else TOC_SCORE(1024, 4);

@@ -33,9 +33,11 @@ __device__ inline float two_to(float y) { return __builtin_amdgcn_exp2f(y); }
 // What logits are measured from: 0 where all of them are minus infinity.
 __device__ inline float from(float m) { return m == kNone ? 0.0f : m; }
 
-// The sums as they are measured from base instead of a.m <= base.
+// The sums as they are measured from base instead of a.m <= base.  (Lanes that add each other's have
+// to get the same bits: the products must not become part of one's addition.)
 template <bool kT>
 __device__ inline Sums moved(Sums a, float base, float c) {
+#pragma clang fp contract(off)
   const float y = fmaxf((a.m - base) * c, kFar), f = two_to(y);
   return Sums{base, a.s * f, kT ? fmaf(a.s, y, a.t) * f : 0.0f};
 }
@@ -57,17 +59,20 @@ __device__ inline Sums group_sums(Sums a, float c, Sums *lds) {
   if (kLanes == 64) return w;
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = w;
   __syncthreads();
-  m = lds[0].m;
+  // every wave's sums again by all waves, one in a lane
+  constexpr int kWaves = kLanes / 64;
+  w = lds[threadIdx.x % kWaves];
+  m = w.m;
 #pragma unroll
-  for (int i = 1; i < kLanes / 64; ++i) m = fmaxf(m, lds[i].m);
-  Sums all{m, 0.0f, 0.0f};
+  for (int o = kWaves / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  w = moved<kT>(w, from(m), c);
 #pragma unroll
-  for (int i = 0; i < kLanes / 64; ++i) {
-    const Sums x = moved<kT>(lds[i], from(m), c);
-    all.s += x.s;
-    if (kT) all.t += x.t;
+  for (int o = kWaves / 2; o > 0; o >>= 1) {
+    w.s += __shfl_xor(w.s, o, 64);
+    if (kT) w.t += __shfl_xor(w.t, o, 64);
   }
-  return all;
+  w.m = m;
+  return w;
 }
 
 // What a group's lanes wrote to LDS is there for all of them.
@@ -83,77 +88,135 @@ __device__ inline void group_sync() {
 
 // --- a row's columns -------------------------------------------------------------
 
-// Up to kPer chunks of a lane of a group, of the chunks q .. end - 1 of a row of d columns: lane i
-// holds chunks q + i, q + i + kLanes and so on, as they lie in memory.  All loads are asked for
-// before any is used.
+// A chunk of T whose columns from `left` on are minus infinity.
+template <typename T>
+__device__ inline Chunk cut(Chunk x, int left) {
+  constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, bf16>::value ? 0xff80u : 0xfc00u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      x[i] = i < left ? x[i] : none;
+    } else {
+      const uint32_t low = 2 * i < left ? x[i] & 0xffffu : none;
+      const uint32_t high = 2 * i + 1 < left ? x[i] & 0xffff0000u : none << 16;
+      x[i] = low | high;
+    }
+  }
+  return x;
+}
+
+// A chunk whose first column is `at` of a row of d columns, the columns from stop <= d on as
+// minus infinity.
+template <typename T>
+__device__ inline Chunk edge_chunk(const T *row, int at, int stop, int d) {
+  const Place<T, true> l = place<T, true>(at, d);
+  return cut<T>(settle(fetch(row, l), l), stop - at);
+}
+
+// Chunks q .. end - 1 of a row of d columns, or as many of them as a batch takes, as they lie in
+// memory: up to kPer rows of kLanes whole chunks, lane i's the i-th of each, and what is left
+// after them where that is less than such a row (`edge`: minus infinity past the row's end and in
+// chunks from `end` on).  All loads are asked for before any is used.  What is the same in all
+// lanes (the row, q, end, d) is in scalar registers, and a lane's offset is one vector register
+// for all its loads.
 template <typename T, int kLanes, int kPer>
 struct Batch {
   static constexpr int N = kCols<T>;
-  Chunk in[kPer];
-  int q, end, d, lane;
+  Chunk in[kPer], edge;
+  int q, rows, next, lane;        // first chunk, rows of whole chunks, first chunk after the batch
+  bool ragged;                    // whether there is an edge
 
-  // Whether any lane has a chunk k, and whether all have whole ones (the same in all lanes).
-  __device__ inline bool any(int k) const { return q + k * kLanes < end; }
-  __device__ inline bool whole(int k) const { return q + (k + 1) * kLanes <= min(end, d / N); }
   __device__ inline int column(int k) const { return N * (q + k * kLanes + lane); }
 
-  __device__ inline void load(const T *row, int q_, int end_, int d_, int lane_) {
+  __device__ inline void load(const T *row, int q_, int end, int d, int lane_) {
     q = q_;
-    end = end_;
-    d = d_;
     lane = lane_;
+    const int whole = min(end, d / N);
+    rows = min(kPer, (whole - q) / kLanes);
+    next = q + rows * kLanes;
+    ragged = next < end && whole - next < kLanes;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      if (!any(k)) continue;
-      if (whole(k)) in[k] = *(const Unaligned *)(row + column(k));
-      else in[k] = fetch(row, place<T, true>(column(k), d));
+    for (int k = 0; k < kPer; ++k)
+      if (k < rows) in[k] = *(const Unaligned *)((const char *)(row + N * (q + k * kLanes)) + (uint32_t)(16 * lane));
+    if (ragged) {
+      edge = edge_chunk(row, N * (next + lane), min(d, N * end), d);
+      next = end;
     }
   }
-  // The numbers of chunk k: minus infinity past the row's end, and in a chunk past `end`.
-  __device__ inline void numbers(int k, float (&v)[N]) const {
-    if (whole(k)) {
-      widen<T>(in[k], v);
-      return;
-    }
-    const int at = column(k), stop = min(d, N * end);
-    widen<T>(settle(in[k], place<T, true>(at, d)), v);
+  // Keeps the compiler from holding the widened numbers, at twice the registers, from one pass over
+  // the batch to the next.
+  __device__ inline void again() {
+    if (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = at + i < stop ? v[i] : kNone;
+      for (int k = 0; k < kPer; ++k) asm volatile("" : "+v"(in[k]));
+    }
+  }
+  // f(k, chunk) for each of a lane's chunks; the scheduler keeps them apart, so that one chunk's
+  // numbers at a time are in registers.
+  template <typename F>
+  __device__ inline void each(F f) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (k < rows) f(k, in[k]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (ragged) f(rows, edge);
   }
 };
 
 // A lane's sums with its batch's numbers added; most: the first column of the first chunk that
 // holds its largest logit.
 template <bool kT, typename T, int kLanes, int kPer>
-__device__ inline void add_batch(const Batch<T, kLanes, kPer> &b, float c, Sums &a, int &most) {
+__device__ inline void add_batch(Batch<T, kLanes, kPer> &b, float c, Sums &a, int &most) {
   constexpr int N = kCols<T>;
   float m = a.m;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (!b.any(k)) continue;
+  b.each([&](int k, Chunk in) {
     float v[N];
-    b.numbers(k, v);
+    widen<T>(in, v);
     float x = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) x = fmaxf(x, v[i]);
     if (x > m) most = b.column(k);
     m = fmaxf(m, x);
-  }
+  });
   const float base = from(m);
   a = moved<kT>(a, base, c);
   a.m = m;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (!b.any(k)) continue;
+  b.again();
+  b.each([&](int, Chunk in) {
     float v[N];
-    b.numbers(k, v);
+    widen<T>(in, v);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float y = (v[i] - base) * c, e = two_to(y);
       a.s += e;
       if (kT) a.t = fmaf(e, fmaxf(y, kFar), a.t);
     }
-  }
+  });
+}
+
+// Workgroups of kBlock threads, or kLanes where those are more; a group of kLanes lanes has one row.
+// (Without a loop over rows: hoisted out of one, constants took some thirty registers a lane.)
+template <int kLanes>
+constexpr int kThreads = kLanes > kBlock ? kLanes : kBlock;
+template <int kLanes>
+inline dim3 grid_of(int64_t rows) {
+  const int64_t blocks = (rows + kThreads<kLanes> / kLanes - 1) / (kThreads<kLanes> / kLanes);
+  const int64_t wide = std::min<int64_t>(blocks, 1 << 20);
+  return dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide));
+}
+// A thread's group of the workgroup, its row, both the same in all lanes of a wave, and its lane.
+template <int kLanes>
+__device__ inline int group_of() {
+  return kLanes >= kBlock ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);
+}
+template <int kLanes>
+__device__ inline int64_t row_of() {
+  return ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads<kLanes> / kLanes) + group_of<kLanes>();
+}
+template <int kLanes>
+__device__ inline int lane_of() {
+  return kLanes >= kBlock ? (int)threadIdx.x : (int)threadIdx.x % kLanes;
 }
 
 // --- a row's end -----------------------------------------------------------------
@@ -183,11 +246,21 @@ struct Ids {
   const void *p;   // or NULL: no token anywhere
   int bits;
 };
+__device__ inline int token_of(int64_t id, int d) { return id >= 0 && id < d ? (int)id : -1; }
 // Token number i, or -1 where it is none of 0..d-1.
 __device__ inline int token(const Ids &ids, int64_t i, int d) {
+  if (ids.bits == 32) return token_of(((const int32_t *)ids.p)[i], d);
+  return token_of(((const int64_t *)ids.p)[i], d);
+}
+// p[i] for an i that is the same in all lanes of a wave, by a scalar load, which no wait for a row's
+// loads holds up; what it reads is written by no launch that it runs in.
+template <typename V>
+__device__ inline V scalar(const V *p, int64_t i) {
+  return *(const __attribute__((address_space(4))) V *)(p + i);
+}
+__device__ inline int scalar_token(const Ids &ids, int64_t i, int d) {
   if (!ids.p) return -1;
-  const int64_t id = ids.bits == 32 ? (int64_t)((const int32_t *)ids.p)[i] : ((const int64_t *)ids.p)[i];
-  return id >= 0 && id < d ? (int)id : -1;
+  return token_of(ids.bits == 32 ? (int64_t)scalar((const int32_t *)ids.p, i) : scalar((const int64_t *)ids.p, i), d);
 }
 
 // --- arguments -------------------------------------------------------------------
@@ -228,108 +301,97 @@ struct Teacher {
 };
 
 // The numbers of a row's score, by one lane.  z: the given token's logit, if there is one.
-__device__ inline void score_row(const Score &a, uint32_t row, int id, float z, const End &e, float scale) {
+__device__ inline void score_row(const Score &a, int64_t row, int id, float z, const End &e, float scale) {
   if (a.logp) a.logp[row] = id < 0 ? 0.0f : log_p(z, e, scale);
   if (a.lse) a.lse[row] = log_sum(e, scale);
   if (a.entropy) a.entropy[row] = entropy(e);
 }
 
-// A lane's entries of a teacher's row: entry lane + i kLanes.
-template <int kLanes>
+__device__ inline float wave_sum(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ inline float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+// A teacher's row, by the first wave of a group while the others go on with theirs: a lane's entries
+// are lane, lane + 64 and so on.
 struct Taught {
-  static constexpr int kPer = (kMaxTeacher + kLanes - 1) / kLanes;
+  static constexpr int kPer = kMaxTeacher / 64;
   int id[kPer];        // -1: none
-  float t[kPer];       // scaled saved logit, then log q
+  float t[kPer];       // saved logit, then log q
   float z[kPer];       // the row's own logit there
   float q[kPer];
   float sum;           // of q over the row
+
+  // The columns and the saved logits: what the loads of the row's own logits wait for.
+  __device__ inline void ask(const Teacher &a, int64_t row, int d, int lane) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      id[i] = -1;
+      t[i] = kNone;
+      const int e = lane + 64 * i;
+      if (64 * i >= a.k || e >= a.k) continue;
+      id[i] = token(a.ids, row * a.ldi + e, d);
+      const int64_t at = row * a.ldt + e;
+      t[i] = a.type == TOC_F32 ? ((const float *)a.t)[at]
+             : a.type == TOC_BF16 ? (float)((const bf16 *)a.t)[at] : (float)((const f16 *)a.t)[at];
+    }
+  }
+  template <typename T>
+  __device__ inline void gather(const Teacher &a, const T *row) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      z[i] = 0.0f;
+      if (64 * i < a.k && id[i] >= 0) z[i] = (float)row[id[i]];
+    }
+  }
+  // The teacher's probabilities: q_a = exp(scale T_a - lse), or exp(scale (T_a - max T)) over its sum
+  // without lse.
+  __device__ inline void learn(const Teacher &a, int64_t row) {
+    float log_sum;
+    if (a.lse) {
+      log_sum = scalar(a.lse, row);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) t[i] = id[i] < 0 ? kNone : fmaf(a.scale, t[i], -log_sum);
+    } else {
+      float most = kNone;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) most = fmaxf(most, id[i] < 0 ? kNone : t[i]);
+      most = from(wave_max(most));
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        t[i] = id[i] < 0 ? kNone : a.scale * (t[i] - most);
+        if (64 * i < a.k) s += expf(t[i]);
+      }
+      s = wave_sum(s);
+      log_sum = logf(s);
+      // (no saved logit above minus infinity: s is 0, every q 0)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) t[i] = s == 0.0f ? kNone : t[i] - log_sum;
+    }
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      q[i] = id[i] < 0 ? 0.0f : expf(t[i]);
+      sum += q[i];
+    }
+    sum = wave_sum(sum);
+  }
+  // The row's loss: sum of q (log q - log p); an entry with q = 0 adds nothing.
+  __device__ inline float loss(const End &e, float scale) const {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (q[i] != 0.0f) s = fmaf(q[i], t[i] - log_p(z[i], e, scale), s);
+    return wave_sum(s);
+  }
 };
-
-template <int kLanes>
-__device__ inline float lanes_sum(float x, float *lds) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  if (kLanes == 64) return x;
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
-  __syncthreads();
-  x = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kLanes / 64; ++i) x += lds[i];
-  return x;
-}
-template <int kLanes>
-__device__ inline float lanes_max(float x, float *lds) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-  if (kLanes == 64) return x;
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
-  __syncthreads();
-  x = lds[0];
-#pragma unroll
-  for (int i = 1; i < kLanes / 64; ++i) x = fmaxf(x, lds[i]);
-  return x;
-}
-
-// Reads the entries and makes the teacher's probabilities:
-//   q_a = exp(scale T_a - lse), or exp(scale (T_a - max T)) over its sum without lse
-// lds: three times kLanes / 64 words, free again after the caller's next barrier.
-template <typename T, int kLanes>
-__device__ inline Taught<kLanes> teach(const Teacher &a, uint32_t row, const T *zrow, int d, int lane,
-                                       float *lds) {
-  Taught<kLanes> x;
-  float most = kNone;
-#pragma unroll
-  for (int i = 0; i < x.kPer; ++i) {
-    const int e = lane + i * kLanes;
-    x.id[i] = -1;
-    x.t[i] = kNone;
-    x.z[i] = 0.0f;
-    if (e < a.k) x.id[i] = token(a.ids, (int64_t)row * a.ldi + e, d);
-    if (x.id[i] >= 0) {
-      x.z[i] = (float)zrow[x.id[i]];
-      const int64_t at = (int64_t)row * a.ldt + e;
-      x.t[i] = a.type == TOC_F32 ? ((const float *)a.t)[at]
-               : a.type == TOC_BF16 ? (float)((const bf16 *)a.t)[at] : (float)((const f16 *)a.t)[at];
-    }
-    most = fmaxf(most, x.t[i]);
-  }
-  float sum = 0.0f, log_sum;
-  if (a.lse) {
-    log_sum = a.lse[row];
-#pragma unroll
-    for (int i = 0; i < x.kPer; ++i) x.t[i] = x.id[i] < 0 ? kNone : fmaf(a.scale, x.t[i], -log_sum);
-  } else {
-    most = from(lanes_max<kLanes>(most, lds));
-#pragma unroll
-    for (int i = 0; i < x.kPer; ++i) {
-      x.t[i] = x.id[i] < 0 ? kNone : a.scale * (x.t[i] - most);
-      sum += expf(x.t[i]);
-    }
-    sum = lanes_sum<kLanes>(sum, lds + kLanes / 64);
-    log_sum = logf(sum);
-    // (no saved logit above minus infinity: sum is 0, every q 0)
-#pragma unroll
-    for (int i = 0; i < x.kPer; ++i) x.t[i] = sum == 0.0f ? kNone : x.t[i] - log_sum;
-  }
-  sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < x.kPer; ++i) {
-    x.q[i] = x.id[i] < 0 ? 0.0f : expf(x.t[i]);
-    sum += x.q[i];
-  }
-  x.sum = lanes_sum<kLanes>(sum, lds + 2 * (kLanes / 64));
-  return x;
-}
-
-// The row's loss, in every lane: sum of q (log q - log p); an entry with q = 0 adds nothing.
-template <int kLanes>
-__device__ inline float taught_loss(const Taught<kLanes> &x, const End &e, float scale, float *lds) {
-  float sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < x.kPer; ++i)
-    if (x.q[i] != 0.0f) sum = fmaf(x.q[i], x.t[i] - log_p(x.z[i], e, scale), sum);
-  return lanes_sum<kLanes>(sum, lds);
-}
 
 // --- checks ------------------------------------------------------------------------
 

@@ -15,120 +15,155 @@ struct Grad {
   int64_t lddz;
   const float *dlogp, *dlse, *dentropy;   // each may be NULL: zeros
   const float *dloss;
+  bool stream;
 };
 
-// A column's gradient before its target's part: e = 2^y of the softmax, y kept above kFar.
+// A column's gradient but for its target's part is e (a + b y), e = 2^y of the softmax.
 struct Slope {
-  float a, b;          // dz = e (a + b y)
-  bool none;           // the row's coefficients are all zero, or it has no probabilities
+  float a, b;
+  bool none;           // 0 throughout: the coefficients are 0, or there are no probabilities
 };
 
-template <typename T, int kLanes, bool kTeach, bool kEntropy>
-__global__ __launch_bounds__(kBlock) void grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g) {
+// The gradient of a lane's chunks; hit: what the column `id` gets on top.
+template <typename T, int kLanes, int kPer, bool kEntropy>
+__device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base, Slope k, int id, float hit,
+                                 T *dz, int d, bool stream) {
   constexpr int N = kCols<T>;
-  __shared__ Sums sums[kLanes / 64];
-  __shared__ float lds[kLanes / 64 * 4];
-  __shared__ int ids[kMaxTeacher];
-  __shared__ float qs[kMaxTeacher];
-  const int lane = threadIdx.x;
-  for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-    const T *z = a.Z + (int64_t)row * a.ldz;
-    T *dz = g.dZ + (int64_t)row * g.lddz;
-    __syncthreads();
-    Taught<kLanes> x;
-    int id = -1;
-    float zt = 0.0f, gl = 0.0f, gs = 0.0f, ge = 0.0f;
-    if (kTeach) {
-      x = teach<T, kLanes>(t, row, z, a.d, lane, lds);
-      gs = g.dloss[row] * x.sum;
-      if (g.dloss[row] == 0.0f) gs = 0.0f;
-    } else {
-      id = token(o.ids, row, a.d);
-      if (id >= 0) zt = (float)z[id];
-      if (id >= 0 && g.dlogp) gl = g.dlogp[row];
-      if (g.dlse) gs = g.dlse[row];
-      if (g.dentropy) ge = g.dentropy[row];
+  b.again();
+  b.each([&](int j, Chunk in) {
+    float v[N];
+    widen<T>(in, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = (v[i] - base) * c;
+      v[i] = two_to(y) * (kEntropy ? fmaf(k.b, fmaxf(y, kFar), k.a) : k.a);
     }
-    Sums s{kNone, 0.0f, 0.0f};
-    int most = 0;
-    Batch<T, kLanes, 4> b;
-    for (int q = 0; q < a.chunks; q += kLanes * 4) {
-      b.load(z, q, a.chunks, a.d, lane);
-      add_batch<kEntropy>(b, a.c, s, most);
+    const int at = b.column(j);
+    if ((uint32_t)(id - at) < (uint32_t)N) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += at + i == id ? hit : 0.0f;
     }
-    s = group_sums<kLanes, kEntropy>(s, a.c, sums);
-    const End e = end_of(s);
-    float loss = 0.0f;
-    if (kTeach) loss = taught_loss<kLanes>(x, e, a.scale, lds + 3 * (kLanes / 64));
-    else __syncthreads();          // the given token's logit is read before dZ, which may be Z, is written
-    if (lane == 0) {
-      if (kTeach) {
-        if (t.loss) t.loss[row] = loss;
-      } else {
-        score_row(o, row, id, zt, e, a.scale);
-      }
+    T *to = (T *)((char *)(dz + N * (b.q + j * kLanes)) + (uint32_t)(16 * b.lane));
+    if (j < b.rows) put(to, N, narrow<T>(v), stream);
+    else if (at < d) put(to, d - at, narrow<T>(v), stream);
+  });
+}
+
+// kLanes lanes to a row, kPer chunks to a lane: a row of as many chunks stays in registers between
+// its one read and its one write, a longer one is read twice.
+template <typename T, int kLanes, int kPer, bool kTeach, bool kEntropy>
+__global__ __launch_bounds__(kThreads<kLanes>) void grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g) {
+  constexpr int N = kCols<T>;
+  constexpr int kGroups = kThreads<kLanes> / kLanes;
+  __shared__ Sums sums[kGroups][kLanes / 64];
+  __shared__ float q_sum[kGroups];
+  __shared__ int ids_lds[kGroups][kTeach ? kMaxTeacher : 1];
+  __shared__ float q_lds[kGroups][kTeach ? kMaxTeacher : 1];
+  const int lane = lane_of<kLanes>(), group = group_of<kLanes>();
+  const int64_t row = row_of<kLanes>();
+  if (row >= a.n) return;
+  const T *z = a.Z + row * a.ldz;
+  T *dz = g.dZ + row * g.lddz;
+  const bool first = lane < 64;          // the wave that has the row's few numbers
+  Taught x;
+  if (kTeach && first) x.ask(t, row, a.d, lane);
+  int id = -1;
+  float gl = 0.0f, gs = 0.0f, ge = 0.0f;
+  if (kTeach) {
+    gl = scalar(g.dloss, row);
+  } else {
+    id = scalar_token(o.ids, row, a.d);
+    if (id >= 0 && g.dlogp) gl = scalar(g.dlogp, row);
+    if (g.dlse) gs = scalar(g.dlse, row);
+    if (g.dentropy) ge = scalar(g.dentropy, row);
+  }
+  Batch<T, kLanes, kPer> b;
+  b.load(z, 0, a.chunks, a.d, lane);
+  float zt = 0.0f;
+  if (kTeach && first) x.gather(t, z);
+  if (!kTeach && id >= 0) zt = (float)z[id];
+  Sums s{kNone, 0.0f, 0.0f};
+  int most = 0;
+  add_batch<kEntropy>(b, a.c, s, most);
+  while (b.next < a.chunks) {
+    b.load(z, b.next, a.chunks, a.d, lane);
+    add_batch<kEntropy>(b, a.c, s, most);
+  }
+  if (kTeach && first) {
+    x.learn(t, row);
+    if (lane == 0) q_sum[group] = x.sum;
+  }
+  // (behind this barrier dZ, which may be Z, is written: all of Z that is not read again is there)
+  s = group_sums<kLanes, kEntropy>(s, a.c, sums[group]);
+  const End e = end_of(s);
+  if (kTeach) {
+    if (kLanes == 64) group_sync<kLanes>();
+    gs = gl == 0.0f ? 0.0f : gl * q_sum[group];
+    if (first && t.loss) {
+      const float loss = x.loss(e, a.scale);
+      if (lane == 0) t.loss[row] = loss;
     }
-    Slope k;
+  } else if (lane == 0) {
+    score_row(o, row, id, zt, e, a.scale);
+  }
+  Slope k;
+  if (kTeach) {
+    k.none = e.empty || gs == 0.0f;
+    k.a = a.scale * gs / s.s;
+    k.b = 0.0f;
+  } else {
     k.none = e.empty || (gl == 0.0f && gs == 0.0f && ge == 0.0f);
     k.a = a.scale * (gs - gl + ge * e.t_s) / s.s;
     k.b = -a.scale * ge * kLn2 / s.s;
-    const float base = from(e.m);
-    for (int q = 0; q < a.chunks; q += kLanes * 4) {
-      b.load(z, q, a.chunks, a.d, lane);
+  }
+  if (k.none) {
+    for (int q = lane; q < a.chunks; q += kLanes) put(dz + N * q, a.d - N * q, Chunk{0u, 0u, 0u, 0u}, g.stream);
+    return;
+  }
+  const float base = from(e.m);
+  const bool held = b.q == 0;
+  for (int q = 0; q < a.chunks; q = b.next) {
+    if (!held) b.load(z, q, a.chunks, a.d, lane);
+    put_batch<T, kLanes, kPer, kEntropy>(b, a.c, base, k, id, a.scale * gl, dz, a.d, g.stream);
+  }
+  if (kTeach) {
+    // the columns with entries, written again: an entry's column by its first one, with the sum of
+    // them all
+    group_sync<kLanes>();
+    if (!first) return;
+    int *ids = ids_lds[group];
+    float *qs = q_lds[group];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!b.any(j)) continue;
-        float v[N];
-        b.numbers(j, v);
-        const int at = b.column(j);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          float y = (v[i] - base) * a.c;
-          const float p = two_to(y);
-          y = fmaxf(y, kFar);
-          v[i] = k.none ? 0.0f : p * (kEntropy ? fmaf(k.b, y, k.a) : k.a);
-          if (!kTeach && at + i == id && !k.none) v[i] = fmaf(a.scale, gl, v[i]);
-        }
-        if (at < a.d) store(dz + at, a.d - at, v, false);
-      }
+    for (int i = 0; i < x.kPer; ++i) {
+      ids[lane + 64 * i] = x.id[i];
+      qs[lane + 64 * i] = x.q[i];
     }
-    if (kTeach) {
-      // the columns with entries, written again: an entry's column by its first one, with the sum of
-      // them all
+    group_sync<64>();
 #pragma unroll
-      for (int i = 0; i < x.kPer; ++i) {
-        if (lane + i * kLanes < t.k) {
-          ids[lane + i * kLanes] = x.id[i];
-          qs[lane + i * kLanes] = x.q[i];
-        }
+    for (int i = 0; i < x.kPer; ++i) {
+      if (64 * i >= t.k || x.id[i] < 0) continue;
+      float q = 0.0f;
+      bool one = true;
+      for (int j = 0; j < t.k; ++j) {
+        if (ids[j] != x.id[i]) continue;
+        one = one && j >= lane + 64 * i;
+        q += qs[j];
       }
-      __syncthreads();
-      if (k.none) continue;
-#pragma unroll
-      for (int i = 0; i < x.kPer; ++i) {
-        if (x.id[i] < 0) continue;
-        float q = 0.0f;
-        bool first = true;
-        for (int b = 0; b < t.k; ++b) {
-          if (ids[b] != x.id[i]) continue;
-          first = first && b >= lane + i * kLanes;
-          q += qs[b];
-        }
-        const float p = two_to((x.z[i] - base) * a.c);
-        const float v = fmaf(p, k.a, -a.scale * g.dloss[row] * q);
-        if (first) dz[x.id[i]] = (T)v;
-      }
+      const float v = fmaf(two_to((x.z[i] - base) * a.c), k.a, -a.scale * gl * q);
+      if (one) dz[x.id[i]] = (T)v;
     }
   }
 }
 
-template <typename T, bool kTeach>
+template <typename T, bool kTeach, bool kEntropy>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad<T> &g, hipStream_t s) {
-  const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 20));
-  if (!kTeach && (o.entropy || g.dentropy))
-    hipLaunchKernelGGL((grad_kernel<T, kBlock, false, true>), grid, dim3(kBlock), 0, s, a, o, t, g);
-  else
-    hipLaunchKernelGGL((grad_kernel<T, kBlock, kTeach, false>), grid, dim3(kBlock), 0, s, a, o, t, g);
+#define TOC_GRAD(L, K)                                                                           \
+  hipLaunchKernelGGL((grad_kernel<T, L, K, kTeach, kEntropy>),                                   \
+                     grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
+  if (a.chunks <= 256) TOC_GRAD(64, 4);
+  else if (a.chunks <= 2048) TOC_GRAD(256, 8);
+  else TOC_GRAD(1024, 6);
+#undef TOC_GRAD
   return launched("grad_kernel");
 }
 
@@ -137,8 +172,11 @@ toc_status grad(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale, c
                 const Teacher &t, void *dZ, int64_t lddz, const float *dlogp, const float *dlse,
                 const float *dentropy, const float *dloss, void *stream) {
   const Rows<T> a = rows_of<T>(n, d, Z, ldz, scale);
-  const Grad<T> g{(T *)dZ, lddz, dlogp, dlse, dentropy, dloss};
-  return launch<T, kTeach>(a, o, t, g, (hipStream_t)stream);
+  const Grad<T> g{(T *)dZ, lddz, dlogp, dlse, dentropy, dloss, stream_out(n, d, sizeof(T))};
+  if constexpr (!kTeach) {
+    if (o.entropy || dentropy) return launch<T, false, true>(a, o, t, g, (hipStream_t)stream);
+  }
+  return launch<T, kTeach, false>(a, o, t, g, (hipStream_t)stream);
 }
 
 }  // namespace
