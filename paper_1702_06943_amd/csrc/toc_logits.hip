@@ -184,7 +184,10 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
   Batch<T, kLanes, kPer> b;
   b.load(z, 0, a.chunks, a.d, lane);
   float zt = 0.0f;
-  if ((kWhat & kTeach) && first) x.gather(t, z);
+  if ((kWhat & kTeach) && first) {
+    x.gather(t, z);
+    x.learn(t, row);
+  }
   if (id >= 0) zt = (float)z[id];
   Sums s{kNone, 0.0f, 0.0f};
   int most = 0;
@@ -193,13 +196,12 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
     b.load(z, b.next, a.chunks, a.d, lane);
     add_batch<kT>(b, a.c, s, most);
   }
+  if ((kWhat & kTeach) && first) x.compare();
   const float m = s.m;
   const End e = end_of(group_sums<kLanes, kT>(s, a.c, sums_lds[group]));
   if (first) {
     if (kWhat & kTeach) {
-      x.learn(t, row);
-      const float loss = x.loss(e, a.scale);
-      if (lane == 0) t.loss[row] = loss;
+      if (lane == 0) t.loss[row] = x.loss(e, a.scale);
     } else if (lane == 0) {
       score_row(o, row, id, zt, e, a.scale);
     }

@@ -319,14 +319,18 @@ __device__ inline float wave_max(float x) {
 }
 
 // A teacher's row, by the first wave of a group while the others go on with theirs: a lane's entries
-// are lane, lane + 64 and so on.
+// are lane, lane + 64 and so on.  The loss is
+//   sum q log q - sum q log p = sum q log q - scale (sum q (z - r) + (r - m) sum q) + log S sum q
+// with r the largest logit of the row at an entry's column: what the entries give is known before the
+// row's own sums are.
 struct Taught {
   static constexpr int kPer = kMaxTeacher / 64;
   int id[kPer];        // -1: none
-  float t[kPer];       // saved logit, then log q
+  float t[kPer];       // saved logit
   float z[kPer];       // the row's own logit there
   float q[kPer];
-  float sum;           // of q over the row
+  float sum, sum_log;  // of q and of q log q over the row
+  float r, sum_z;      // r, and the sum of q (z - r)
 
   // The columns and the saved logits: what the loads of the row's own logits wait for.
   __device__ inline void ask(const Teacher &a, int64_t row, int d, int lane) {
@@ -346,12 +350,12 @@ struct Taught {
   __device__ inline void gather(const Teacher &a, const T *row) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      z[i] = 0.0f;
+      z[i] = kNone;
       if (64 * i < a.k && id[i] >= 0) z[i] = (float)row[id[i]];
     }
   }
   // The teacher's probabilities: q_a = exp(scale T_a - lse), or exp(scale (T_a - max T)) over its sum
-  // without lse.
+  // without lse.  An entry that is none has q = 0.
   __device__ inline void learn(const Teacher &a, int64_t row) {
     float log_sum;
     if (a.lse) {
@@ -375,21 +379,35 @@ struct Taught {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) t[i] = s == 0.0f ? kNone : t[i] - log_sum;
     }
-    sum = 0.0f;
+    sum = sum_log = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      q[i] = id[i] < 0 ? 0.0f : expf(t[i]);
+      q[i] = 0.0f;
+      if (64 * i >= a.k) continue;
+      q[i] = expf(t[i]);
       sum += q[i];
+      if (q[i] != 0.0f) sum_log = fmaf(q[i], t[i], sum_log);
     }
     sum = wave_sum(sum);
+    sum_log = wave_sum(sum_log);
   }
-  // The row's loss: sum of q (log q - log p); an entry with q = 0 adds nothing.
-  __device__ inline float loss(const End &e, float scale) const {
-    float s = 0.0f;
+  // An entry with q = 0 adds nothing.  (Where entries of a column were put together, the same.)
+  __device__ inline void compare() {
+    r = kNone;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (q[i] != 0.0f) s = fmaf(q[i], t[i] - log_p(z[i], e, scale), s);
-    return wave_sum(s);
+      if (q[i] != 0.0f) r = fmaxf(r, z[i]);
+    r = from(wave_max(r));
+    sum_z = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (q[i] != 0.0f) sum_z = fmaf(q[i], z[i] - r, sum_z);
+    sum_z = wave_sum(sum_z);
+  }
+  __device__ inline float loss(const End &e, float scale) const {
+    if (sum == 0.0f) return 0.0f;
+    if (e.empty) return INFINITY;
+    return sum_log - scale * fmaf(r - e.m, sum, sum_z) + e.log_s * sum;
   }
 };
 

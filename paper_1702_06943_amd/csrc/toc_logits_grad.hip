@@ -24,10 +24,83 @@ struct Slope {
   bool none;           // 0 throughout: the coefficients are 0, or there are no probabilities
 };
 
-// The gradient of a lane's chunks; hit: what the column `id` gets on top.
-template <typename T, int kLanes, int kPer, bool kEntropy>
+// A teacher's entries by the chunk of a window of kChunks chunks that holds their column: head[c] is
+// 0 or the number, from 1, of the first entry of a list that goes on with next.  Made by one wave.
+template <int kChunks>
+struct Marks {
+  static constexpr int kHeads = (kChunks + 511) / 512 * 512;
+  uint16_t head[kHeads];
+  uint16_t next[kMaxTeacher];
+  int column[kMaxTeacher];
+  float q[kMaxTeacher];
+  float weight[kMaxTeacher];   // what an entry's column gets: q, or that of all entries of the column
+  float sum;                   // of q over the row
+
+  __device__ inline void keep(const Taught &x, int lane) {
+#pragma unroll
+    for (int i = 0; i < x.kPer; ++i) {
+      column[64 * i + lane] = x.id[i];
+      q[64 * i + lane] = x.q[i];
+    }
+    if (lane == 0) sum = x.sum;
+  }
+  // Marks the first k entries whose column is in chunks first .. first + kChunks - 1, chunks of n
+  // columns.
+  __device__ inline void mark(int k, int first, int n, int lane) {
+    for (int i = lane; i < kHeads / 8; i += 64) ((uint4 *)head)[i] = make_uint4(0, 0, 0, 0);
+    group_sync<64>();
+    bool crowded = false;
+    for (int e = lane; e < k; e += 64) {
+      const uint32_t c = (uint32_t)(column[e] / n - first);
+      weight[e] = q[e];
+      if (column[e] < 0 || c >= (uint32_t)kChunks) continue;
+      // (two heads to a word)
+      uint32_t *word = (uint32_t *)head + c / 2;
+      const uint32_t shift = c % 2 * 16;
+      uint32_t old = *word, seen;
+      do {
+        seen = old;
+        old = atomicCAS(word, seen, (seen & ~(0xffffu << shift)) | (uint32_t)(e + 1) << shift);
+      } while (old != seen);
+      next[e] = (uint16_t)(old >> shift);
+      crowded = crowded || next[e] != 0;
+    }
+    group_sync<64>();
+    if (!__any(crowded)) return;
+    // Entries of one chunk come in no fixed order.  Those of one column are put together in the first of
+    // them and the others count 0, so that the order of the rest does not matter: two along their
+    // list, as a sum of two has one value; of more, in the order of the entries.
+    for (int e = lane; e < k; e += 64) {
+      const uint32_t c = (uint32_t)(column[e] / n - first);
+      if (column[e] < 0 || c >= (uint32_t)kChunks) continue;
+      int same = 0;
+      float s = q[e];
+      for (uint32_t o = head[c]; o != 0; o = next[o - 1]) {
+        if (column[o - 1] != column[e] || (int)o - 1 == e) continue;
+        ++same;
+        s = (int)o - 1 < e ? 0.0f : q[e] + q[o - 1];
+      }
+      if (same > 1) {
+        s = 0.0f;
+        bool one = true;
+        for (int o = 0; o < k; ++o) {
+          if (column[o] != column[e]) continue;
+          one = one && o >= e;
+          s += q[o];
+        }
+        s = one ? s : 0.0f;
+      }
+      weight[e] = s;
+    }
+  }
+};
+struct NoMarks {};
+
+// The gradient of a lane's chunks.  hit: what the column `id` gets on top, or with a teacher's entries
+// what each gets for its q; window: the first chunk that they are marked from.
+template <bool kEntropy, typename T, int kLanes, int kPer, typename M>
 __device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base, Slope k, int id, float hit,
-                                 T *dz, int d, bool stream) {
+                                 const M &marks, T *dz, int d, bool stream) {
   constexpr int N = kCols<T>;
   b.again();
   b.each([&](int j, Chunk in) {
@@ -39,9 +112,18 @@ __device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base,
       v[i] = two_to(y) * (kEntropy ? fmaf(k.b, fmaxf(y, kFar), k.a) : k.a);
     }
     const int at = b.column(j);
-    if ((uint32_t)(id - at) < (uint32_t)N) {
+    if constexpr (std::is_same<M, NoMarks>::value) {
+      if ((uint32_t)(id - at) < (uint32_t)N) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += at + i == id ? hit : 0.0f;
+        for (int i = 0; i < N; ++i) v[i] += at + i == id ? hit : 0.0f;
+      }
+    } else {
+      for (uint32_t e = marks.head[j * kLanes + b.lane]; e != 0; e = marks.next[e - 1]) {
+        const int column = marks.column[e - 1];
+        const float q = marks.weight[e - 1];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = at + i == column ? fmaf(hit, q, v[i]) : v[i];
+      }
     }
     T *to = (T *)((char *)(dz + N * (b.q + j * kLanes)) + (uint32_t)(16 * b.lane));
     if (j < b.rows) put(to, N, narrow<T>(v), stream);
@@ -52,18 +134,19 @@ __device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base,
 // kLanes lanes to a row, kPer chunks to a lane: a row of as many chunks stays in registers between
 // its one read and its one write, a longer one is read twice.
 template <typename T, int kLanes, int kPer, bool kTeach, bool kEntropy>
-__global__ __launch_bounds__(kThreads<kLanes>) void grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g) {
+__global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 : 4) void grad_kernel(Rows<T> a, Score o,
+                                                                                                  Teacher t, Grad<T> g) {
   constexpr int N = kCols<T>;
   constexpr int kGroups = kThreads<kLanes> / kLanes;
+  using M = typename std::conditional<kTeach, Marks<kLanes *(kPer + 1)>, NoMarks>::type;
   __shared__ Sums sums[kGroups][kLanes / 64];
-  __shared__ float q_sum[kGroups];
-  __shared__ int ids_lds[kGroups][kTeach ? kMaxTeacher : 1];
-  __shared__ float q_lds[kGroups][kTeach ? kMaxTeacher : 1];
+  __shared__ M all_marks[kGroups];
   const int lane = lane_of<kLanes>(), group = group_of<kLanes>();
   const int64_t row = row_of<kLanes>();
   if (row >= a.n) return;
   const T *z = a.Z + row * a.ldz;
   T *dz = g.dZ + row * g.lddz;
+  M &marks = all_marks[group];
   const bool first = lane < 64;          // the wave that has the row's few numbers
   Taught x;
   if (kTeach && first) x.ask(t, row, a.d, lane);
@@ -82,6 +165,13 @@ __global__ __launch_bounds__(kThreads<kLanes>) void grad_kernel(Rows<T> a, Score
   float zt = 0.0f;
   if (kTeach && first) x.gather(t, z);
   if (!kTeach && id >= 0) zt = (float)z[id];
+  if constexpr (kTeach) {
+    if (first) {
+      x.learn(t, row);
+      marks.keep(x, lane);
+      marks.mark(t.k, 0, N, lane);
+    }
+  }
   Sums s{kNone, 0.0f, 0.0f};
   int most = 0;
   add_batch<kEntropy>(b, a.c, s, most);
@@ -89,20 +179,14 @@ __global__ __launch_bounds__(kThreads<kLanes>) void grad_kernel(Rows<T> a, Score
     b.load(z, b.next, a.chunks, a.d, lane);
     add_batch<kEntropy>(b, a.c, s, most);
   }
-  if (kTeach && first) {
-    x.learn(t, row);
-    if (lane == 0) q_sum[group] = x.sum;
-  }
+  if (kTeach && first) x.compare();
   // (behind this barrier dZ, which may be Z, is written: all of Z that is not read again is there)
   s = group_sums<kLanes, kEntropy>(s, a.c, sums[group]);
   const End e = end_of(s);
-  if (kTeach) {
+  if constexpr (kTeach) {
     if (kLanes == 64) group_sync<kLanes>();
-    gs = gl == 0.0f ? 0.0f : gl * q_sum[group];
-    if (first && t.loss) {
-      const float loss = x.loss(e, a.scale);
-      if (lane == 0) t.loss[row] = loss;
-    }
+    gs = gl == 0.0f ? 0.0f : gl * marks.sum;
+    if (lane == 0 && t.loss) t.loss[row] = x.loss(e, a.scale);
   } else if (lane == 0) {
     score_row(o, row, id, zt, e, a.scale);
   }
@@ -120,38 +204,20 @@ __global__ __launch_bounds__(kThreads<kLanes>) void grad_kernel(Rows<T> a, Score
     for (int q = lane; q < a.chunks; q += kLanes) put(dz + N * q, a.d - N * q, Chunk{0u, 0u, 0u, 0u}, g.stream);
     return;
   }
-  const float base = from(e.m);
+  const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
   const bool held = b.q == 0;
   for (int q = 0; q < a.chunks; q = b.next) {
-    if (!held) b.load(z, q, a.chunks, a.d, lane);
-    put_batch<T, kLanes, kPer, kEntropy>(b, a.c, base, k, id, a.scale * gl, dz, a.d, g.stream);
-  }
-  if (kTeach) {
-    // the columns with entries, written again: an entry's column by its first one, with the sum of
-    // them all
-    group_sync<kLanes>();
-    if (!first) return;
-    int *ids = ids_lds[group];
-    float *qs = q_lds[group];
-#pragma unroll
-    for (int i = 0; i < x.kPer; ++i) {
-      ids[lane + 64 * i] = x.id[i];
-      qs[lane + 64 * i] = x.q[i];
-    }
-    group_sync<64>();
-#pragma unroll
-    for (int i = 0; i < x.kPer; ++i) {
-      if (64 * i >= t.k || x.id[i] < 0) continue;
-      float q = 0.0f;
-      bool one = true;
-      for (int j = 0; j < t.k; ++j) {
-        if (ids[j] != x.id[i]) continue;
-        one = one && j >= lane + 64 * i;
-        q += qs[j];
+    if (!held) {
+      b.load(z, q, a.chunks, a.d, lane);
+      if constexpr (kTeach) {
+        if (q > 0) {
+          group_sync<kLanes>();
+          if (first) marks.mark(t.k, q, N, lane);
+          group_sync<kLanes>();
+        }
       }
-      const float v = fmaf(two_to((x.z[i] - base) * a.c), k.a, -a.scale * gl * q);
-      if (one) dz[x.id[i]] = (T)v;
     }
+    put_batch<kEntropy>(b, a.c, base, k, id, hit, marks, dz, a.d, g.stream);
   }
 }
 
@@ -162,7 +228,8 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
                      grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
   if (a.chunks <= 256) TOC_GRAD(64, 4);
   else if (a.chunks <= 2048) TOC_GRAD(256, 8);
-  else TOC_GRAD(1024, 6);
+  else if (a.chunks < 1024 * 7) TOC_GRAD(1024, 6);
+  else TOC_GRAD(1024, 12);
 #undef TOC_GRAD
   return launched("grad_kernel");
 }
