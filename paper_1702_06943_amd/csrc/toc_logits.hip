@@ -42,28 +42,34 @@ struct TopLds {
   uint32_t lanes, count;
 };
 
-// The numbers of chunk q < end of a row.
+// A row's chunks q0 .. end - 1.
 template <typename T>
-__device__ inline void chunk_numbers(const T *z, int q, int end, int d, float (&v)[kCols<T>]) {
-  widen<T>(edge_chunk(z, kCols<T> * q, min(d, kCols<T> * end), d), v);
-}
+struct Part {
+  const T *z;
+  int d, skew, q0, end;
+
+  __device__ inline int column(int q) const { return kCols<T> * q - skew; }
+  __device__ inline void numbers(int q, float (&v)[kCols<T>]) const {
+    widen<T>(edge_chunk(z, column(q), min(d, column(end)), d), v);
+  }
+};
 
 __device__ inline uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // The alternatives by k searches for the largest key below the last.
 template <typename T, int kLanes, typename Put>
-__device__ inline void top_searches(const T *z, int d, int q0, int end, int k, int lane, uint64_t *best_lds, Put put) {
+__device__ inline void top_searches(const Part<T> &p, int k, int lane, uint64_t *best_lds, Put put) {
   constexpr int N = kCols<T>;
   uint64_t last = ~(uint64_t)0;
   for (int r = 0; r < k; ++r) {
     uint64_t best = 0;
     if (last) {
-      for (int q = q0 + lane; q < end; q += kLanes) {
+      for (int q = p.q0 + lane; q < p.end; q += kLanes) {
         float v[N];
-        chunk_numbers(z, q, end, d, v);
+        p.numbers(q, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const uint64_t key = key_of(v[i], N * q + i);
+          const uint64_t key = key_of(v[i], p.column(q) + i);
           if (key < last) best = larger(key, best);
         }
       }
@@ -112,7 +118,7 @@ __device__ inline uint64_t kth_largest(uint64_t key, int k) {
   return least;
 }
 
-// The k largest keys of a group's chunks q0 .. end - 1, put(r, key) for the r-th of them (0: there
+// The k largest keys of a part, put(r, key) for the r-th of them (0: there
 // is none).  The sums' pass over the row leaves each lane's largest logit and its chunk.  Of lanes i,
 // i + 64, ... the largest such keys are 64 keys of different columns, so the k-th largest of them is
 // a lower bound of the k-th largest of all, and lanes whose own largest logit is below it have none
@@ -122,10 +128,9 @@ __device__ inline uint64_t kth_largest(uint64_t key, int k) {
 // Where more than kCand are left, which takes most of the largest logits in the columns of a few
 // lanes, k searches follow.
 template <typename T, int kLanes, typename Put>
-__device__ inline void top_of(const T *z, int d, int q0, int end, int k, int lane, float m, int most,
-                              TopLds<kLanes, true> &lds, Put put) {
+__device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int most, TopLds<kLanes, true> &lds, Put put) {
   constexpr int N = kCols<T>;
-  lds.keys[lane] = key_of(m, min(most + N, d) - 1);
+  lds.keys[lane] = key_of(m, min(most + N, p.d) - 1);
   if (lane == 0) lds.lanes = lds.count = 0;
   group_sync<kLanes>();
   uint64_t key = lds.keys[lane % 64];
@@ -134,15 +139,15 @@ __device__ inline void top_of(const T *z, int d, int q0, int end, int k, int lan
   const uint64_t bound = kth_largest(key, k);
   if (key_of(m, 0) >= bound) lds.who[atomicAdd(&lds.lanes, 1u)] = (uint16_t)lane;
   group_sync<kLanes>();
-  const uint32_t lanes = lds.lanes, deals = (uint32_t)(end - q0 + kLanes - 1) / kLanes;
+  const uint32_t lanes = lds.lanes, deals = (uint32_t)(p.end - p.q0 + kLanes - 1) / kLanes;
   for (uint32_t i = lane; i < lanes * deals; i += kLanes) {
-    const int q = q0 + (int)lds.who[i % lanes] + (int)(i / lanes) * kLanes;
-    if (q >= end) continue;
+    const int q = p.q0 + (int)lds.who[i % lanes] + (int)(i / lanes) * kLanes;
+    if (q >= p.end) continue;
     float v[N];
-    chunk_numbers(z, q, end, d, v);
+    p.numbers(q, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const uint64_t key = key_of(v[j], N * q + j);
+      const uint64_t key = key_of(v[j], p.column(q) + j);
       if (key < bound) continue;
       const uint32_t at = atomicAdd(&lds.count, 1u);
       if (at < (uint32_t)kCand<kLanes>) lds.keys[at] = key;
@@ -151,7 +156,7 @@ __device__ inline void top_of(const T *z, int d, int q0, int end, int k, int lan
   group_sync<kLanes>();
   const int count = (int)lds.count;
   if (count > kCand<kLanes>) {
-    top_searches<T, kLanes>(z, d, q0, end, k, lane, lds.best, put);
+    top_searches<T, kLanes>(p, k, lane, lds.best, put);
     return;
   }
   for (int i = lane; i < max(count, k); i += kLanes) {
@@ -182,7 +187,9 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
   if ((kWhat & kTeach) && first) x.ask(t, row, a.d, lane);
   const int id = kWhat & kTeach ? -1 : scalar_token(o.ids, row, a.d);
   Batch<T, kLanes, kPer> b;
-  b.load(z, 0, a.chunks, a.d, lane);
+  const int skew = skew_of(z, a.d);
+  const Part<T> p{z, a.d, skew, 0, chunks_in<T>(a.d, skew)};
+  b.load(z, skew, p.q0, p.end, a.d, lane);
   float zt = 0.0f;
   if ((kWhat & kTeach) && first) {
     x.gather(t, z);
@@ -192,8 +199,8 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
   Sums s{kNone, 0.0f, 0.0f};
   int most = 0;
   add_batch<kT>(b, a.c, s, most);
-  while (b.next < a.chunks) {
-    b.load(z, b.next, a.chunks, a.d, lane);
+  while (b.next < p.end) {
+    b.load(z, skew, b.next, p.end, a.d, lane);
     add_batch<kT>(b, a.c, s, most);
   }
   if ((kWhat & kTeach) && first) x.compare();
@@ -207,7 +214,7 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
     }
   }
   if constexpr ((kWhat & kTop) != 0)
-    top_of<T, kLanes>(z, a.d, 0, a.chunks, o.k, lane, m, most, top_lds[group], [&](int r, uint64_t key) {
+    top_of<T, kLanes>(p, o.k, lane, m, most, top_lds[group], [&](int r, uint64_t key) {
       put_top(o, row * o.k + r, key, e, a.scale);
     });
 }
@@ -218,7 +225,8 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_
   hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>),                                             \
                      grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t)
   if (a.chunks <= 256) TOC_SCORE(64, 4);
-  else if (a.n >= 512 || a.chunks <= 1024) TOC_SCORE(256, 4);
+  else if (a.chunks <= 2048) TOC_SCORE(256, 4);
+  else if (a.n >= 512) TOC_SCORE(512, 6);
   else TOC_SCORE(1024, 4);
 #undef TOC_SCORE
   return launched("score_kernel");

@@ -33,46 +33,56 @@ __device__ inline float two_to(float y) { return __builtin_amdgcn_exp2f(y); }
 // What logits are measured from: 0 where all of them are minus infinity.
 __device__ inline float from(float m) { return m == kNone ? 0.0f : m; }
 
-// The sums as they are measured from base instead of a.m <= base.  (Lanes that add each other's have
-// to get the same bits: the products must not become part of one's addition.)
+// The sums as they are measured from base instead of a.m <= base.
 template <bool kT>
 __device__ inline Sums moved(Sums a, float base, float c) {
-#pragma clang fp contract(off)
   const float y = fmaxf((a.m - base) * c, kFar), f = two_to(y);
   return Sums{base, a.s * f, kT ? fmaf(a.s, y, a.t) * f : 0.0f};
 }
 
+// Over a wave's lanes, the same in all of them: by shifts within rows of 16 lanes and broadcasts of
+// their last ones, each one operation on the way into the adder (lanes without a source take the
+// operation's neutral number); the last lane has the result.
+template <typename Op>
+__device__ inline float wave_all(float x, float neutral, Op op) {
+#define TOC_STEP(ctrl, rows)                                                                             \
+  x = op(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(neutral),          \
+                                                                  (int)__float_as_uint(x), ctrl, rows, 0xf, false)))
+  TOC_STEP(0x111, 0xf);   // from 1, 2, 4, 8 lanes below
+  TOC_STEP(0x112, 0xf);
+  TOC_STEP(0x114, 0xf);
+  TOC_STEP(0x118, 0xf);
+  TOC_STEP(0x142, 0xa);   // lane 15 of a row to the next, rows 1 and 3
+  TOC_STEP(0x143, 0xc);   // lane 31 to rows 2 and 3
+#undef TOC_STEP
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+__device__ inline float wave_sum(float x) {
+  return wave_all(x, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ inline float wave_max(float x) {
+  return wave_all(x, kNone, [](float a, float b) { return fmaxf(a, b); });
+}
+
+template <bool kT>
+__device__ inline Sums wave_sums(Sums a, float c) {
+  const float m = wave_max(a.m);
+  a = moved<kT>(a, from(m), c);
+  return Sums{m, wave_sum(a.s), kT ? wave_sum(a.t) : 0.0f};
+}
 // The sums of a group of kLanes lanes (64: a wave; else the whole workgroup, by way of
 // kLanes / 64 words of lds, which are free again after the caller's next barrier).
 template <int kLanes, bool kT>
 __device__ inline Sums group_sums(Sums a, float c, Sums *lds) {
-  float m = a.m;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  Sums w = moved<kT>(a, from(m), c);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    w.s += __shfl_xor(w.s, o, 64);
-    if (kT) w.t += __shfl_xor(w.t, o, 64);
-  }
-  w.m = m;
-  if (kLanes == 64) return w;
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = w;
+  a = wave_sums<kT>(a, c);
+  if (kLanes == 64) return a;
+  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = a;
   __syncthreads();
   // every wave's sums again by all waves, one in a lane
-  constexpr int kWaves = kLanes / 64;
-  w = lds[threadIdx.x % kWaves];
-  m = w.m;
-#pragma unroll
-  for (int o = kWaves / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  w = moved<kT>(w, from(m), c);
-#pragma unroll
-  for (int o = kWaves / 2; o > 0; o >>= 1) {
-    w.s += __shfl_xor(w.s, o, 64);
-    if (kT) w.t += __shfl_xor(w.t, o, 64);
-  }
-  w.m = m;
-  return w;
+  const int lane = (int)threadIdx.x % 64;
+  a = Sums{kNone, 0.0f, 0.0f};
+  if (lane < kLanes / 64) a = lds[lane];
+  return wave_sums<kT>(a, c);
 }
 
 // What a group's lanes wrote to LDS is there for all of them.
@@ -88,29 +98,68 @@ __device__ inline void group_sync() {
 
 // --- a row's columns -------------------------------------------------------------
 
-// A chunk of T whose columns from `left` on are minus infinity.
+// Rows start at any multiple of their elements' size, but loads and stores of 16 bytes are at their
+// best at multiples of 16 (8,192 x 32,767 bf16, whose rows start at odd multiples of 2: gradient
+// 191 us, 235 with chunks that start where rows do).  So a row's chunks are those of memory: its
+// first one starts `skew` columns before the row (nothing is read there: the row's first 16 bytes
+// are, and shifted).  Rows too short to gain have skew 0.
 template <typename T>
-__device__ inline Chunk cut(Chunk x, int left) {
+__device__ inline int skew_of(const T *z, int d) {
+  constexpr int N = kCols<T>;
+  return d < 2 * N ? 0 : (int)((uintptr_t)z / sizeof(T) % N);
+}
+template <typename T>
+__device__ inline int chunks_in(int d, int skew) {
+  return (d + skew + kCols<T> - 1) / kCols<T>;
+}
+
+// A chunk of T, minus infinity but for its columns low .. left - 1.
+template <typename T>
+__device__ inline Chunk cut(Chunk x, int low, int left) {
   constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, bf16>::value ? 0xff80u : 0xfc00u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (sizeof(T) == 4) {
-      x[i] = i < left ? x[i] : none;
+      x[i] = i >= low && i < left ? x[i] : none;
     } else {
-      const uint32_t low = 2 * i < left ? x[i] & 0xffffu : none;
-      const uint32_t high = 2 * i + 1 < left ? x[i] & 0xffff0000u : none << 16;
-      x[i] = low | high;
+      const uint32_t first = 2 * i >= low && 2 * i < left ? x[i] & 0xffffu : none;
+      const uint32_t second = 2 * i + 1 >= low && 2 * i + 1 < left ? x[i] & 0xffff0000u : none << 16;
+      x[i] = first | second;
     }
   }
   return x;
 }
 
-// A chunk whose first column is `at` of a row of d columns, the columns from stop <= d on as
-// minus infinity.
+// A chunk moved up by 0 < by < kCols columns.
+template <typename T>
+__device__ inline Chunk raise(Chunk c, int by) {
+  const int bits = by * 8 * (int)sizeof(T);
+  if (bits & 64) c = Chunk{0u, 0u, c[0], c[1]};
+  if (bits & 32) c = Chunk{0u, c[0], c[1], c[2]};
+  if (sizeof(T) == 2 && (bits & 16))
+    c = Chunk{c[0] << 16, c[1] << 16 | c[0] >> 16, c[2] << 16 | c[1] >> 16, c[3] << 16 | c[2] >> 16};
+  return c;
+}
+
+// A chunk whose first column is `at` (below 0 in a skewed row's first) of a row of d columns: minus
+// infinity before the row's first column and from stop <= d on.
 template <typename T>
 __device__ inline Chunk edge_chunk(const T *row, int at, int stop, int d) {
-  const Place<T, true> l = place<T, true>(at, d);
-  return cut<T>(settle(fetch(row, l), l), stop - at);
+  const Place<T, true> l = place<T, true>(max(at, 0), d);
+  Chunk c = settle(fetch(row, l), l);
+  if (at < 0) c = raise<T>(c, -at);
+  return cut<T>(c, -at, stop - at);
+}
+
+// The columns low .. left - 1 of a chunk to p and on.
+template <typename T>
+__device__ inline void put_some(T *p, int low, int left, Chunk c) {
+#pragma unroll
+  for (int i = 0; i < kCols<T>; ++i) {
+    if (i < low || i >= left) continue;
+    if (sizeof(T) == 4) ((uint32_t *)p)[i] = c[i];
+    else ((uint16_t *)p)[i] = (uint16_t)(c[i / 2] >> (16 * (i % 2)));
+  }
 }
 
 // Chunks q .. end - 1 of a row of d columns, or as many of them as a batch takes, as they lie in
@@ -124,24 +173,32 @@ struct Batch {
   static constexpr int N = kCols<T>;
   Chunk in[kPer], edge;
   int q, rows, next, lane;        // first chunk, rows of whole chunks, first chunk after the batch
-  bool ragged;                    // whether there is an edge
+  int skew;
+  bool ragged;                    // whether the lane's wave has a part of an edge
 
-  __device__ inline int column(int k) const { return N * (q + k * kLanes + lane); }
+  __device__ inline int column(int k) const { return N * (q + k * kLanes + lane) - skew; }
 
-  __device__ inline void load(const T *row, int q_, int end, int d, int lane_) {
+  __device__ inline void load(const T *row, int skew_, int q_, int end, int d, int lane_) {
     q = q_;
     lane = lane_;
-    const int whole = min(end, d / N);
+    skew = skew_;
+    const int whole = min(end, (d + skew) / N);
     rows = min(kPer, (whole - q) / kLanes);
     next = q + rows * kLanes;
-    ragged = next < end && whole - next < kLanes;
+    const bool last = whole - next < kLanes;
+    ragged = last && next + __builtin_amdgcn_readfirstlane(lane) < end;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (k < rows) in[k] = *(const Unaligned *)((const char *)(row + N * (q + k * kLanes)) + (uint32_t)(16 * lane));
-    if (ragged) {
-      edge = edge_chunk(row, N * (next + lane), min(d, N * end), d);
-      next = end;
+    for (int k = 0; k < kPer; ++k) {
+      uint32_t at = (uint32_t)(16 * lane);
+      if (k == 0 && q == 0 && lane == 0) at = (uint32_t)skew * (uint32_t)sizeof(T);
+      if (k < rows) in[k] = *(const Unaligned *)((const char *)(row + (N * (q + k * kLanes) - skew)) + at);
     }
+    if (ragged) edge = edge_chunk(row, N * (next + lane) - skew, min(d, N * end - skew), d);
+    if (last) next = end;
+  }
+  // Puts a skewed row's first chunk right, before its first use.
+  __device__ inline void trim() {
+    if (q == 0 && skew > 0 && rows > 0 && lane == 0) in[0] = cut<T>(raise<T>(in[0], skew), skew, N);
   }
   // Keeps the compiler from holding the widened numbers, at twice the registers, from one pass over
   // the batch to the next.
@@ -170,6 +227,7 @@ template <bool kT, typename T, int kLanes, int kPer>
 __device__ inline void add_batch(Batch<T, kLanes, kPer> &b, float c, Sums &a, int &most) {
   constexpr int N = kCols<T>;
   float m = a.m;
+  b.trim();
   b.each([&](int k, Chunk in) {
     float v[N];
     widen<T>(in, v);
@@ -272,7 +330,7 @@ struct Rows {
   const T *Z;
   int64_t ldz;
   float scale, c;      // c = scale log2(e)
-  int chunks;          // of a row
+  int chunks;          // of a row that is not skewed
 };
 template <typename T>
 Rows<T> rows_of(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale) {
@@ -305,17 +363,6 @@ __device__ inline void score_row(const Score &a, int64_t row, int id, float z, c
   if (a.logp) a.logp[row] = id < 0 ? 0.0f : log_p(z, e, scale);
   if (a.lse) a.lse[row] = log_sum(e, scale);
   if (a.entropy) a.entropy[row] = entropy(e);
-}
-
-__device__ inline float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
-}
-__device__ inline float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-  return x;
 }
 
 // A teacher's row, by the first wave of a group while the others go on with theirs: a lane's entries

@@ -46,12 +46,12 @@ struct Marks {
   }
   // Marks the first k entries whose column is in chunks first .. first + kChunks - 1, chunks of n
   // columns.
-  __device__ inline void mark(int k, int first, int n, int lane) {
+  __device__ inline void mark(int k, int first, int n, int skew, int lane) {
     for (int i = lane; i < kHeads / 8; i += 64) ((uint4 *)head)[i] = make_uint4(0, 0, 0, 0);
     group_sync<64>();
     bool crowded = false;
     for (int e = lane; e < k; e += 64) {
-      const uint32_t c = (uint32_t)(column[e] / n - first);
+      const uint32_t c = (uint32_t)((column[e] + skew) / n - first);
       weight[e] = q[e];
       if (column[e] < 0 || c >= (uint32_t)kChunks) continue;
       // (two heads to a word)
@@ -71,7 +71,7 @@ struct Marks {
     // them and the others count 0, so that the order of the rest does not matter: two along their
     // list, as a sum of two has one value; of more, in the order of the entries.
     for (int e = lane; e < k; e += 64) {
-      const uint32_t c = (uint32_t)(column[e] / n - first);
+      const uint32_t c = (uint32_t)((column[e] + skew) / n - first);
       if (column[e] < 0 || c >= (uint32_t)kChunks) continue;
       int same = 0;
       float s = q[e];
@@ -125,9 +125,10 @@ __device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base,
         for (int i = 0; i < N; ++i) v[i] = at + i == column ? fmaf(hit, q, v[i]) : v[i];
       }
     }
-    T *to = (T *)((char *)(dz + N * (b.q + j * kLanes)) + (uint32_t)(16 * b.lane));
-    if (j < b.rows) put(to, N, narrow<T>(v), stream);
-    else if (at < d) put(to, d - at, narrow<T>(v), stream);
+    T *to = (T *)((char *)(dz + (N * (b.q + j * kLanes) - b.skew)) + (uint32_t)(16 * b.lane));
+    const Chunk out = narrow<T>(v);
+    if ((j < b.rows || at + N <= d) && (j > 0 || at >= 0)) put(to, N, out, stream);
+    else put_some(to, -at, d - at, out);
   });
 }
 
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     if (g.dentropy) ge = scalar(g.dentropy, row);
   }
   Batch<T, kLanes, kPer> b;
-  b.load(z, 0, a.chunks, a.d, lane);
+  const int skew = skew_of(z, a.d), chunks = chunks_in<T>(a.d, skew);
+  b.load(z, skew, 0, chunks, a.d, lane);
   float zt = 0.0f;
   if (kTeach && first) x.gather(t, z);
   if (!kTeach && id >= 0) zt = (float)z[id];
@@ -169,14 +171,14 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     if (first) {
       x.learn(t, row);
       marks.keep(x, lane);
-      marks.mark(t.k, 0, N, lane);
+      marks.mark(t.k, 0, N, skew, lane);
     }
   }
   Sums s{kNone, 0.0f, 0.0f};
   int most = 0;
   add_batch<kEntropy>(b, a.c, s, most);
-  while (b.next < a.chunks) {
-    b.load(z, b.next, a.chunks, a.d, lane);
+  while (b.next < chunks) {
+    b.load(z, skew, b.next, chunks, a.d, lane);
     add_batch<kEntropy>(b, a.c, s, most);
   }
   if (kTeach && first) x.compare();
@@ -206,13 +208,14 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   }
   const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
   const bool held = b.q == 0;
-  for (int q = 0; q < a.chunks; q = b.next) {
+  for (int q = 0; q < chunks; q = b.next) {
     if (!held) {
-      b.load(z, q, a.chunks, a.d, lane);
+      b.load(z, skew, q, chunks, a.d, lane);
+      b.trim();
       if constexpr (kTeach) {
         if (q > 0) {
           group_sync<kLanes>();
-          if (first) marks.mark(t.k, q, N, lane);
+          if (first) marks.mark(t.k, q, N, skew, lane);
           group_sync<kLanes>();
         }
       }
@@ -226,10 +229,14 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
 #define TOC_GRAD(L, K)                                                                           \
   hipLaunchKernelGGL((grad_kernel<T, L, K, kTeach, kEntropy>),                                   \
                      grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
-  if (a.chunks <= 256) TOC_GRAD(64, 4);
-  else if (a.chunks <= 2048) TOC_GRAD(256, 8);
-  else if (a.chunks < 1024 * 7) TOC_GRAD(1024, 6);
-  else TOC_GRAD(1024, 12);
+  const auto fits = [&](int lanes, int per) { return a.chunks + 1 < lanes * (per + 1); };
+  if (fits(64, 2)) TOC_GRAD(64, 2);
+  else if (fits(64, 8)) TOC_GRAD(64, 8);
+  else if (fits(256, 8)) TOC_GRAD(256, 8);
+  else if (fits(512, 6)) TOC_GRAD(512, 6);
+  else if (fits(1024, 12) && !fits(1024, 6)) TOC_GRAD(1024, 12);
+  else if (fits(1024, 16) && !fits(1024, 6)) TOC_GRAD(1024, 16);
+  else TOC_GRAD(1024, 6);
 #undef TOC_GRAD
   return launched("grad_kernel");
 }
