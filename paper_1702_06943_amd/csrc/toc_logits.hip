@@ -13,9 +13,10 @@ constexpr int kEntropy = 1, kTop = 2, kTeach = 4;   // what a kernel is asked fo
 // Logits in the order that the alternatives have them: the larger first, of equal ones the
 // lower column.  A key is never 0 for a column above minus infinity; a NaN has none.
 __device__ inline uint64_t key_of(float z, int column) {
-  if (!(z > kNone)) return 0;
   const uint32_t b = __float_as_uint(z + 0.0f);   // (-0 as 0)
-  return (uint64_t)(b ^ (b >> 31 ? 0xffffffffu : 0x80000000u)) << 32 | (uint32_t)~column;
+  const uint32_t high = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  const bool real = z > kNone;
+  return (uint64_t)(real ? high : 0u) << 32 | (real ? (uint32_t)~column : 0u);
 }
 __device__ inline float key_logit(uint64_t key) {
   const uint32_t b = (uint32_t)(key >> 32);
@@ -30,15 +31,16 @@ __device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const E
   a.top_logp[at] = key ? log_p(key_logit(key), e, scale) : kNone;
 }
 
-// Keys of columns that may be among a row's alternatives; at first the lanes' own.
+// Keys of columns that may be among a row's alternatives.
 template <int kLanes>
 constexpr int kCand = kLanes > 64 ? 1024 : 512;
 
 template <int kLanes, bool kOn>
 struct TopLds {
-  uint64_t keys[kOn ? kCand<kLanes> : 1];
+  uint64_t keys[kOn ? kCand<kLanes> : 1];   // at first the lanes' own
   uint64_t best[kLanes / 64];
-  uint16_t who[kOn ? kLanes : 1];      // lanes that may hold some
+  uint16_t who[kOn ? kLanes : 1];           // lanes that may hold some
+  uint64_t bound;
   uint32_t lanes, count;
 };
 
@@ -74,8 +76,8 @@ __device__ inline void top_searches(const Part<T> &p, int k, int lane, uint64_t 
         }
       }
     }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) best = larger(best, __shfl_xor((unsigned long long)best, x, 64));
+    const uint32_t high = wave_max((uint32_t)(best >> 32));
+    best = (uint64_t)high << 32 | wave_max((uint32_t)(best >> 32) == high ? (uint32_t)best : 0u);
     if (kLanes > 64) {
       __syncthreads();
       if (threadIdx.x % 64 == 0) best_lds[threadIdx.x / 64] = best;
@@ -88,69 +90,152 @@ __device__ inline void top_searches(const Part<T> &p, int k, int lane, uint64_t 
   }
 }
 
-// A lower bound, and no key lies between it and the k-th largest of a wave's 64 keys: by bits from
-// the highest on, of the logits first.  1 if fewer than k keys are not 0.
-__device__ inline uint64_t kth_largest(uint64_t key, int k) {
-  if (__popcll(__ballot(key != 0)) < k) return 1;
-  const uint32_t high = (uint32_t)(key >> 32), low = (uint32_t)key;
-  uint32_t t = 0;
-  int count = 64;
-  for (uint32_t bit = 1u << 31; bit && count != k; bit >>= 1) {
-    const int n = __popcll(__ballot(high >= (t | bit)));
+// The k-th largest of a wave's different keys, R in a lane; 1 if fewer than k are not 0.  By bits,
+// from the first one that the largest and the smallest logit do not share, until k keys are left.
+template <int R>
+__device__ inline uint64_t kth_largest(const uint64_t (&key)[R], int k) {
+  uint32_t most = 0, least = ~0u;
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint32_t high = (uint32_t)(key[i] >> 32);
+    most = max(most, high);
+    least = min(least, high ? high : ~0u);
+    count += (int)__popcll(__ballot(high != 0));
+  }
+  if (count < k) return 1;
+  most = wave_max(most);
+  const uint32_t differ = most ^ wave_min(least);
+  int bit = differ ? 63 - __clz((int)differ) : 31;
+  uint64_t t = bit == 63 ? 0 : (uint64_t)most << 32 >> (bit + 1) << (bit + 1);
+  for (; bit >= 0 && count != k; --bit) {
+    const uint64_t trial = t | (uint64_t)1 << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) n += (int)__popcll(__ballot(key[i] >= trial));
     if (n < k) continue;
-    t |= bit;
+    t = trial;
     count = n;
   }
-  uint32_t u = 0;
-  if (count != k) {
-    // more than k at or above t, fewer than k above it: the lowest columns among those at t
-    const int more = k - (int)__popcll(__ballot(high > t));
-    for (uint32_t bit = 1u << 31; bit; bit >>= 1)
-      if ((int)__popcll(__ballot(high == t && low >= (u | bit))) >= more) u |= bit;
-  }
-  const uint64_t bound = (uint64_t)t << 32 | u;
-  uint64_t least = key >= bound ? key : ~(uint64_t)0;
+  // the smallest of the k: its logit, and the highest column with it
+  uint32_t high = ~0u, low = ~0u;
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) {
-    const uint64_t other = __shfl_xor((unsigned long long)least, x, 64);
-    least = other < least ? other : least;
+  for (int i = 0; i < R; ++i)
+    if (key[i] >= t) high = min(high, key[i] ? (uint32_t)(key[i] >> 32) : ~0u);
+  high = wave_min(high);
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (key[i] >= t && (uint32_t)(key[i] >> 32) == high) low = min(low, (uint32_t)key[i]);
+  return (uint64_t)high << 32 | wave_min(low);
+}
+
+// The same for one key in a lane.  Few: one logit after the other; more: each lane counts the logits
+// above its own, 64 comparisons that wait for nothing.
+__device__ inline uint64_t kth_of_wave(uint64_t key, int k) {
+  if ((int)__popcll(__ballot(key != 0)) < k) return 1;
+  const uint32_t high = (uint32_t)(key >> 32);
+  uint32_t t;
+  if (k <= 10) {
+    for (uint32_t left = high;;) {
+      t = wave_max(left);
+      const int n = (int)__popcll(__ballot(left == t));
+      if (n >= k) break;
+      k -= n;
+      left = left == t ? 0u : left;
+    }
+  } else {
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) above += (uint32_t)__builtin_amdgcn_readlane((int)high, i) > high;
+    t = wave_min(above < k ? high : ~0u);
+    k -= (int)__popcll(__ballot(high > t));
   }
-  return least;
+  const bool at = high == t;
+  if ((int)__popcll(__ballot(at)) > k) return kth_largest<1>({at ? key : 0}, k);
+  return (uint64_t)t << 32 | wave_min(at ? (uint32_t)key : ~0u);
+}
+
+// Of the first n keys in LDS, more than k, moves the k largest to the front, in no order: by one
+// wave.
+template <int R>
+__device__ inline void keep_largest(uint64_t *keys, int n, int k, int lane) {
+  uint64_t key[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) key[i] = 64 * i + lane < n ? keys[64 * i + lane] : 0;
+  const uint64_t t = kth_largest(key, k);
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint64_t all = __ballot(key[i] >= t);
+    if (key[i] >= t) keys[at + __popcll(all & (((uint64_t)1 << lane) - 1))] = key[i];
+    at += (int)__popcll(all);
+  }
+  group_sync<64>();
 }
 
 // The k largest keys of a part, put(r, key) for the r-th of them (0: there
-// is none).  The sums' pass over the row leaves each lane's largest logit and its chunk.  Of lanes i,
-// i + 64, ... the largest such keys are 64 keys of different columns, so the k-th largest of them is
-// a lower bound of the k-th largest of all, and lanes whose own largest logit is below it have none
+// is none).  The sums' pass over the row leaves each lane's largest logit and its chunk.  Such
+// keys are of different columns, so the k-th largest of the largest of some groups of lanes is a
+// lower bound of the k-th largest of all, and lanes whose own largest logit is below it have none
 // of those: the chunks of the other lanes, some k, are dealt out to the group and read again, and
-// the keys from the bound on, little more than k, are left in LDS, where each counts those above
-// it.  (A lane's chunk stands for its last column: the key is then at most the column's own.)
+// the keys from the bound on, little more than k, are left in LDS for the first wave.  (A lane's chunk stands for its last column: the key is then at most the column's own.)
 // Where more than kCand are left, which takes most of the largest logits in the columns of a few
 // lanes, k searches follow.
 template <typename T, int kLanes, typename Put>
 __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int most, TopLds<kLanes, true> &lds, Put put) {
   constexpr int N = kCols<T>;
-  lds.keys[lane] = key_of(m, min(most + N, p.d) - 1);
-  if (lane == 0) lds.lanes = lds.count = 0;
-  group_sync<kLanes>();
-  uint64_t key = lds.keys[lane % 64];
+  const uint64_t own = key_of(m, min(most + N, p.d) - 1);
+  if (kLanes > 64) {
+    lds.keys[lane] = own;
+    group_sync<kLanes>();
+  }
+  if (lane < 64) {
+    // groups of lanes with one key each: the more there are, the nearer the bound
+    constexpr int kWaves = kLanes / 64, R = kWaves < 4 ? kWaves : 4;
+    uint64_t key[kWaves], most_of[R];
 #pragma unroll
-  for (int w = 1; w < kLanes / 64; ++w) key = larger(key, lds.keys[w * 64 + lane % 64]);
-  const uint64_t bound = kth_largest(key, k);
-  if (key_of(m, 0) >= bound) lds.who[atomicAdd(&lds.lanes, 1u)] = (uint16_t)lane;
+    for (int w = 0; w < kWaves; ++w) {
+      key[w] = kLanes > 64 ? lds.keys[w * 64 + lane] : own;
+      most_of[w % R] = w < R ? key[w] : larger(most_of[w % R], key[w]);
+    }
+    uint64_t one = most_of[0];
+#pragma unroll
+    for (int i = 1; i < R; ++i) one = larger(one, most_of[i]);
+    const uint64_t bound = k <= 32 ? kth_of_wave(one, k) : kth_largest(most_of, k);
+    uint32_t lanes = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      // (a lane's largest logit may be in a lower column than its key says)
+      const bool may = (key[w] | 0xffffffffu) >= bound && key[w] != 0;
+      const uint64_t all = __ballot(may);
+      if (may) lds.who[lanes + __popcll(all & (((uint64_t)1 << lane) - 1))] = (uint16_t)(w * 64 + lane);
+      lanes += (uint32_t)__popcll(all);
+    }
+    if (lane == 0) {
+      lds.bound = bound;
+      lds.lanes = lanes;
+      lds.count = 0;
+    }
+  }
   group_sync<kLanes>();
+  const uint64_t bound = lds.bound;
   const uint32_t lanes = lds.lanes, deals = (uint32_t)(p.end - p.q0 + kLanes - 1) / kLanes;
   for (uint32_t i = lane; i < lanes * deals; i += kLanes) {
     const int q = p.q0 + (int)lds.who[i % lanes] + (int)(i / lanes) * kLanes;
     if (q >= p.end) continue;
     float v[N];
     p.numbers(q, v);
+    const int at = p.column(q);
+    uint32_t found = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) found |= key_of(v[j], at + j) >= bound ? 1u << j : 0u;
+    if (!found) continue;
+    uint32_t slot = atomicAdd(&lds.count, (uint32_t)__popc(found));
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const uint64_t key = key_of(v[j], p.column(q) + j);
-      if (key < bound) continue;
-      const uint32_t at = atomicAdd(&lds.count, 1u);
-      if (at < (uint32_t)kCand<kLanes>) lds.keys[at] = key;
+      if (!(found >> j & 1u)) continue;
+      if (slot < (uint32_t)kCand<kLanes>) lds.keys[slot] = key_of(v[j], at + j);
+      ++slot;
     }
   }
   group_sync<kLanes>();
@@ -159,16 +244,19 @@ __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int mo
     top_searches<T, kLanes>(p, k, lane, lds.best, put);
     return;
   }
-  for (int i = lane; i < max(count, k); i += kLanes) {
-    if (i >= count) {
-      put(i, (uint64_t)0);
-      continue;
-    }
-    const uint64_t mine = lds.keys[i];
-    int above = 0;
-    for (int j = 0; j < count; ++j) above += lds.keys[j] > mine;
-    if (above < k) put(above, mine);
+  if (lane >= 64) return;
+  // the first wave: no more than 64 of them, in the order of how many are above each
+  if (count > 256) keep_largest<kCand<kLanes> / 64>(lds.keys, count, k, lane);
+  else if (count > 64) keep_largest<4>(lds.keys, count, k, lane);
+  const int left = count > 64 ? k : count;
+  const uint64_t mine = lane < left ? lds.keys[lane] : 0;
+  int above = 0;
+  for (int i = 0; i < left; ++i) {
+    const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), i) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+    above += other > mine;
   }
+  if (lane < left ? above < k : lane < k) put(lane < left ? above : lane, mine);
 }
 
 // kLanes lanes to a row, kPer chunks of a lane asked for at once.

@@ -44,10 +44,9 @@ __device__ inline Sums moved(Sums a, float base, float c) {
 // their last ones, each one operation on the way into the adder (lanes without a source take the
 // operation's neutral number); the last lane has the result.
 template <typename Op>
-__device__ inline float wave_all(float x, float neutral, Op op) {
-#define TOC_STEP(ctrl, rows)                                                                             \
-  x = op(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(neutral),          \
-                                                                  (int)__float_as_uint(x), ctrl, rows, 0xf, false)))
+__device__ inline uint32_t wave_all(uint32_t x, uint32_t neutral, Op op) {
+#define TOC_STEP(ctrl, rows) \
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)x, ctrl, rows, 0xf, false))
   TOC_STEP(0x111, 0xf);   // from 1, 2, 4, 8 lanes below
   TOC_STEP(0x112, 0xf);
   TOC_STEP(0x114, 0xf);
@@ -55,13 +54,23 @@ __device__ inline float wave_all(float x, float neutral, Op op) {
   TOC_STEP(0x142, 0xa);   // lane 15 of a row to the next, rows 1 and 3
   TOC_STEP(0x143, 0xc);   // lane 31 to rows 2 and 3
 #undef TOC_STEP
-  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ inline uint32_t wave_min(uint32_t x) {
+  return wave_all(x, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); });
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+  return wave_all(x, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 __device__ inline float wave_sum(float x) {
-  return wave_all(x, 0.0f, [](float a, float b) { return a + b; });
+  return __uint_as_float(wave_all(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 __device__ inline float wave_max(float x) {
-  return wave_all(x, kNone, [](float a, float b) { return fmaxf(a, b); });
+  return __uint_as_float(wave_all(__float_as_uint(x), __float_as_uint(kNone), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
 }
 
 template <bool kT>

@@ -171,7 +171,8 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     if (first) {
       x.learn(t, row);
       marks.keep(x, lane);
-      marks.mark(t.k, 0, N, skew, lane);
+      const int rows = (a.d + skew) / N / kLanes;          // the last batch's first chunk
+      marks.mark(t.k, rows ? (rows - 1) / kPer * kPer * kLanes : 0, N, skew, lane);
     }
   }
   Sums s{kNone, 0.0f, 0.0f};
@@ -207,20 +208,18 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     return;
   }
   const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
-  const bool held = b.q == 0;
-  for (int q = 0; q < chunks; q = b.next) {
-    if (!held) {
-      b.load(z, skew, q, chunks, a.d, lane);
-      b.trim();
-      if constexpr (kTeach) {
-        if (q > 0) {
-          group_sync<kLanes>();
-          if (first) marks.mark(t.k, q, N, skew, lane);
-          group_sync<kLanes>();
-        }
-      }
-    }
+  // the last batch is still there; the others from the last on, the likelier to be in a cache
+  for (;;) {
     put_batch<kEntropy>(b, a.c, base, k, id, hit, marks, dz, a.d, g.stream);
+    const int q = b.q - kLanes * kPer;
+    if (q < 0) break;
+    b.load(z, skew, q, chunks, a.d, lane);
+    b.trim();
+    if constexpr (kTeach) {
+      group_sync<kLanes>();
+      if (first) marks.mark(t.k, q, N, skew, lane);
+      group_sync<kLanes>();
+    }
   }
 }
 
