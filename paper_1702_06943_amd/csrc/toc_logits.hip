@@ -31,13 +31,13 @@ __device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const E
   a.top_logp[at] = key ? log_p(key_logit(key), e, scale) : kNone;
 }
 
-// Keys of columns that may be among a row's alternatives.
-template <int kLanes>
-constexpr int kCand = kLanes > 64 ? 1024 : 512;
+// Keys of columns that may be among a row's alternatives, at most.  (As many of equal logits are left:
+// 64 chunks' columns.)
+constexpr int kCand = 512;
 
 template <int kLanes, bool kOn>
 struct TopLds {
-  uint64_t keys[kOn ? kCand<kLanes> : 1];   // at first the lanes' own
+  uint64_t keys[!kOn ? 1 : kLanes > kCand ? kLanes : kCand];   // at first the lanes' own
   uint64_t best[kLanes / 64];
   uint16_t who[kOn ? kLanes : 1];           // lanes that may hold some
   uint64_t bound;
@@ -90,26 +90,30 @@ __device__ inline void top_searches(const Part<T> &p, int k, int lane, uint64_t 
   }
 }
 
-// The k-th largest of a wave's different keys, R in a lane; 1 if fewer than k are not 0.  By bits,
-// from the first one that the largest and the smallest logit do not share, until k keys are left.
+// The k-th largest of a wave's different keys, R in a lane; 1 if fewer than k are not 0.  By the bits
+// in which any two differ, until k keys are left.
 template <int R>
 __device__ inline uint64_t kth_largest(const uint64_t (&key)[R], int k) {
-  uint32_t most = 0, least = ~0u;
+  uint32_t most = 0;
   int count = 0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const uint32_t high = (uint32_t)(key[i] >> 32);
-    most = max(most, high);
-    least = min(least, high ? high : ~0u);
-    count += (int)__popcll(__ballot(high != 0));
+    most = max(most, (uint32_t)(key[i] >> 32));
+    count += (int)__popcll(__ballot(key[i] != 0));
   }
   if (count < k) return 1;
   most = wave_max(most);
-  const uint32_t differ = most ^ wave_min(least);
-  int bit = differ ? 63 - __clz((int)differ) : 31;
-  uint64_t t = bit == 63 ? 0 : (uint64_t)most << 32 >> (bit + 1) << (bit + 1);
-  for (; bit >= 0 && count != k; --bit) {
-    const uint64_t trial = t | (uint64_t)1 << bit;
+  uint32_t high = 0, low = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    high |= key[i] ? (uint32_t)(key[i] >> 32) ^ most : 0u;
+    low |= key[i] ? ~(uint32_t)key[i] : 0u;         // (columns: their own upper bits are 0)
+  }
+  uint64_t differ = (uint64_t)wave_or(high) << 32 | wave_or(low);
+  uint64_t t = ((uint64_t)most << 32 | 0xffffffffu) & ~differ;
+  while (differ && count != k) {
+    const uint64_t bit = (uint64_t)1 << (63 - __clzll((long long)differ)), trial = t | bit;
+    differ ^= bit;
     int n = 0;
 #pragma unroll
     for (int i = 0; i < R; ++i) n += (int)__popcll(__ballot(key[i] >= trial));
@@ -118,7 +122,7 @@ __device__ inline uint64_t kth_largest(const uint64_t (&key)[R], int k) {
     count = n;
   }
   // the smallest of the k: its logit, and the highest column with it
-  uint32_t high = ~0u, low = ~0u;
+  high = low = ~0u;
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (key[i] >= t) high = min(high, key[i] ? (uint32_t)(key[i] >> 32) : ~0u);
@@ -151,14 +155,20 @@ __device__ inline uint64_t kth_of_wave(uint64_t key, int k) {
     k -= (int)__popcll(__ballot(high > t));
   }
   const bool at = high == t;
-  if ((int)__popcll(__ballot(at)) > k) return kth_largest<1>({at ? key : 0}, k);
-  return (uint64_t)t << 32 | wave_min(at ? (uint32_t)key : ~0u);
+  if ((int)__popcll(__ballot(at)) == k) return (uint64_t)t << 32 | wave_min(at ? (uint32_t)key : ~0u);
+  // of those with the logit t, the k lowest columns
+  uint32_t left = at ? (uint32_t)key : 0u, u = 0;
+  for (; k > 0; --k) {
+    u = wave_max(left);
+    left = left == u ? 0u : left;
+  }
+  return (uint64_t)t << 32 | u;
 }
 
-// Of the first n keys in LDS, more than k, moves the k largest to the front, in no order: by one
-// wave.
+// Of the first n > k keys in LDS moves the k largest, or those that are not 0, to the front, in no
+// order, and returns how many they are: by one wave.
 template <int R>
-__device__ inline void keep_largest(uint64_t *keys, int n, int k, int lane) {
+__device__ inline int keep_largest(uint64_t *keys, int n, int k, int lane) {
   uint64_t key[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) key[i] = 64 * i + lane < n ? keys[64 * i + lane] : 0;
@@ -171,6 +181,28 @@ __device__ inline void keep_largest(uint64_t *keys, int n, int k, int lane) {
     at += (int)__popcll(all);
   }
   group_sync<64>();
+  return at;
+}
+
+// put(r, key) for the r-th of the k largest of n <= kMost keys in LDS (0: there is none), by one wave:
+// no more than 64 of them, in the order of how many are above each.
+template <int kMost, typename Put>
+__device__ inline void put_largest(uint64_t *keys, int n, int k, int lane, Put put) {
+  const int left = n > 256 ? keep_largest<kMost / 64>(keys, n, k, lane) : n > 64 ? keep_largest<4>(keys, n, k, lane) : n;
+  const uint64_t mine = lane < left ? keys[lane] : 0;
+  int above = 0;
+  for (int i = 0; i < left; i += 8) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {          // (lanes past the last one have 0)
+      const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), i + x) << 32 |
+                             (uint32_t)__builtin_amdgcn_readlane((int)mine, i + x);
+      above += other > mine;
+    }
+  }
+  // (lanes without one have the places after the last)
+  const uint64_t without = __ballot(mine == 0);
+  if (mine == 0) above = 64 - (int)__popcll(without) + (int)__popcll(without & (((uint64_t)1 << lane) - 1));
+  if (above < k) put(above, mine);
 }
 
 // The k largest keys of a part, put(r, key) for the r-th of them (0: there
@@ -234,34 +266,22 @@ __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int mo
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if (!(found >> j & 1u)) continue;
-      if (slot < (uint32_t)kCand<kLanes>) lds.keys[slot] = key_of(v[j], at + j);
+      if (slot < (uint32_t)kCand) lds.keys[slot] = key_of(v[j], at + j);
       ++slot;
     }
   }
   group_sync<kLanes>();
   const int count = (int)lds.count;
-  if (count > kCand<kLanes>) {
+  if (count > kCand) {
     top_searches<T, kLanes>(p, k, lane, lds.best, put);
     return;
   }
-  if (lane >= 64) return;
-  // the first wave: no more than 64 of them, in the order of how many are above each
-  if (count > 256) keep_largest<kCand<kLanes> / 64>(lds.keys, count, k, lane);
-  else if (count > 64) keep_largest<4>(lds.keys, count, k, lane);
-  const int left = count > 64 ? k : count;
-  const uint64_t mine = lane < left ? lds.keys[lane] : 0;
-  int above = 0;
-  for (int i = 0; i < left; ++i) {
-    const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), i) << 32 |
-                           (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
-    above += other > mine;
-  }
-  if (lane < left ? above < k : lane < k) put(lane < left ? above : lane, mine);
+  if (lane < 64) put_largest<kCand>(lds.keys, count, k, lane, put);
 }
 
 // kLanes lanes to a row, kPer chunks of a lane asked for at once.
 template <typename T, int kLanes, int kPer, int kWhat>
-__global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Score o, Teacher t) {
+__global__ __launch_bounds__(kThreads<kLanes>, 8) void score_kernel(Rows<T> a, Score o, Teacher t) {
   constexpr int kGroups = kThreads<kLanes> / kLanes;
   constexpr bool kT = kWhat & kEntropy;
   __shared__ Sums sums_lds[kGroups][kLanes / 64];
@@ -307,6 +327,67 @@ __global__ __launch_bounds__(kThreads<kLanes>) void score_kernel(Rows<T> a, Scor
     });
 }
 
+// The sums, and the k largest keys, of a part of a row.
+template <typename T, bool kT, bool kOfTop>
+__global__ __launch_bounds__(kPartLanes) void part_kernel(Rows<T> a, int k, Split s) {
+  constexpr int kLanes = kPartLanes;
+  __shared__ Sums sums_lds[kLanes / 64];
+  __shared__ TopLds<kLanes, kOfTop> top_lds;
+  const int lane = (int)threadIdx.x;
+  const int64_t row = (int64_t)(blockIdx.x / (uint32_t)s.parts);
+  const T *z = a.Z + row * a.ldz;
+  const int skew = skew_of(z, a.d);
+  const Piece piece = piece_of(s, chunks_in<T>(a.d, skew));
+  Sums x{kNone, 0.0f, 0.0f};
+  int most = 0;
+  Batch<T, kLanes, kPartPer> b;
+  for (int q = piece.q0; q < piece.end; q = b.next) {
+    b.load(z, skew, q, piece.end, a.d, lane);
+    add_batch<kT>(b, a.c, x, most);
+  }
+  const float m = x.m;
+  x = group_sums<kLanes, kT>(x, a.c, sums_lds);
+  if (lane == 0) s.sums[blockIdx.x] = x;
+  if constexpr (kOfTop) {
+    const Part<T> p{z, a.d, skew, piece.q0, piece.end};
+    top_of<T, kLanes>(p, k, lane, m, most, top_lds,
+                      [&](int r, uint64_t key) { s.keys[(int64_t)blockIdx.x * k + r] = key; });
+  }
+}
+
+// What is asked for of a row from its parts, by one wave.
+template <typename T, int kWhat>
+__global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t, Split s) {
+  constexpr int kKeys = 256;
+  __shared__ uint64_t keys[kWhat & kTop ? kKeys : 1];
+  const int lane = (int)threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const T *z = a.Z + row * a.ldz;
+  Taught x;
+  if (kWhat & kTeach) x.ask(t, row, a.d, lane);
+  const int id = kWhat & kTeach ? -1 : scalar_token(o.ids, row, a.d);
+  float zt = 0.0f;
+  if (id >= 0) zt = (float)z[id];
+  if (kWhat & kTeach) {
+    x.gather(t, z);
+    x.learn(t, row);
+    x.compare();
+  }
+  if (kWhat & kTop)
+    for (int i = lane; i < s.parts * o.k; i += 64) keys[i] = s.keys[row * s.parts * o.k + i];
+  const End e = end_of(parts_sums<(kWhat & kEntropy) != 0>(s, row, a.c));
+  if (lane == 0) {
+    if (kWhat & kTeach) t.loss[row] = x.loss(e, a.scale);
+    else score_row(o, row, id, zt, e, a.scale);
+  }
+  if constexpr ((kWhat & kTop) != 0) {
+    group_sync<64>();
+    put_largest<kKeys>(keys, s.parts * o.k, o.k, lane, [&](int r, uint64_t key) {
+      put_top(o, row * o.k + r, key, e, a.scale);
+    });
+  }
+}
+
 template <typename T, int kWhat>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_t s) {
 #define TOC_SCORE(L, K)                                                                          \
@@ -321,13 +402,55 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_
 }
 
 template <typename T>
-toc_status score(const Rows<T> &a, const Score &o, hipStream_t s) {
+toc_status distill(const Rows<T> &a, const Teacher &t, void *ws, hipStream_t s) {
+  const Score o{};
+  const Split split = split_of(a.n, a.chunks, 0, ws);
+  if (split.parts == 1) return launch<T, kTeach>(a, o, t, s);
+  const toc_status st = add_parts<T>(a, 0, false, split, s);
+  return st ? st : join_parts<T>(a, o, t, split, s);
+}
+
+template <typename T>
+toc_status score(const Rows<T> &a, const Score &o, void *ws, hipStream_t s) {
   const Teacher t{};
+  const Split split = split_of(a.n, a.chunks, o.k, ws);
+  if (split.parts > 1) {
+    const toc_status st = add_parts<T>(a, o.k, o.entropy != nullptr, split, s);
+    return st ? st : join_parts<T>(a, o, t, split, s);
+  }
   if (o.k) return o.entropy ? launch<T, kTop | kEntropy>(a, o, t, s) : launch<T, kTop>(a, o, t, s);
   return o.entropy ? launch<T, kEntropy>(a, o, t, s) : launch<T, 0>(a, o, t, s);
 }
 
 }  // namespace
+
+template <typename T>
+toc_status add_parts(const Rows<T> &a, int k, bool entropy, const Split &s, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.n * (uint32_t)s.parts)), block(kPartLanes);
+  if (k > 0 && entropy) hipLaunchKernelGGL((part_kernel<T, true, true>), grid, block, 0, stream, a, k, s);
+  else if (k > 0) hipLaunchKernelGGL((part_kernel<T, false, true>), grid, block, 0, stream, a, k, s);
+  else if (entropy) hipLaunchKernelGGL((part_kernel<T, true, false>), grid, block, 0, stream, a, k, s);
+  else hipLaunchKernelGGL((part_kernel<T, false, false>), grid, block, 0, stream, a, k, s);
+  return launched("part_kernel");
+}
+
+template <typename T>
+toc_status join_parts(const Rows<T> &a, const Score &o, const Teacher &t, const Split &s, hipStream_t stream) {
+  const dim3 grid(a.n), block(64);
+  if (t.k > 0) hipLaunchKernelGGL((join_kernel<T, kTeach>), grid, block, 0, stream, a, o, t, s);
+  else if (o.k > 0) hipLaunchKernelGGL((join_kernel<T, kEntropy | kTop>), grid, block, 0, stream, a, o, t, s);
+  else hipLaunchKernelGGL((join_kernel<T, kEntropy>), grid, block, 0, stream, a, o, t, s);
+  return launched("join_kernel");
+}
+
+#define TOC_PARTS(T)                                                                         \
+  template toc_status add_parts<T>(const Rows<T> &, int, bool, const Split &, hipStream_t);   \
+  template toc_status join_parts<T>(const Rows<T> &, const Score &, const Teacher &, const Split &, hipStream_t);
+TOC_PARTS(float)
+TOC_PARTS(bf16)
+TOC_PARTS(f16)
+#undef TOC_PARTS
+
 }  // namespace logits
 }  // namespace toc
 
@@ -342,7 +465,9 @@ toc_status toc_logits_workspace_size(int64_t n, int32_t d, int32_t k, size_t *by
   if (const toc_status st = check_sizes(n, d, TOC_F32)) return st;
   if (k < 0) return fail(TOC_EINVAL, "%d alternatives", k);
   if (k > kMaxTop) return fail(TOC_EUNSUPPORTED, "more than %d alternatives a row", kMaxTop);
-  *bytes = 0;
+  // the most that a call of 1 .. n rows, of the type with the most chunks, takes
+  const int64_t most = parts_of(1, chunks_of<float>(d), 0), pieces = std::min(n * most, (int64_t)kMaxPieces);
+  *bytes = most > 1 ? (size_t)pieces * (sizeof(Sums) + sizeof(uint64_t) * (size_t)k) : 0;
   return TOC_OK;
 }
 
@@ -363,9 +488,9 @@ toc_status toc_logprob(int64_t n, int32_t d, int32_t type, const void *Z, int64_
   if (n == 0) return TOC_OK;
   const Score o{Ids{ids, id_bits}, logp, lse, entropy, k, top_ids, top_logp};
   switch (type) {
-    case TOC_F32: return score(rows_of<float>(n, d, Z, ldz, scale), o, (hipStream_t)stream);
-    case TOC_BF16: return score(rows_of<bf16>(n, d, Z, ldz, scale), o, (hipStream_t)stream);
-    default: return score(rows_of<f16>(n, d, Z, ldz, scale), o, (hipStream_t)stream);
+    case TOC_F32: return score(rows_of<float>(n, d, Z, ldz, scale), o, ws, (hipStream_t)stream);
+    case TOC_BF16: return score(rows_of<bf16>(n, d, Z, ldz, scale), o, ws, (hipStream_t)stream);
+    default: return score(rows_of<f16>(n, d, Z, ldz, scale), o, ws, (hipStream_t)stream);
   }
 }
 
@@ -381,12 +506,11 @@ toc_status toc_distill(int64_t n, int32_t d, int32_t type, const void *Z, int64_
     return st;
   if (n == 0) return TOC_OK;
   const Teacher t{Ids{top_ids, id_bits}, ldi, k, t_type, top_z, ldt, top_scale, top_lse, loss};
-  const Score o{};
   const hipStream_t s = (hipStream_t)stream;
   switch (type) {
-    case TOC_F32: return launch<float, kTeach>(rows_of<float>(n, d, Z, ldz, scale), o, t, s);
-    case TOC_BF16: return launch<bf16, kTeach>(rows_of<bf16>(n, d, Z, ldz, scale), o, t, s);
-    default: return launch<f16, kTeach>(rows_of<f16>(n, d, Z, ldz, scale), o, t, s);
+    case TOC_F32: return distill(rows_of<float>(n, d, Z, ldz, scale), t, ws, s);
+    case TOC_BF16: return distill(rows_of<bf16>(n, d, Z, ldz, scale), t, ws, s);
+    default: return distill(rows_of<f16>(n, d, Z, ldz, scale), t, ws, s);
   }
 }
 

@@ -62,6 +62,9 @@ __device__ inline uint32_t wave_min(uint32_t x) {
 __device__ inline uint32_t wave_max(uint32_t x) {
   return wave_all(x, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
+__device__ inline uint32_t wave_or(uint32_t x) {
+  return wave_all(x, 0u, [](uint32_t a, uint32_t b) { return a | b; });
+}
 __device__ inline float wave_sum(float x) {
   return __uint_as_float(wave_all(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) {
     return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
@@ -466,6 +469,64 @@ struct Taught {
     return sum_log - scale * fmaf(r - e.m, sum, sum_z) + e.log_s * sum;
   }
 };
+
+// --- few long rows ---------------------------------------------------------------
+
+// A row dealt out to `parts` workgroups, `per` chunks to each: their sums (and their largest keys) are
+// left in the workspace and put together by a second launch.
+struct Split {
+  int parts, per;
+  Sums *sums;          // n x parts
+  uint64_t *keys;      // n x parts x alternatives
+};
+constexpr int kMaxParts = 64;
+constexpr int64_t kMaxPieces = 512;        // rows times parts, where there are parts
+constexpr int kPartLanes = 512, kPartPer = 6;
+
+// A row's part of a workgroup of the launches over parts.
+struct Piece {
+  int64_t row;
+  int part, q0, end;
+};
+__device__ inline Piece piece_of(const Split &s, int chunks) {
+  Piece p;
+  p.row = (int64_t)(blockIdx.x / (uint32_t)s.parts);
+  p.part = (int)(blockIdx.x % (uint32_t)s.parts);
+  p.q0 = min(p.part * s.per, chunks);
+  p.end = min(p.q0 + s.per, chunks);
+  return p;
+}
+// A whole row's sums from its parts', in every wave.
+template <bool kT>
+__device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
+  const int lane = (int)threadIdx.x % 64;
+  Sums a{kNone, 0.0f, 0.0f};
+  if (lane < s.parts) a = s.sums[row * s.parts + lane];
+  return wave_sums<kT>(a, c);
+}
+
+// The split of n rows of `chunks` chunks, k alternatives: parts of 1,024 chunks at least, so many
+// that the second launch, of some 2 us, is worth it, of 4,096 where alternatives are looked for in each
+// and at most 256 of them come together; 1 where there are rows enough.
+inline int parts_of(int64_t n, int64_t chunks, int k) {
+  if (n >= 128) return 1;
+  const int64_t most = k ? std::min(chunks / 4096, (int64_t)256 / k) : std::min(chunks / 1024, (int64_t)kMaxParts);
+  return (int)std::max<int64_t>(1, std::min(most, kMaxPieces / n));
+}
+inline Split split_of(int64_t n, int64_t chunks, int k, void *ws) {
+  Split s{};
+  s.parts = n ? parts_of(n, chunks, k) : 1;
+  // (a skewed row has a chunk more)
+  s.per = (int)((chunks + 1 + s.parts - 1) / s.parts);
+  s.keys = (uint64_t *)ws;
+  s.sums = (Sums *)(s.keys + n * s.parts * k);
+  return s;
+}
+// Sums of parts for the gradients, and what is made of a row's parts, in toc_logits.hip.
+template <typename T>
+toc_status add_parts(const Rows<T> &a, int k, bool entropy, const Split &s, hipStream_t stream);
+template <typename T>
+toc_status join_parts(const Rows<T> &a, const Score &o, const Teacher &t, const Split &s, hipStream_t stream);
 
 // --- checks ------------------------------------------------------------------------
 
