@@ -185,13 +185,14 @@ struct Batch {
   static constexpr int N = kCols<T>;
   Chunk in[kPer], edge;
   int q, rows, next, lane;        // first chunk, rows of whole chunks, first chunk after the batch
-  int skew;
+  int skew, end;
   bool ragged;                    // whether the lane's wave has a part of an edge
 
   __device__ inline int column(int k) const { return N * (q + k * kLanes + lane) - skew; }
 
-  __device__ inline void load(const T *row, int skew_, int q_, int end, int d, int lane_) {
+  __device__ inline void load(const T *row, int skew_, int q_, int end_, int d, int lane_) {
     q = q_;
+    end = end_;
     lane = lane_;
     skew = skew_;
     const int whole = min(end, (d + skew) / N);
@@ -505,11 +506,13 @@ __device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
   return wave_sums<kT>(a, c);
 }
 
-// The split of n rows of `chunks` chunks, k alternatives: parts of 1,024 chunks at least, so many
-// that the second launch, of some 2 us, is worth it, of 4,096 where alternatives are looked for in each
-// and at most 256 of them come together; 1 where there are rows enough.
+// The split of n rows of `chunks` chunks, k alternatives, into parts of 1,024 chunks or more; 1
+// where rows are short or enough (us, whole and in parts: log probabilities of 1 x 262,144 f32 17.9,
+// 5.2, of 64 x 262,144 bf16 18.3, 10.3, of 16 x 47,236 bf16 6.1, 6.7, of 200 x 100,000 bf16 10.2,
+// 12.8; gradient of 1 x 100,000 bf16 13.3, 8.7, of 64 x 65,536 bf16 10.1, 11.5).  Alternatives are
+// looked for in each part, so parts are of 4,096 chunks then, and at most 256 come together.
 inline int parts_of(int64_t n, int64_t chunks, int k) {
-  if (n >= 128) return 1;
+  if (n >= 128 || chunks <= 8192) return 1;
   const int64_t most = k ? std::min(chunks / 4096, (int64_t)256 / k) : std::min(chunks / 1024, (int64_t)kMaxParts);
   return (int)std::max<int64_t>(1, std::min(most, kMaxPieces / n));
 }

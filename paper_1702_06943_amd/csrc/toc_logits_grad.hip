@@ -24,6 +24,22 @@ struct Slope {
   bool none;           // 0 throughout: the coefficients are 0, or there are no probabilities
 };
 
+// gl, gs, ge: the coefficients of log p, of the sum and of the entropy; with a teacher gs is that of p.
+template <bool kTeach>
+__device__ inline Slope slope_of(float scale, const Sums &s, const End &e, float gl, float gs, float ge) {
+  Slope k;
+  if (kTeach) {
+    k.none = e.empty || gs == 0.0f;
+    k.a = scale * gs / s.s;
+    k.b = 0.0f;
+  } else {
+    k.none = e.empty || (gl == 0.0f && gs == 0.0f && ge == 0.0f);
+    k.a = scale * (gs - gl + ge * e.t_s) / s.s;
+    k.b = -scale * ge * kLn2 / s.s;
+  }
+  return k;
+}
+
 // A teacher's entries by the chunk of a window of kChunks chunks that holds their column: head[c] is
 // 0 or the number, from 1, of the first entry of a list that goes on with next.  Made by one wave.
 template <int kChunks>
@@ -127,9 +143,23 @@ __device__ inline void put_batch(Batch<T, kLanes, kPer> &b, float c, float base,
     }
     T *to = (T *)((char *)(dz + (N * (b.q + j * kLanes) - b.skew)) + (uint32_t)(16 * b.lane));
     const Chunk out = narrow<T>(v);
+    // (an edge's lanes past the batch's last chunk have what others write)
+    if (j == b.rows && b.q + j * kLanes + b.lane >= b.end) return;
     if ((j < b.rows || at + N <= d) && (j > 0 || at >= 0)) put(to, N, out, stream);
     else put_some(to, -at, d - at, out);
   });
+}
+
+// Zeros to chunks q, q + step and so on below end.
+template <typename T>
+__device__ inline void put_zeros(T *dz, int skew, int q, int end, int step, int d) {
+  constexpr int N = kCols<T>;
+  const Chunk zero = {0u, 0u, 0u, 0u};
+  for (; q < end; q += step) {
+    const int at = N * q - skew;
+    if (at >= 0 && at + N <= d) put(dz + at, N, zero, false);
+    else put_some(dz + at, -at, d - at, zero);
+  }
 }
 
 // kLanes lanes to a row, kPer chunks to a lane: a row of as many chunks stays in registers between
@@ -193,18 +223,9 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   } else if (lane == 0) {
     score_row(o, row, id, zt, e, a.scale);
   }
-  Slope k;
-  if (kTeach) {
-    k.none = e.empty || gs == 0.0f;
-    k.a = a.scale * gs / s.s;
-    k.b = 0.0f;
-  } else {
-    k.none = e.empty || (gl == 0.0f && gs == 0.0f && ge == 0.0f);
-    k.a = a.scale * (gs - gl + ge * e.t_s) / s.s;
-    k.b = -a.scale * ge * kLn2 / s.s;
-  }
+  const Slope k = slope_of<kTeach>(a.scale, s, e, gl, gs, ge);
   if (k.none) {
-    for (int q = lane; q < a.chunks; q += kLanes) put(dz + N * q, a.d - N * q, Chunk{0u, 0u, 0u, 0u}, g.stream);
+    put_zeros<T>(dz, skew, lane, chunks, kLanes, a.d);
     return;
   }
   const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
@@ -223,11 +244,69 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   }
 }
 
+// A part of a row, from the sums of all its parts.
 template <typename T, bool kTeach, bool kEntropy>
-toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad<T> &g, hipStream_t s) {
+__global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g, Split split) {
+  constexpr int N = kCols<T>, kLanes = kPartLanes;
+  using M = typename std::conditional<kTeach, Marks<kLanes *(kPartPer + 1)>, NoMarks>::type;
+  __shared__ M marks;
+  const int lane = (int)threadIdx.x;
+  const int64_t row = (int64_t)(blockIdx.x / (uint32_t)split.parts);
+  const T *z = a.Z + row * a.ldz;
+  T *dz = g.dZ + row * g.lddz;
+  const int skew = skew_of(z, a.d);
+  const Piece p = piece_of(split, chunks_in<T>(a.d, skew));
+  const bool first = lane < 64;
+  int id = -1;
+  float gl = 0.0f, gs = 0.0f, ge = 0.0f;
+  if constexpr (kTeach) {
+    gl = scalar(g.dloss, row);
+    if (first) {
+      Taught x;
+      x.ask(t, row, a.d, lane);
+      x.learn(t, row);
+      marks.keep(x, lane);
+    }
+  } else {
+    id = scalar_token(o.ids, row, a.d);
+    if (id >= 0 && g.dlogp) gl = scalar(g.dlogp, row);
+    if (g.dlse) gs = scalar(g.dlse, row);
+    if (g.dentropy) ge = scalar(g.dentropy, row);
+  }
+  const Sums s = parts_sums<kEntropy>(split, row, a.c);
+  const End e = end_of(s);
+  __syncthreads();
+  if constexpr (kTeach) gs = gl == 0.0f ? 0.0f : gl * marks.sum;
+  const Slope k = slope_of<kTeach>(a.scale, s, e, gl, gs, ge);
+  if (k.none) {
+    put_zeros<T>(dz, skew, p.q0 + lane, p.end, kLanes, a.d);
+    return;
+  }
+  const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
+  Batch<T, kLanes, kPartPer> b;
+  for (int q = p.q0; q < p.end; q = b.next) {
+    if constexpr (kTeach) {
+      __syncthreads();             // the batch before is done with its marks
+      if (first) marks.mark(t.k, q, N, skew, lane);
+      __syncthreads();
+    }
+    b.load(z, skew, q, p.end, a.d, lane);
+    b.trim();
+    put_batch<kEntropy>(b, a.c, base, k, id, hit, marks, dz, a.d, g.stream);
+  }
+}
+
+template <typename T, bool kTeach, bool kEntropy>
+toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad<T> &g, const Split &split,
+                  hipStream_t s) {
 #define TOC_GRAD(L, K)                                                                           \
   hipLaunchKernelGGL((grad_kernel<T, L, K, kTeach, kEntropy>),                                   \
                      grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
+  if (split.parts > 1) {
+    hipLaunchKernelGGL((part_grad_kernel<T, kTeach, kEntropy>), dim3((unsigned)(a.n * (uint32_t)split.parts)),
+                       dim3(kPartLanes), 0, s, a, o, t, g, split);
+    return launched("part_grad_kernel");
+  }
   const auto fits = [&](int lanes, int per) { return a.chunks + 1 < lanes * (per + 1); };
   if (fits(64, 2)) TOC_GRAD(64, 2);
   else if (fits(64, 8)) TOC_GRAD(64, 8);
@@ -243,13 +322,22 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
 template <typename T, bool kTeach>
 toc_status grad(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale, const Score &o,
                 const Teacher &t, void *dZ, int64_t lddz, const float *dlogp, const float *dlse,
-                const float *dentropy, const float *dloss, void *stream) {
+                const float *dentropy, const float *dloss, void *ws, void *stream) {
   const Rows<T> a = rows_of<T>(n, d, Z, ldz, scale);
   const Grad<T> g{(T *)dZ, lddz, dlogp, dlse, dentropy, dloss, stream_out(n, d, sizeof(T))};
-  if constexpr (!kTeach) {
-    if (o.entropy || dentropy) return launch<T, false, true>(a, o, t, g, (hipStream_t)stream);
+  const hipStream_t s = (hipStream_t)stream;
+  const Split split = split_of(n, a.chunks, 0, ws);
+  const bool entropy = !kTeach && (o.entropy || dentropy);
+  if (split.parts > 1) {
+    // (what is asked for beside dZ before it is written: it may be Z)
+    toc_status st = add_parts<T>(a, 0, entropy, split, s);
+    if (!st && (o.logp || o.lse || o.entropy || t.loss)) st = join_parts<T>(a, o, t, split, s);
+    if (st) return st;
   }
-  return launch<T, kTeach, false>(a, o, t, g, (hipStream_t)stream);
+  if constexpr (!kTeach) {
+    if (entropy) return launch<T, false, true>(a, o, t, g, split, s);
+  }
+  return launch<T, kTeach, false>(a, o, t, g, split, s);
 }
 
 }  // namespace
@@ -280,11 +368,11 @@ toc_status toc_logprob_grad(int64_t n, int32_t d, int32_t type, const void *Z, i
   const Teacher t{};
   switch (type) {
     case TOC_F32:
-      return grad<float, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, stream);
+      return grad<float, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, ws, stream);
     case TOC_BF16:
-      return grad<bf16, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, stream);
+      return grad<bf16, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, ws, stream);
     default:
-      return grad<f16, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, stream);
+      return grad<f16, false>(n, d, Z, ldz, scale, o, t, dZ, lddz, dlogp, dlse, dentropy, nullptr, ws, stream);
   }
 }
 
@@ -305,11 +393,11 @@ toc_status toc_distill_grad(int64_t n, int32_t d, int32_t type, const void *Z, i
   const Teacher t{Ids{top_ids, id_bits}, ldi, k, t_type, top_z, ldt, top_scale, top_lse, loss};
   switch (type) {
     case TOC_F32:
-      return grad<float, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, stream);
+      return grad<float, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, ws, stream);
     case TOC_BF16:
-      return grad<bf16, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, stream);
+      return grad<bf16, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, ws, stream);
     default:
-      return grad<f16, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, stream);
+      return grad<f16, true>(n, d, Z, ldz, scale, o, t, dZ, lddz, nullptr, nullptr, nullptr, dloss, ws, stream);
   }
 }
 
