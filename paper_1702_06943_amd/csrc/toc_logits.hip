@@ -291,15 +291,22 @@ __global__ __launch_bounds__(kThreads<kLanes>, 8) void score_kernel(Rows<T> a, S
   if (row >= a.n) return;
   const T *z = a.Z + row * a.ldz;
   const bool first = lane < 64;          // the wave that has the row's few numbers
-  Taught x;
-  if ((kWhat & kTeach) && first) x.ask(t, row, a.d, lane);
-  const int id = kWhat & kTeach ? -1 : scalar_token(o.ids, row, a.d);
+  Taught::Raw entries;
+  RawId given{~0u, ~0u};
+  if (kWhat & kTeach) {
+    if (first) entries = Taught::ask(t, row, lane);
+  } else {
+    given = scalar_id(o.ids, row);
+  }
   Batch<T, kLanes, kPer> b;
   const int skew = skew_of(z, a.d);
   const Part<T> p{z, a.d, skew, 0, chunks_in<T>(a.d, skew)};
   b.load(z, skew, p.q0, p.end, a.d, lane);
+  Taught x;
   float zt = 0.0f;
+  const int id = token_of(given, o.ids.bits, a.d);
   if ((kWhat & kTeach) && first) {
+    x.read(t, entries, a.d);
     x.gather(t, z);
     x.learn(t, row);
   }
@@ -364,11 +371,11 @@ __global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t,
   const int64_t row = blockIdx.x;
   const T *z = a.Z + row * a.ldz;
   Taught x;
-  if (kWhat & kTeach) x.ask(t, row, a.d, lane);
-  const int id = kWhat & kTeach ? -1 : scalar_token(o.ids, row, a.d);
+  const int id = kWhat & kTeach ? -1 : token_of(scalar_id(o.ids, row), o.ids.bits, a.d);
   float zt = 0.0f;
   if (id >= 0) zt = (float)z[id];
   if (kWhat & kTeach) {
+    x.read(t, Taught::ask(t, row, lane), a.d);
     x.gather(t, z);
     x.learn(t, row);
     x.compare();

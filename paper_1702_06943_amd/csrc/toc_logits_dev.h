@@ -317,11 +317,14 @@ struct Ids {
   const void *p;   // or NULL: no token anywhere
   int bits;
 };
-__device__ inline int token_of(int64_t id, int d) { return id >= 0 && id < d ? (int)id : -1; }
-// Token number i, or -1 where it is none of 0..d-1.
-__device__ inline int token(const Ids &ids, int64_t i, int d) {
-  if (ids.bits == 32) return token_of(((const int32_t *)ids.p)[i], d);
-  return token_of(((const int64_t *)ids.p)[i], d);
+// A token number as it is loaded, so that the loads after it do not wait for it; -1 is no token.
+struct RawId {
+  uint32_t low, high;
+};
+// The token, or -1 where it is none of 0..d-1.
+__device__ inline int token_of(RawId r, int bits, int d) {
+  const int64_t id = bits == 32 ? (int64_t)(int32_t)r.low : (int64_t)((uint64_t)r.high << 32 | r.low);
+  return id >= 0 && id < d ? (int)id : -1;
 }
 // p[i] for an i that is the same in all lanes of a wave, by a scalar load, which no wait for a row's
 // loads holds up; what it reads is written by no launch that it runs in.
@@ -329,9 +332,16 @@ template <typename V>
 __device__ inline V scalar(const V *p, int64_t i) {
   return *(const __attribute__((address_space(4))) V *)(p + i);
 }
-__device__ inline int scalar_token(const Ids &ids, int64_t i, int d) {
-  if (!ids.p) return -1;
-  return token_of(ids.bits == 32 ? (int64_t)scalar((const int32_t *)ids.p, i) : scalar((const int64_t *)ids.p, i), d);
+__device__ inline RawId scalar_id(const Ids &ids, int64_t i) {
+  RawId r{~0u, ~0u};
+  if (!ids.p) return r;
+  if (ids.bits == 32) {
+    r.low = scalar((const uint32_t *)ids.p, i);
+  } else {
+    r.low = scalar((const uint32_t *)ids.p, 2 * i);
+    r.high = scalar((const uint32_t *)ids.p, 2 * i + 1);
+  }
+  return r;
 }
 
 // --- arguments -------------------------------------------------------------------
@@ -392,18 +402,36 @@ struct Taught {
   float sum, sum_log;  // of q and of q log q over the row
   float r, sum_z;      // r, and the sum of q (z - r)
 
-  // The columns and the saved logits: what the loads of the row's own logits wait for.
-  __device__ inline void ask(const Teacher &a, int64_t row, int d, int lane) {
+  // The columns and the saved logits as they lie in memory.
+  struct Raw {
+    RawId id[kPer];
+    uint32_t t[kPer];
+  };
+  __device__ static inline Raw ask(const Teacher &a, int64_t row, int lane) {
+    Raw raw;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      id[i] = -1;
-      t[i] = kNone;
+      raw.id[i] = RawId{~0u, ~0u};
+      raw.t[i] = 0;
       const int e = lane + 64 * i;
       if (64 * i >= a.k || e >= a.k) continue;
-      id[i] = token(a.ids, row * a.ldi + e, d);
-      const int64_t at = row * a.ldt + e;
-      t[i] = a.type == TOC_F32 ? ((const float *)a.t)[at]
-             : a.type == TOC_BF16 ? (float)((const bf16 *)a.t)[at] : (float)((const f16 *)a.t)[at];
+      const int64_t at = row * a.ldi + e, to = row * a.ldt + e;
+      if (a.ids.bits == 32) {
+        raw.id[i].low = ((const uint32_t *)a.ids.p)[at];
+      } else {
+        const uint2 v = ((const uint2 *)a.ids.p)[at];
+        raw.id[i] = RawId{v.x, v.y};
+      }
+      raw.t[i] = a.type == TOC_F32 ? ((const uint32_t *)a.t)[to] : (uint32_t)((const uint16_t *)a.t)[to];
+    }
+    return raw;
+  }
+  __device__ inline void read(const Teacher &a, const Raw &raw, int d) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      id[i] = token_of(raw.id[i], a.ids.bits, d);
+      t[i] = a.type == TOC_F32 ? __uint_as_float(raw.t[i])
+             : a.type == TOC_BF16 ? __uint_as_float(raw.t[i] << 16) : (float)__builtin_bit_cast(f16, (uint16_t)raw.t[i]);
     }
   }
   template <typename T>

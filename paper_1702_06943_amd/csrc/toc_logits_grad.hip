@@ -179,26 +179,30 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   T *dz = g.dZ + row * g.lddz;
   M &marks = all_marks[group];
   const bool first = lane < 64;          // the wave that has the row's few numbers
-  Taught x;
-  if (kTeach && first) x.ask(t, row, a.d, lane);
-  int id = -1;
+  Taught::Raw entries;
+  RawId given{~0u, ~0u};
   float gl = 0.0f, gs = 0.0f, ge = 0.0f;
   if (kTeach) {
+    if (first) entries = Taught::ask(t, row, lane);
     gl = scalar(g.dloss, row);
   } else {
-    id = scalar_token(o.ids, row, a.d);
-    if (id >= 0 && g.dlogp) gl = scalar(g.dlogp, row);
+    given = scalar_id(o.ids, row);
+    if (g.dlogp) gl = scalar(g.dlogp, row);
     if (g.dlse) gs = scalar(g.dlse, row);
     if (g.dentropy) ge = scalar(g.dentropy, row);
   }
-  Batch<T, kLanes, kPer> b;
   const int skew = skew_of(z, a.d), chunks = chunks_in<T>(a.d, skew);
+  Batch<T, kLanes, kPer> b;
   b.load(z, skew, 0, chunks, a.d, lane);
+  Taught x;
   float zt = 0.0f;
-  if (kTeach && first) x.gather(t, z);
+  const int id = token_of(given, o.ids.bits, a.d);
+  if (!kTeach && id < 0) gl = 0.0f;
   if (!kTeach && id >= 0) zt = (float)z[id];
   if constexpr (kTeach) {
     if (first) {
+      x.read(t, entries, a.d);
+      x.gather(t, z);
       x.learn(t, row);
       marks.keep(x, lane);
       const int rows = (a.d + skew) / N / kLanes;          // the last batch's first chunk
@@ -263,12 +267,12 @@ __global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score 
     gl = scalar(g.dloss, row);
     if (first) {
       Taught x;
-      x.ask(t, row, a.d, lane);
+      x.read(t, Taught::ask(t, row, lane), a.d);
       x.learn(t, row);
       marks.keep(x, lane);
     }
   } else {
-    id = scalar_token(o.ids, row, a.d);
+    id = token_of(scalar_id(o.ids, row), o.ids.bits, a.d);
     if (id >= 0 && g.dlogp) gl = scalar(g.dlogp, row);
     if (g.dlse) gs = scalar(g.dlse, row);
     if (g.dentropy) ge = scalar(g.dentropy, row);
@@ -312,8 +316,10 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
   else if (fits(64, 8)) TOC_GRAD(64, 8);
   else if (fits(256, 8)) TOC_GRAD(256, 8);
   else if (fits(512, 6)) TOC_GRAD(512, 6);
-  else if (fits(1024, 12) && !fits(1024, 6)) TOC_GRAD(1024, 12);
-  else if (fits(1024, 16) && !fits(1024, 6)) TOC_GRAD(1024, 16);
+  else if (fits(1024, 6)) TOC_GRAD(1024, 6);
+  else if (sizeof(T) == 2 && fits(512, 20)) TOC_GRAD(512, 20);
+  else if (fits(1024, 12)) TOC_GRAD(1024, 12);
+  else if (fits(1024, 16)) TOC_GRAD(1024, 16);
   else TOC_GRAD(1024, 6);
 #undef TOC_GRAD
   return launched("grad_kernel");
