@@ -199,14 +199,19 @@ struct Batch {
     rows = min(kPer, (whole - q) / kLanes);
     next = q + rows * kLanes;
     const bool last = whole - next < kLanes;
-    ragged = last && next + __builtin_amdgcn_readfirstlane(lane) < end;
+    const int wave = next + __builtin_amdgcn_readfirstlane(lane);
+    ragged = last && wave < end;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       uint32_t at = (uint32_t)(16 * lane);
       if (k == 0 && q == 0 && lane == 0) at = (uint32_t)skew * (uint32_t)sizeof(T);
       if (k < rows) in[k] = *(const Unaligned *)((const char *)(row + (N * (q + k * kLanes) - skew)) + at);
     }
-    if (ragged) edge = edge_chunk(row, N * (next + lane) - skew, min(d, N * end - skew), d);
+    if (ragged) {
+      const int at = N * (next + lane) - skew;
+      if (wave > 0 && wave + 64 <= whole) edge = *(const Unaligned *)(row + at);   // (all of the wave's are whole)
+      else edge = edge_chunk(row, at, min(d, N * end - skew), d);
+    }
     if (last) next = end;
   }
   // Puts a skewed row's first chunk right, before its first use.
