@@ -38,7 +38,7 @@ constexpr int kCand = 512;
 template <int kLanes, bool kOn>
 struct TopLds {
   uint64_t keys[!kOn ? 1 : kLanes > kCand ? kLanes : kCand];   // at first the lanes' own
-  uint64_t best[kLanes / 64];
+  uint64_t best[(kLanes + 63) / 64];
   uint16_t who[kOn ? kLanes : 1];           // lanes that may hold some
   uint64_t bound;
   uint32_t lanes, count;
@@ -284,7 +284,7 @@ template <typename T, int kLanes, int kPer, int kWhat>
 __global__ __launch_bounds__(kThreads<kLanes>, 8) void score_kernel(Rows<T> a, Score o, Teacher t) {
   constexpr int kGroups = kThreads<kLanes> / kLanes;
   constexpr bool kT = kWhat & kEntropy;
-  __shared__ Sums sums_lds[kGroups][kLanes / 64];
+  __shared__ Sums sums_lds[kGroups][(kLanes + 63) / 64];
   __shared__ TopLds<kLanes, (kWhat & kTop) != 0> top_lds[kGroups];
   const int lane = lane_of<kLanes>(), group = group_of<kLanes>();
   const int64_t row = row_of<kLanes>();
@@ -296,10 +296,10 @@ __global__ __launch_bounds__(kThreads<kLanes>, 8) void score_kernel(Rows<T> a, S
   if (kWhat & kTeach) {
     if (first) entries = Taught::ask(t, row, lane);
   } else {
-    given = scalar_id(o.ids, row);
+    given = id_of_row<kLanes>(o.ids, row);
   }
   Batch<T, kLanes, kPer> b;
-  const int skew = skew_of(z, a.d);
+  const int skew = skew_of<kLanes>(z, a.d);
   const Part<T> p{z, a.d, skew, 0, chunks_in<T>(a.d, skew)};
   b.load(z, skew, p.q0, p.end, a.d, lane);
   Taught x;
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kPartLanes) void part_kernel(Rows<T> a, int k, Spli
   const int lane = (int)threadIdx.x;
   const int64_t row = (int64_t)(blockIdx.x / (uint32_t)s.parts);
   const T *z = a.Z + row * a.ldz;
-  const int skew = skew_of(z, a.d);
+  const int skew = skew_of<kLanes>(z, a.d);
   const Piece piece = piece_of(s, chunks_in<T>(a.d, skew));
   Sums x{kNone, 0.0f, 0.0f};
   int most = 0;
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t,
   const int64_t row = blockIdx.x;
   const T *z = a.Z + row * a.ldz;
   Taught x;
-  const int id = kWhat & kTeach ? -1 : token_of(scalar_id(o.ids, row), o.ids.bits, a.d);
+  const int id = kWhat & kTeach ? -1 : token_of(id_of_row<64>(o.ids, row), o.ids.bits, a.d);
   float zt = 0.0f;
   if (id >= 0) zt = (float)z[id];
   if (kWhat & kTeach) {
@@ -400,6 +400,12 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_
 #define TOC_SCORE(L, K)                                                                          \
   hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>),                                             \
                      grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t)
+  if constexpr ((kWhat & (kTop | kTeach)) == 0) {
+    if (a.n >= kShortRows && a.chunks + 1 < 16 * 9) {
+      TOC_SCORE(16, 8);
+      return launched("score_kernel");
+    }
+  }
   if (a.chunks <= 256) TOC_SCORE(64, 4);
   else if (a.chunks <= 2048) TOC_SCORE(256, 4);
   else if (a.n >= 512) TOC_SCORE(512, 6);

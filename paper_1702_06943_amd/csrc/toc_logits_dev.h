@@ -40,10 +40,10 @@ __device__ inline Sums moved(Sums a, float base, float c) {
   return Sums{base, a.s * f, kT ? fmaf(a.s, y, a.t) * f : 0.0f};
 }
 
-// Over a wave's lanes, the same in all of them: by shifts within rows of 16 lanes and broadcasts of
-// their last ones, each one operation on the way into the adder (lanes without a source take the
-// operation's neutral number); the last lane has the result.
-template <typename Op>
+// Over kLanes lanes (a wave or its rows of 16), the same in all of them: by shifts within rows of 16
+// lanes and broadcasts of their last ones, each one operation on the way into the adder (lanes
+// without a source take the operation's neutral number); the last lane has the result.
+template <int kLanes = 64, typename Op>
 __device__ inline uint32_t wave_all(uint32_t x, uint32_t neutral, Op op) {
 #define TOC_STEP(ctrl, rows) \
   x = op(x, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)x, ctrl, rows, 0xf, false))
@@ -51,6 +51,7 @@ __device__ inline uint32_t wave_all(uint32_t x, uint32_t neutral, Op op) {
   TOC_STEP(0x112, 0xf);
   TOC_STEP(0x114, 0xf);
   TOC_STEP(0x118, 0xf);
+  if (kLanes == 16) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x15f, 0xf, 0xf, false);   // lane 15
   TOC_STEP(0x142, 0xa);   // lane 15 of a row to the next, rows 1 and 3
   TOC_STEP(0x143, 0xc);   // lane 31 to rows 2 and 3
 #undef TOC_STEP
@@ -65,29 +66,31 @@ __device__ inline uint32_t wave_max(uint32_t x) {
 __device__ inline uint32_t wave_or(uint32_t x) {
   return wave_all(x, 0u, [](uint32_t a, uint32_t b) { return a | b; });
 }
+template <int kLanes = 64>
 __device__ inline float wave_sum(float x) {
-  return __uint_as_float(wave_all(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) {
+  return __uint_as_float(wave_all<kLanes>(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) {
     return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
   }));
 }
+template <int kLanes = 64>
 __device__ inline float wave_max(float x) {
-  return __uint_as_float(wave_all(__float_as_uint(x), __float_as_uint(kNone), [](uint32_t a, uint32_t b) {
+  return __uint_as_float(wave_all<kLanes>(__float_as_uint(x), __float_as_uint(kNone), [](uint32_t a, uint32_t b) {
     return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   }));
 }
 
-template <bool kT>
+template <bool kT, int kLanes = 64>
 __device__ inline Sums wave_sums(Sums a, float c) {
-  const float m = wave_max(a.m);
+  const float m = wave_max<kLanes>(a.m);
   a = moved<kT>(a, from(m), c);
-  return Sums{m, wave_sum(a.s), kT ? wave_sum(a.t) : 0.0f};
+  return Sums{m, wave_sum<kLanes>(a.s), kT ? wave_sum<kLanes>(a.t) : 0.0f};
 }
-// The sums of a group of kLanes lanes (64: a wave; else the whole workgroup, by way of
+// The sums of a group of kLanes lanes (16 or 64: of a wave; else the whole workgroup, by way of
 // kLanes / 64 words of lds, which are free again after the caller's next barrier).
 template <int kLanes, bool kT>
 __device__ inline Sums group_sums(Sums a, float c, Sums *lds) {
-  a = wave_sums<kT>(a, c);
-  if (kLanes == 64) return a;
+  a = wave_sums<kT, kLanes == 16 ? 16 : 64>(a, c);
+  if (kLanes <= 64) return a;
   if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = a;
   __syncthreads();
   // every wave's sums again by all waves, one in a lane
@@ -114,11 +117,12 @@ __device__ inline void group_sync() {
 // best at multiples of 16 (8,192 x 32,767 bf16, whose rows start at odd multiples of 2: gradient
 // 191 us, 235 with chunks that start where rows do).  So a row's chunks are those of memory: its
 // first one starts `skew` columns before the row (nothing is read there: the row's first 16 bytes
-// are, and shifted).  Rows too short to gain have skew 0.
-template <typename T>
+// are, and shifted).  Rows too short to gain have skew 0, and those of less than a wave, whose
+// chunks would not be alike then.
+template <int kLanes, typename T>
 __device__ inline int skew_of(const T *z, int d) {
   constexpr int N = kCols<T>;
-  return d < 2 * N ? 0 : (int)((uintptr_t)z / sizeof(T) % N);
+  return kLanes < 64 || d < 2 * N ? 0 : (int)((uintptr_t)z / sizeof(T) % N);
 }
 template <typename T>
 __device__ inline int chunks_in(int d, int skew) {
@@ -209,7 +213,7 @@ struct Batch {
     }
     if (ragged) {
       const int at = N * (next + lane) - skew;
-      if (wave > 0 && wave + 64 <= whole) edge = *(const Unaligned *)(row + at);   // (all of the wave's are whole)
+      if (wave > 0 && wave + (kLanes < 64 ? kLanes : 64) <= whole) edge = *(const Unaligned *)(row + at);   // (all of the wave's are whole)
       else edge = edge_chunk(row, at, min(d, N * end - skew), d);
     }
     if (last) next = end;
@@ -281,10 +285,13 @@ inline dim3 grid_of(int64_t rows) {
   const int64_t wide = std::min<int64_t>(blocks, 1 << 20);
   return dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide));
 }
+// From so many short rows on 16 lanes have one.
+constexpr uint32_t kShortRows = 4096;
 // A thread's group of the workgroup, its row, both the same in all lanes of a wave, and its lane.
 template <int kLanes>
 __device__ inline int group_of() {
-  return kLanes >= kBlock ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);
+  const int group = (int)threadIdx.x / kLanes;
+  return kLanes >= kBlock ? 0 : kLanes == 64 ? __builtin_amdgcn_readfirstlane(group) : group;
 }
 template <int kLanes>
 __device__ inline int64_t row_of() {
@@ -337,14 +344,21 @@ template <typename V>
 __device__ inline V scalar(const V *p, int64_t i) {
   return *(const __attribute__((address_space(4))) V *)(p + i);
 }
-__device__ inline RawId scalar_id(const Ids &ids, int64_t i) {
+// A row's number: a scalar load where all lanes of a wave have the same row.
+template <int kLanes, typename V>
+__device__ inline V of_row(const V *p, int64_t i) {
+  if constexpr (kLanes >= 64) return scalar(p, i);
+  else return p[i];
+}
+template <int kLanes>
+__device__ inline RawId id_of_row(const Ids &ids, int64_t i) {
   RawId r{~0u, ~0u};
   if (!ids.p) return r;
   if (ids.bits == 32) {
-    r.low = scalar((const uint32_t *)ids.p, i);
+    r.low = of_row<kLanes>((const uint32_t *)ids.p, i);
   } else {
-    r.low = scalar((const uint32_t *)ids.p, 2 * i);
-    r.high = scalar((const uint32_t *)ids.p, 2 * i + 1);
+    r.low = of_row<kLanes>((const uint32_t *)ids.p, 2 * i);
+    r.high = of_row<kLanes>((const uint32_t *)ids.p, 2 * i + 1);
   }
   return r;
 }

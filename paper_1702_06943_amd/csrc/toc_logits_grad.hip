@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   constexpr int N = kCols<T>;
   constexpr int kGroups = kThreads<kLanes> / kLanes;
   using M = typename std::conditional<kTeach, Marks<kLanes *(kPer + 1)>, NoMarks>::type;
-  __shared__ Sums sums[kGroups][kLanes / 64];
+  __shared__ Sums sums[kGroups][(kLanes + 63) / 64];
   __shared__ M all_marks[kGroups];
   const int lane = lane_of<kLanes>(), group = group_of<kLanes>();
   const int64_t row = row_of<kLanes>();
@@ -184,14 +184,14 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   float gl = 0.0f, gs = 0.0f, ge = 0.0f;
   if (kTeach) {
     if (first) entries = Taught::ask(t, row, lane);
-    gl = scalar(g.dloss, row);
+    gl = of_row<kLanes>(g.dloss, row);
   } else {
-    given = scalar_id(o.ids, row);
-    if (g.dlogp) gl = scalar(g.dlogp, row);
-    if (g.dlse) gs = scalar(g.dlse, row);
-    if (g.dentropy) ge = scalar(g.dentropy, row);
+    given = id_of_row<kLanes>(o.ids, row);
+    if (g.dlogp) gl = of_row<kLanes>(g.dlogp, row);
+    if (g.dlse) gs = of_row<kLanes>(g.dlse, row);
+    if (g.dentropy) ge = of_row<kLanes>(g.dentropy, row);
   }
-  const int skew = skew_of(z, a.d), chunks = chunks_in<T>(a.d, skew);
+  const int skew = skew_of<kLanes>(z, a.d), chunks = chunks_in<T>(a.d, skew);
   Batch<T, kLanes, kPer> b;
   b.load(z, skew, 0, chunks, a.d, lane);
   Taught x;
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score 
   const int64_t row = (int64_t)(blockIdx.x / (uint32_t)split.parts);
   const T *z = a.Z + row * a.ldz;
   T *dz = g.dZ + row * g.lddz;
-  const int skew = skew_of(z, a.d);
+  const int skew = skew_of<kLanes>(z, a.d);
   const Piece p = piece_of(split, chunks_in<T>(a.d, skew));
   const bool first = lane < 64;
   int id = -1;
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score 
       marks.keep(x, lane);
     }
   } else {
-    id = token_of(scalar_id(o.ids, row), o.ids.bits, a.d);
+    id = token_of(id_of_row<64>(o.ids, row), o.ids.bits, a.d);
     if (id >= 0 && g.dlogp) gl = scalar(g.dlogp, row);
     if (g.dlse) gs = scalar(g.dlse, row);
     if (g.dentropy) ge = scalar(g.dentropy, row);
@@ -312,6 +312,12 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
     return launched("part_grad_kernel");
   }
   const auto fits = [&](int lanes, int per) { return a.chunks + 1 < lanes * (per + 1); };
+  if constexpr (!kTeach) {
+    if (a.n >= kShortRows && fits(16, 8)) {
+      TOC_GRAD(16, 8);
+      return launched("grad_kernel");
+    }
+  }
   if (fits(64, 2)) TOC_GRAD(64, 2);
   else if (fits(64, 8)) TOC_GRAD(64, 8);
   else if (fits(256, 8)) TOC_GRAD(256, 8);

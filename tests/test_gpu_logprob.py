@@ -287,10 +287,44 @@ def test_more_rows_than_workgroups():
     assert float((dZ - want).abs().max()) < 2e-6
 
 
-def test_equal_calls_and_rows_alone():
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("d", [1, 2, 7, 8, 9, 31, 127, 128, 129, 300, 572, 900, 1001, 1135, 1136, 1152])
+def test_many_short_rows(d, kind):
+    """So many rows that several share a wave, the last wave only partly filled; masked, padded and empty
+    rows beside others."""
+    rng = np.random.default_rng(d)
+    n, scale = 4097 + 6, float(np.float32(0.9))
+    Z, Z64 = logits(rng, n, d, kind, gap=3, shift=1, masked=0.2)
+    Z[5], Z[n - 2] = -INF, -INF
+    ids, idt = given(rng, n, d, 32)
+    g = rng.standard_normal((3, n)).astype(np.float32)
+    g[:, 7] = 0
+    dZ = blank(n, d, kind, 3, 1)
+    out = [torch.full((n,), 7.0, device=DEV) for _ in range(3)]
+    only = torch.full((n,), 7.0, device=DEV)
+    T.toc_logprob_grad(Z, dZ, idt, *(vec(x) for x in g), *out, scale)
+    T.toc_logprob(Z, idt, only, scale=scale)
+    assert gaps_untouched(dZ)
+    at = np.r_[:40, n - 40:n]
+    Z64, ids, g = Z[at].double().cpu().numpy(), ids[at], g[:, at]
+    s, real = Soft(Z64, scale), (ids >= 0) & (ids < d)
+    want = L.logprob_grad(Z64, ids, scale, *g)
+    close(dZ[at], want, grad_tol(s, want, kind, g[0] * real, g[1], g[2], np.arange(d) == ids[:, None]), "dZ")
+    score = L.logprob(Z64, ids, scale)
+    for got in (out[0][at], only[at]):
+        finite(got, score["logp"], s.logp_tol(np.where(real, ids, 0)[:, None])[:, 0], "logp")
+    finite(out[1][at], score["lse"], s.lse_tol(), "lse")
+    close(out[2][at], score["entropy"], s.entropy_tol(), "entropy")
+    again = blank(n, d, kind, 3, 1)
+    again.copy_(Z)
+    T.toc_logprob_grad(again, again, idt, *(vec(x) for x in rng.standard_normal((3, n))), scale=scale)
+    assert gaps_untouched(again)
+
+
+@pytest.mark.parametrize("n,d,k", [(33, 20000, 40), (33, 1500, 40), (9, 6001, 64), (3, 140001, 20), (700, 9000, 5)])
+def test_equal_calls_and_rows_alone(n, d, k):
     """Equal bits from equal calls; nothing is left in a workspace that a next call would find."""
     rng = np.random.default_rng(5)
-    n, d, k = 33, 20000, 40
     Z, _ = logits(rng, n, d, "bf16")
     _, idt = given(rng, n, d, 64)
     res = []
