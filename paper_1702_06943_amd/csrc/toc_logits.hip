@@ -281,7 +281,7 @@ __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int mo
 
 // kLanes lanes to a row, kPer chunks of a lane asked for at once.
 template <typename T, int kLanes, int kPer, int kWhat>
-__global__ __launch_bounds__(kThreads<kLanes>, 8) void score_kernel(Rows<T> a, Score o, Teacher t) {
+__global__ __launch_bounds__(kThreads<kLanes>, kLanes == 16 ? 6 : 8) void score_kernel(Rows<T> a, Score o, Teacher t) {
   constexpr int kGroups = kThreads<kLanes> / kLanes;
   constexpr bool kT = kWhat & kEntropy;
   __shared__ Sums sums_lds[kGroups][(kLanes + 63) / 64];

@@ -251,6 +251,40 @@ def test_logits_far_apart_and_overflowing():
         assert np.isfinite(host(dZ)).all()
 
 
+@pytest.mark.parametrize("size", [1e3, 1e5, 3e7, 3.7e8, 4e8, 1e9, 1e12, 1e25, 3e38])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("d", [40, 5000, 140000])
+def test_large_logits(d, sign, size):
+    """Logits whose scaled size passes what binary32 holds to one: neighbouring numbers, equal ones and far
+    ones, anywhere in a row."""
+    rng = np.random.default_rng(d)
+    n = 6
+    top = np.float32(sign * size)
+    Z = np.full((n, d), top, np.float32)
+    Z -= np.abs(top) * rng.random((n, d)).astype(np.float32) * np.float32(1e-3)
+    for i in range(n):
+        at = rng.permutation(d)[:12]
+        Z[i, at[:4]] = top
+        Z[i, at[4:8]] = np.nextafter(top, np.float32(-np.inf))
+        Z[i, at[8:]] = np.nextafter(Z[i, at[4:8]], np.float32(-np.inf))
+        if i % 2:
+            Z[i, at[:4]] = Z[i, at[9]]
+    Z = np.maximum(Z, -np.finfo(np.float32).max)
+    Zt, Z64 = torch.from_numpy(Z).to(DEV), Z.astype(np.float64)
+    ids = np.argmax(Z, axis=1)
+    ids[0] = np.argmin(Z[0])
+    g = rng.standard_normal((3, n)).astype(np.float32)
+    for scale in (1.0, float(np.float32(0.3))):
+        s = Soft(Z64, scale)
+        dZ, logp, h = torch.empty_like(Zt), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        idt = torch.from_numpy(ids).to(DEV)
+        T.toc_logprob_grad(Zt, dZ, idt, *(vec(x) for x in g), logp, None, h, scale, workspace(n, d))
+        want, score = L.logprob_grad(Z64, ids, scale, *g), L.logprob(Z64, ids, scale)
+        close(dZ, want, grad_tol(s, want, "f32", g[0], g[1], g[2], np.arange(d) == ids[:, None]), "dZ")
+        close(logp, score["logp"], s.logp_tol(ids[:, None])[:, 0], "logp")
+        close(h, score["entropy"], s.entropy_tol(), "entropy")
+
+
 def test_offsets_past_32_bits():
     ld, d, n = 1 << 26, 1000, 70
     buf = torch.empty(n * ld, dtype=torch.bfloat16, device=DEV)
