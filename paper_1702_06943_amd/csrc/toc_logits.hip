@@ -297,6 +297,11 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 16 ? 6 : 8) void score_
     if (first) entries = Taught::ask(t, row, lane);
   } else {
     given = id_of_row<kLanes>(o.ids, row);
+    // (what is asked for of a row without a token may need nothing of it)
+    if (!o.lse && !o.entropy && !o.k && token_of(given, o.ids.bits, a.d) < 0) {
+      if (lane == 0 && o.logp) o.logp[row] = 0.0f;
+      return;
+    }
   }
   Batch<T, kLanes, kPer> b;
   const int skew = skew_of<kLanes>(z, a.d);

@@ -192,12 +192,19 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     if (g.dentropy) ge = of_row<kLanes>(g.dentropy, row);
   }
   const int skew = skew_of<kLanes>(z, a.d), chunks = chunks_in<T>(a.d, skew);
+  const int id = token_of(given, o.ids.bits, a.d);
+  if (!kTeach && id < 0) gl = 0.0f;
+  // a row that takes no part, and of which nothing is asked for, is not read
+  if (kTeach ? gl == 0.0f && !t.loss
+             : gl == 0.0f && gs == 0.0f && ge == 0.0f && !o.lse && !o.entropy && !(o.logp && id >= 0)) {
+    if (!kTeach && lane == 0 && o.logp) o.logp[row] = 0.0f;
+    put_zeros<T>(dz, skew, lane, chunks, kLanes, a.d);
+    return;
+  }
   Batch<T, kLanes, kPer> b;
   b.load(z, skew, 0, chunks, a.d, lane);
   Taught x;
   float zt = 0.0f;
-  const int id = token_of(given, o.ids.bits, a.d);
-  if (!kTeach && id < 0) gl = 0.0f;
   if (!kTeach && id >= 0) zt = (float)z[id];
   if constexpr (kTeach) {
     if (first) {
