@@ -527,7 +527,7 @@ struct Split {
   Sums *sums;          // n x parts
   uint64_t *keys;      // n x parts x alternatives
 };
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 64;              // a wave puts them together
 constexpr int64_t kMaxPieces = 512;        // rows times parts, where there are parts
 constexpr int kPartLanes = 512, kPartPer = 6;
 
@@ -560,8 +560,8 @@ __device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
 // looked for in each part, so parts are of 4,096 chunks then, and at most 256 come together.
 inline int parts_of(int64_t n, int64_t chunks, int k) {
   if (n >= 128 || chunks <= 8192) return 1;
-  const int64_t most = k ? std::min(chunks / 4096, (int64_t)256 / k) : std::min(chunks / 1024, (int64_t)kMaxParts);
-  return (int)std::max<int64_t>(1, std::min(most, kMaxPieces / n));
+  const int64_t most = k ? std::min(chunks / 4096, (int64_t)256 / k) : chunks / 1024;
+  return (int)std::max<int64_t>(1, std::min({most, (int64_t)kMaxParts, kMaxPieces / n}));
 }
 inline Split split_of(int64_t n, int64_t chunks, int k, void *ws) {
   Split s{};

@@ -143,6 +143,9 @@ def test_bad_rows_that_take_no_part():
     T.toc_distill_grad(Z, dZ, ids, t, torch.tensor([0.0, 1.0, 1.0, 1.0], device=DEV), loss, ws=workspace(4, 900))
     assert not host(dZ)[:2].any() and np.isnan(host(dZ)[2]).all() and np.isfinite(host(dZ)[3]).all()
     assert np.isnan(host(loss)[[0, 2]]).all() and host(loss)[1] == 0
+    again = torch.full_like(Z, 7.0)
+    T.toc_distill_grad(Z, again, ids, t, torch.tensor([0.0, 1.0, 1.0, 1.0], device=DEV), ws=workspace(4, 900))
+    assert np.array_equal(host(again), host(dZ), equal_nan=True)
 
 
 def test_strided_teacher():

@@ -119,6 +119,59 @@ def test_ties(kind):
             assert np.array_equal(top.cpu().numpy(), want), width
 
 
+@pytest.mark.parametrize("lanes", [16, 64, 256, 512, 1024])
+@pytest.mark.parametrize("n,d", [(3, 2500), (3, 40001), (130, 400001), (3, 400001), (600, 17000)])
+def test_largest_in_few_lanes(n, d, lanes):
+    """The largest logits of each row, many times the alternatives, all in the columns of one lane of 16 bytes
+    in so many, rising, falling and equal."""
+    j = torch.arange(d, device=DEV)
+    rng = np.random.default_rng(d + lanes)
+    Z = torch.randn((n, d), device=DEV, generator=torch.Generator(DEV).manual_seed(d)).to(torch.bfloat16)
+    at = j // 8 % lanes == 5
+    for i, x in enumerate((j * (8 / d) + 10, 20 - j * (8 / d), torch.full((d,), 11.0, device=DEV))):
+        Z[i::3, at] = x[at].to(torch.bfloat16)
+    k = 64
+    top, lp = torch.empty((n, k), dtype=torch.int32, device=DEV), torch.empty((n, k), device=DEV)
+    T.toc_logprob(Z, top_ids=top, top_logp=lp, ws=workspace(n, d, k))
+    for i in {0, 1, 2, n - 1, n - 2}:
+        want = torch.sort(Z[i].float(), descending=True, stable=True).indices[:k]
+        assert torch.equal(top[i].long(), want), i
+
+
+@pytest.mark.parametrize("n,d,kind", [(1, 1 << 28, "f32"), (1, (1 << 26) + 3, "bf16"), (128, (1 << 21) + 5, "bf16")])
+def test_longest_rows(n, d, kind):
+    g = torch.Generator(DEV).manual_seed(n)
+    Z = torch.randn((n, d), generator=g, device=DEV).to(TYPES[kind])
+    Z[0, d - 1], Z[0, 12345] = 9.0, 9.0
+    ids = torch.full((n,), d - 1, device=DEV)
+    logp, h, lse = (torch.empty(n, device=DEV) for _ in range(3))
+    top, tl = torch.empty((n, 3), dtype=torch.int64, device=DEV), torch.empty((n, 3), device=DEV)
+    T.toc_logprob(Z, ids, logp, lse, h, top, tl, ws=workspace(n, d, 3))
+    z = Z[0].double()
+    want = torch.logsumexp(z, 0)
+    lp = z - want
+    # sums of positive numbers in binary32, some d / 4096 of a lane in a row: 4e-3 at the worst, 1e-4 in
+    # fact (roundings of either sign)
+    assert abs(float(lse[0] - want)) < 1e-4 and abs(float(logp[0] - lp[-1])) < 1e-4
+    assert abs(float(h[0] + (lp.exp() * lp).sum())) < 2e-3
+    assert top[0, :2].tolist() == [12345, d - 1]
+    # the same numbers as a teacher's, and the gradients in place
+    entries = torch.tensor([12345, 7, d - 1, -1, 7], device=DEV).expand(n, 5).contiguous()
+    t = torch.tensor([1.0, 2.0, 0.5, 9.0, 0.0], device=DEV).expand(n, 5).contiguous()
+    loss = torch.empty(n, device=DEV)
+    dZ, c = torch.empty_like(Z), torch.ones(n, device=DEV)
+    T.toc_distill_grad(Z, dZ, entries, t, c, loss, ws=workspace(n, d))
+    q = torch.softmax(torch.tensor([1.0, 2.0, 0.5, 0.0], dtype=torch.float64, device=DEV), 0)
+    at = torch.tensor([12345, 7, d - 1, 7], device=DEV)
+    assert abs(float(loss[0] - (q * (q.log() - lp[at])).sum())) < 2e-4
+    back = lp.exp().index_add_(0, at, -q)
+    assert float((dZ[0].double() - back).abs().max()) < 4e-3
+    T.toc_logprob_grad(Z, Z, ids, c, ws=workspace(n, d))
+    back = -lp.exp()
+    back[-1] += 1
+    assert float((Z[0].double() - back).abs().max()) < 4e-3
+
+
 @pytest.mark.parametrize("kind", sorted(TYPES))
 @pytest.mark.parametrize("d", [300, 3001, 30000])
 def test_infinities_and_nan(d, kind):
@@ -145,6 +198,11 @@ def test_infinities_and_nan(d, kind):
     g = host(dZ)
     assert np.isnan(g[0]).any() and np.isnan(g[2]).all()
     assert not g[1].any() and not g[3].any()                       # no coefficient: 0, whatever it holds
+    again = torch.full_like(Z, 7.0)
+    T.toc_logprob_grad(Z, again, ids, gl, logp=logp, ws=workspace(6, d))
+    assert np.array_equal(host(again), g, equal_nan=True) and np.isnan(host(logp)[1]) and host(logp)[3] == 0
+    T.toc_logprob(Z, ids, logp, ws=workspace(6, d))                # a row without a token is not read
+    assert np.isnan(host(logp)[1]) and host(logp)[3] == 0
     assert abs(g[4, 0] - 1) < 1e-2 and np.isfinite(g[4:]).all()    # the masked token's own part remains
 
 
