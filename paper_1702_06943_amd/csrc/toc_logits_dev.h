@@ -213,7 +213,8 @@ struct Batch {
     }
     if (ragged) {
       const int at = N * (next + lane) - skew;
-      if (wave > 0 && wave + (kLanes < 64 ? kLanes : 64) <= whole) edge = *(const Unaligned *)(row + at);   // (all of the wave's are whole)
+      // (a wave whose chunks are all whole reads them as they are)
+      if (wave > 0 && wave + (kLanes < 64 ? kLanes : 64) <= whole) edge = *(const Unaligned *)(row + at);
       else edge = edge_chunk(row, at, min(d, N * end - skew), d);
     }
     if (last) next = end;
@@ -450,7 +451,8 @@ struct Taught {
     for (int i = 0; i < kPer; ++i) {
       id[i] = token_of(raw.id[i], a.ids.bits, d);
       t[i] = a.type == TOC_F32 ? __uint_as_float(raw.t[i])
-             : a.type == TOC_BF16 ? __uint_as_float(raw.t[i] << 16) : (float)__builtin_bit_cast(f16, (uint16_t)raw.t[i]);
+             : a.type == TOC_BF16 ? __uint_as_float(raw.t[i] << 16)
+                                  : (float)__builtin_bit_cast(f16, (uint16_t)raw.t[i]);
     }
   }
   template <typename T>

@@ -2,7 +2,13 @@
 // from a teacher's saved logits.  With p_j and H as in the forward pass, row by row:
 //   dz_j = scale (gl (1[j = t] - p_j) + gs p_j - ge p_j (log p_j + H))
 //   dz_j = scale c (Q p_j - sum of q_a over the entries with i_a = j)
-// The probabilities are formed again from the logits: nothing is kept from the forward pass.
+// The probabilities are formed again from the logits: nothing is kept from the forward pass, and what it
+// would have given comes along, so that a training step is one read and one write of the logits.
+//   grad_kernel       bound by memory: 8,192 x 47,236 bf16 269 us, 5.75 TB/s (a plain map of as many bytes
+//                     takes 250), with entropy 271, a teacher's 64 entries 278; 250 x 47,236 f32 20 us, a row a
+//                     CU whose read and write are one after the other; 512 x 200,003 bf16 95 us, the
+//                     rows read once more, three quarters of that from memory
+//   part_grad_kernel  few long rows, after part_kernel: one of 262,144 f32 8.4 us, 64 of bf16 20.9
 #include "toc_logits_dev.h"
 
 namespace toc {
@@ -165,8 +171,8 @@ __device__ inline void put_zeros(T *dz, int skew, int q, int end, int step, int 
 // kLanes lanes to a row, kPer chunks to a lane: a row of as many chunks stays in registers between
 // its one read and its one write, a longer one is read twice.
 template <typename T, int kLanes, int kPer, bool kTeach, bool kEntropy>
-__global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 : 4) void grad_kernel(Rows<T> a, Score o,
-                                                                                                  Teacher t, Grad<T> g) {
+__global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 : 4) void grad_kernel(
+    Rows<T> a, Score o, Teacher t, Grad<T> g) {
   constexpr int N = kCols<T>;
   constexpr int kGroups = kThreads<kLanes> / kLanes;
   using M = typename std::conditional<kTeach, Marks<kLanes *(kPer + 1)>, NoMarks>::type;
@@ -257,7 +263,8 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
 
 // A part of a row, from the sums of all its parts.
 template <typename T, bool kTeach, bool kEntropy>
-__global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g, Split split) {
+__global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score o, Teacher t, Grad<T> g,
+                                                               Split split) {
   constexpr int N = kCols<T>, kLanes = kPartLanes;
   using M = typename std::conditional<kTeach, Marks<kLanes *(kPartPer + 1)>, NoMarks>::type;
   __shared__ M marks;
@@ -310,14 +317,20 @@ __global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score 
 template <typename T, bool kTeach, bool kEntropy>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad<T> &g, const Split &split,
                   hipStream_t s) {
-#define TOC_GRAD(L, K)                                                                           \
-  hipLaunchKernelGGL((grad_kernel<T, L, K, kTeach, kEntropy>),                                   \
-                     grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
+#define TOC_GRAD(L, K)                                                                             \
+  hipLaunchKernelGGL((grad_kernel<T, L, K, kTeach, kEntropy>), grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t, g)
   if (split.parts > 1) {
     hipLaunchKernelGGL((part_grad_kernel<T, kTeach, kEntropy>), dim3((unsigned)(a.n * (uint32_t)split.parts)),
                        dim3(kPartLanes), 0, s, a, o, t, g, split);
     return launched("part_grad_kernel");
   }
+  // The fewest lanes that hold a row, so that a CU has several rows in turns of reading and writing (us, bf16
+  // gradients): 40,000 x 1,800 by 64 x 8, 256 x 8 lanes and chunks 52, 102; 10,000 x 8,003 by 256 x 8, 1,024 x 2
+  // 52, 99; 8,000 x 16,384 by 512 x 6, 256 x 8 80, 86; but 8,192 x 47,236 by 1,024 x 6, 512 x 12, 256 x 24 270, 302,
+  // 315, whose rows in flight are fewer at once; 2,000 x 65,536 by 512 x 20, 1,024 x 12 85, 95, and the other
+  // way with binary32: 4,000 x 47,236 by 1,024 x 12, 512 x 24 291, 309.  Longer rows are read twice, by 1,024 x 6
+  // rather than 1,024 x 16, which holds more of them but has a row a CU (512 x 200,003 84, 89).  Many
+  // short rows: 18,750 x 900 f16 by 16, 64 lanes 16.8, 18.9, of 100 bf16 6.1, 13.1; 2,000 of 900 6.4, 5.3.
   const auto fits = [&](int lanes, int per) { return a.chunks + 1 < lanes * (per + 1); };
   if constexpr (!kTeach) {
     if (a.n >= kShortRows && fits(16, 8)) {
