@@ -51,7 +51,7 @@ __device__ inline Slope slope_of(float scale, const Sums &s, const End &e, float
 template <int kChunks>
 struct Marks {
   static constexpr int kHeads = (kChunks + 511) / 512 * 512;
-  uint16_t head[kHeads];
+  alignas(16) uint16_t head[kHeads];       // (cleared 16 bytes at a time)
   uint16_t next[kMaxTeacher];
   int column[kMaxTeacher];
   float q[kMaxTeacher];
@@ -229,8 +229,12 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
     b.load(z, skew, b.next, chunks, a.d, lane);
     add_batch<kEntropy>(b, a.c, s, most);
   }
-  if (kTeach && first) x.compare();
-  // (behind this barrier dZ, which may be Z, is written: all of Z that is not read again is there)
+  // (behind the next barrier dZ, which may be Z, is written: all of Z that is not read again has to be there)
+  if (kTeach) {
+    if (first) x.compare();
+  } else {
+    asm volatile("" ::"v"(zt));
+  }
   s = group_sums<kLanes, kEntropy>(s, a.c, sums[group]);
   const End e = end_of(s);
   if constexpr (kTeach) {
