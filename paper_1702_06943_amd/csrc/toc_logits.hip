@@ -427,7 +427,7 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_
   if (a.chunks <= 256) TOC_SCORE(64, 4);
   else if (a.chunks <= 2048) TOC_SCORE(256, 4);
   else if (a.n >= 512) TOC_SCORE(512, 6);
-  else TOC_SCORE(1024, 4);
+  else TOC_SCORE(1024, 6);
 #undef TOC_SCORE
   return launched("score_kernel");
 }
