@@ -44,7 +44,7 @@ constexpr int kCand = 512;
 
 template <int kLanes, bool kOn>
 struct TopLds {
-  uint64_t keys[!kOn ? 1 : kLanes > kCand ? kLanes : kCand];   // at first the lanes' own
+  alignas(16) uint64_t keys[kOn ? kCand : 1];   // at first those of groups of lanes
   uint64_t best[(kLanes + 63) / 64];
   uint16_t who[kOn ? kLanes : 1];           // lanes that may hold some
   uint64_t bound;
@@ -214,6 +214,14 @@ __device__ inline void put_largest(uint64_t *keys, int n, int k, int lane, Put p
   if (above < k) put(above, mine);
 }
 
+// A key from another lane of the same four.
+template <int kPerm>
+__device__ inline uint64_t neighbour(uint64_t key) {
+  const int high = (int)(key >> 32), low = (int)key;
+  return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, high, kPerm, 0xf, 0xf, false) << 32 |
+         (uint32_t)__builtin_amdgcn_update_dpp(0, low, kPerm, 0xf, 0xf, false);
+}
+
 // The k largest keys of a part, put(r, key) for the r-th of them (0: there is none).  The sums' pass over
 // the row leaves each lane's largest logit and its chunk.  Such keys are of different columns, so the
 // k-th largest of the largest of some groups of lanes is a lower bound of the k-th largest of all,
@@ -226,41 +234,29 @@ template <typename T, int kLanes, typename Put>
 __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int most,
                               TopLds<kLanes, true> &lds, Put put) {
   constexpr int N = kCols<T>;
-  const uint64_t own = key_of(m, min(most + N, p.d) - 1);
-  if (kLanes > 64) {
-    lds.keys[lane] = own;
-    group_sync<kLanes>();
-  }
+  // groups of lanes with one key each, 256 or 64 of them: the more there are, the nearer the bound
+  constexpr int kGroups = kLanes < 256 ? kLanes : 256, R = kGroups / 64;
+  uint64_t key = key_of(m, min(most + N, p.d) - 1);
+  if (kLanes / kGroups > 1) key = larger(key, neighbour<0xb1>(key));     // lanes 1 apart
+  if (kLanes / kGroups > 2) key = larger(key, neighbour<0x4e>(key));     // 2 apart
+  if (kLanes > 64 && lane % (kLanes / kGroups) == 0) lds.keys[lane / (kLanes / kGroups)] = key;
+  if (lane == 0) lds.lanes = lds.count = 0;
+  group_sync<kLanes>();
   if (lane < 64) {
-    // groups of lanes with one key each: the more there are, the nearer the bound
-    constexpr int kWaves = kLanes / 64, R = kWaves < 4 ? kWaves : 4;
-    uint64_t key[kWaves], most_of[R];
+    uint64_t of[R], one = key;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      key[w] = kLanes > 64 ? lds.keys[w * 64 + lane] : own;
-      most_of[w % R] = w < R ? key[w] : larger(most_of[w % R], key[w]);
-    }
-    uint64_t one = most_of[0];
+    for (int i = 0; i < R; ++i) of[i] = kLanes > 64 ? lds.keys[R * lane + i] : key;
+    if (kLanes > 64) one = of[0];
 #pragma unroll
-    for (int i = 1; i < R; ++i) one = larger(one, most_of[i]);
-    const uint64_t bound = k <= 32 ? kth_of_wave(one, k) : kth_largest(most_of, k);
-    uint32_t lanes = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      // (a lane's largest logit may be in a lower column than its key says)
-      const bool may = (key[w] | 0xffffffffu) >= bound && key[w] != 0;
-      const uint64_t all = __ballot(may);
-      if (may) lds.who[lanes + __popcll(all & (((uint64_t)1 << lane) - 1))] = (uint16_t)(w * 64 + lane);
-      lanes += (uint32_t)__popcll(all);
-    }
-    if (lane == 0) {
-      lds.bound = bound;
-      lds.lanes = lanes;
-      lds.count = 0;
-    }
+    for (int i = 1; i < R; ++i) one = larger(one, of[i]);
+    const uint64_t bound = k <= 32 ? kth_of_wave(one, k) : kth_largest(of, k);
+    if (lane == 0) lds.bound = bound;
   }
   group_sync<kLanes>();
   const uint64_t bound = lds.bound;
+  // (a lane's largest logit may be in a lower column than its key says)
+  if (key_of(m, 0) >= bound) lds.who[atomicAdd(&lds.lanes, 1u)] = (uint16_t)lane;
+  group_sync<kLanes>();
   const uint32_t lanes = lds.lanes, deals = (uint32_t)(p.end - p.q0 + kLanes - 1) / kLanes;
   for (uint32_t i = lane; i < lanes * deals; i += kLanes) {
     const int q = p.q0 + (int)lds.who[i % lanes] + (int)(i / lanes) * kLanes;
