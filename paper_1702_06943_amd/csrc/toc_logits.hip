@@ -409,9 +409,11 @@ __global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t,
 
 template <typename T, int kWhat>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_t s) {
-  // Lanes and chunks at once by the length and the number of rows (us, 8,192 x 47,236 bf16 by 256 x 4,
-  // 512 x 6, 1,024 x 6: 139, 134, 146; 1,001 x 9,973 f16 by 256 x 4, 512 x 6, 1,024 x 6: 7.3, 8.3, 11.3; 18,750
-  // rows of 900 f16 by 64, 16 lanes 11.8, 9.8, 2,000 of them 3.8, 4.0)
+  // Lanes and chunks at once by the length and the number of rows (us: 8,192 x 47,236 bf16 by 256 x 4, 512 x 6,
+  // 1,024 x 6 139, 134, 146, one such row by 512 x 12, 1,024 x 6 7.7, 5.0; 8,000 x 4,001 by 64 x 4, 256 x 4 15.5, 17.8, 64
+  // of them 4.5, 3.6; 64 x 16,000 by 256 x 4, 512 x 6 4.7, 4.2, 3,000 of them 19.8, 20.9; 18,750 x 900 f16 by 16, 64 lanes
+  // 9.8, 11.8, 2,000 of them 4.0, 3.8).  More alternatives than 32 need more groups of lanes than 64 lanes have (18,750 x
+  // 900 f16, 64 of them, by 64 and 256 lanes 187, 108; 100 such rows 91, 12).
 #define TOC_SCORE(L, K)                                                                              \
   hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>), grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t)
   if constexpr ((kWhat & (kTop | kTeach)) == 0) {
@@ -420,9 +422,10 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_
       return launched("score_kernel");
     }
   }
-  if (a.chunks <= 256) TOC_SCORE(64, 4);
-  else if (a.chunks <= 2048) TOC_SCORE(256, 4);
-  else if (a.n >= 512) TOC_SCORE(512, 6);
+  const bool many = a.n >= 512;
+  if (a.chunks <= (a.n >= 2048 ? 768 : 256) && !((kWhat & kTop) && o.k > 32)) TOC_SCORE(64, 4);
+  else if (a.chunks <= (many ? 2048 : 1024)) TOC_SCORE(256, 4);
+  else if (many || a.chunks <= 2048) TOC_SCORE(512, 6);
   else TOC_SCORE(1024, 6);
 #undef TOC_SCORE
   return launched("score_kernel");

@@ -328,8 +328,9 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
                        dim3(kPartLanes), 0, s, a, o, t, g, split);
     return launched("part_grad_kernel");
   }
-  // The fewest lanes that hold a row, so that a CU has several rows in turns of reading and writing (us, bf16
-  // gradients): 40,000 x 1,800 by 64 x 8, 256 x 8 lanes and chunks 52, 102; 10,000 x 8,003 by 256 x 8, 1,024 x 2
+  // The fewest lanes that hold a row, so that a CU has several rows in turns of reading and writing, where there are
+  // that many (us, bf16 gradients): 64 x 4,000 by 64 x 8, 256 x 2 lanes and chunks 6.1, 4.3, 2,000 of them 8.5, 9.5; 64 x
+  // 16,000 by 256 x 8, 512 x 6 6.4, 5.8; 40,000 x 1,800 by 64 x 8, 256 x 8 52, 102; 10,000 x 8,003 by 256 x 8, 1,024 x 2
   // 52, 99; 8,000 x 16,384 by 512 x 6, 256 x 8 80, 86; but 8,192 x 47,236 by 1,024 x 6, 512 x 12, 256 x 24 270, 302,
   // 315, whose rows in flight are fewer at once; 2,000 x 65,536 by 512 x 20, 1,024 x 12 85, 95, and the other
   // way with binary32: 4,000 x 47,236 by 1,024 x 12, 512 x 24 291, 309.  Longer rows are read twice, by 1,024 x 6
@@ -343,8 +344,9 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
     }
   }
   if (fits(64, 2)) TOC_GRAD(64, 2);
-  else if (fits(64, 8)) TOC_GRAD(64, 8);
-  else if (fits(256, 8)) TOC_GRAD(256, 8);
+  else if (a.n >= 1024 && fits(64, 8)) TOC_GRAD(64, 8);
+  else if (fits(256, 2)) TOC_GRAD(256, 2);
+  else if (a.n >= 512 && fits(256, 8)) TOC_GRAD(256, 8);
   else if (fits(512, 6)) TOC_GRAD(512, 6);
   else if (fits(1024, 6)) TOC_GRAD(1024, 6);
   else if (sizeof(T) == 2 && fits(512, 20)) TOC_GRAD(512, 20);
