@@ -5,8 +5,8 @@
 // One pass: a lane keeps the sums of its chunks relative to its largest logit so far, lanes, waves and
 // parts are put together with the same step.
 //   score_kernel  bound by memory where rows are many: 8,192 x 47,236 bf16 131 us, 5.9 TB/s, with
-//                 entropy and distance from 64 saved logits alike; with 20 alternatives 157 us.  One row 5.6
-//                 us, with 5 alternatives 9.0: the look for them is a chain of some 3.5 us.  18,750 x 900
+//                 entropy and distance from 64 saved logits alike; with 20 alternatives 152 us.  One row 5.1
+//                 us, with 5 alternatives 7.9: the look for them is a chain of some 2.9 us.  18,750 x 900
 //                 f16 9.8 us, 3.5 TB/s, bound by a short row's own instructions.
 //   part_kernel, join_kernel  few long rows: one of 262,144 f32 5.2 us, 64 of bf16 10.4
 #include "toc_logits_dev.h"
