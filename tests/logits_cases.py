@@ -5,7 +5,7 @@ Tolerances, u = 2^-24, x = scale (z - max) of a column, E a mean under the row's
   two that much relatively and 2 u of its own.  Each time a lane, a wave or a row is measured from a
   new largest logit its sums move by such a power and a product, and these distances add up to |x| at
   most: in all 4 u |x| + 3 u a move.  A lane adds at most d / 64 columns one after the other, or
-  d / 256 of a row longer than 4,096, and at most 64 sums of lanes, waves and parts follow; it moves no more often.  So S is off by
+  d / 256 of a row longer than 6,144 (768 chunks of 8 are the most that a wave has alone), and at most 64 sums of lanes, waves and parts follow; it moves no more often.  So S is off by
   sum_error(), relatively, log S by that and its own rounding; a term of sum p x by its p's share and
   that of x; outputs are then rounded to their type (half a step, UNIT).  Powers below 2^-126 are 0.
 """
@@ -20,7 +20,7 @@ INTS = {32: torch.int32, 64: torch.int64}
 
 def steps(d):
     """Roundings that one sum of a row goes through, moves included (3 each)."""
-    lane = d / 64 if d <= 4096 else d / 256
+    lane = d / 64 if d <= 6144 else d / 256
     return 4 * (lane + 64)
 
 

@@ -71,7 +71,9 @@ def test_long_rows(n, d, kind):
     check(Z, Z64, ids, idt, t64, t, rng.standard_normal(n), 1.0, 1.0, None, kind, blank(n, d, kind))
 
 
-@pytest.mark.parametrize("n,d,kind", [(300, 140001, "bf16"), (1100, 8192, "f32"), (3000, 700, "f16")])
+@pytest.mark.parametrize("n,d,kind", [(300, 140001, "bf16"), (1100, 8192, "f32"), (3000, 700, "f16"),
+                                      (1000, 4003, "bf16"), (500, 9001, "f16"), (600, 9001, "bf16"), (1023, 1501, "f32"),
+                                      (2051, 6001, "bf16")])
 def test_many_rows(n, d, kind):
     """The first and the last of many rows are as they would be alone."""
     rng = np.random.default_rng(d)

@@ -65,6 +65,33 @@ def test_logprob_long_and_many(n, d):
         check(Z, Z64, ids, idt, 1.0, k, kind)
 
 
+@pytest.mark.parametrize("n,d,kind,k", [(2051, 5003, "bf16", 5), (2051, 6001, "f16", 0), (2050, 2003, "f32", 32),
+                                        (2050, 1501, "f16", 33), (600, 12007, "f16", 3), (400, 12007, "bf16", 64),
+                                        (300, 1003, "bf16", 64), (70, 13, "f32", 64), (5003, 900, "f16", 0),
+                                        (1500, 9000, "bf16", 20), (513, 17001, "bf16", 0)])
+def test_lanes_by_rows(n, d, kind, k):
+    """As many rows as are given, of which some are looked at."""
+    rng = np.random.default_rng(n * d)
+    Z = torch.randn((n, d), device=DEV, generator=torch.Generator(DEV).manual_seed(d)).mul_(3).to(TYPES[kind])
+    Z[1, ::2] = -INF
+    ids, idt = given(rng, n, d, 32)
+    logp, lse, h = (torch.full((n,), 7.0, device=DEV) for _ in range(3))
+    top = torch.full((n, k), 7, dtype=idt.dtype, device=DEV) if k else None
+    top_logp = torch.full((n, k), 7.0, device=DEV) if k else None
+    at = np.r_[:5, n // 2, n - 3:n]
+    Z64, scale = Z[at].double().cpu().numpy(), float(np.float32(0.8))
+    s, want = Soft(Z64, scale), L.logprob(Z64, ids[at], scale, k)
+    real = (ids[at] >= 0) & (ids[at] < d)
+    for entropy in (h, None):
+        T.toc_logprob(Z, idt, logp, lse, entropy, top, top_logp, scale, workspace(n, d, k))
+        finite(logp[at], want["logp"], s.logp_tol(np.where(real, ids[at], 0)[:, None])[:, 0], "logp")
+        finite(lse[at], want["lse"], s.lse_tol(), "lse")
+        close(h[at], want["entropy"], s.entropy_tol(), "entropy")
+        if k:
+            assert np.array_equal(top[at].cpu().numpy(), want["top_ids"])
+            finite(top_logp[at], want["top_logp"], s.logp_tol(want["top_ids"]), "top_logp")
+
+
 @pytest.mark.parametrize("low", [False, True], ids=["inf", "lowest"])
 @pytest.mark.parametrize("kind", sorted(TYPES))
 @pytest.mark.parametrize("d", [9, 700, 5000, 20011])
@@ -242,7 +269,8 @@ def test_grad(d, kind):
 
 
 @pytest.mark.parametrize("n,d,kind", [(1, 47236, "bf16"), (2, 70001, "f32"), (1, 262144, "bf16"), (3, 140001, "f16"),
-                                      (300, 140001, "bf16"), (1100, 8192, "f32")])
+                                      (300, 140001, "bf16"), (1100, 8192, "f32"), (1100, 4003, "bf16"), (1000, 4003, "bf16"),
+                                      (500, 9001, "f16"), (600, 9001, "bf16"), (1023, 1501, "f32"), (5003, 900, "f16")])
 def test_grad_long_and_many(n, d, kind):
     rng = np.random.default_rng(n + d)
     Z = torch.randn((n, d), device=DEV, generator=torch.Generator(DEV).manual_seed(d)).mul_(3).to(TYPES[kind])
