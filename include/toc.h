@@ -760,7 +760,7 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
  *   A row with a NaN or +infinity: what depends on its sum is NaN.
  * Sums are binary32; their order depends on n, d, `type`, on what is asked for and on where in 16
  * bytes a row begins: equal calls on the same memory give equal bits.
- * dZ may be Z; outputs overlap nothing else.
+ * dZ may be Z, with its row stride; outputs overlap nothing else.
  * Limits (TOC_EUNSUPPORTED): n below 2^31, d at most 2^28, 64 alternatives, 256 saved logits.
  * ------------------------------------------------------------------------- */
 

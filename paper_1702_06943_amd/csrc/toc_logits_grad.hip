@@ -378,6 +378,12 @@ toc_status grad(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale, c
   return launch<T, kTeach, false>(a, o, t, g, split, s);
 }
 
+// dZ in the place of Z has Z's rows.
+inline toc_status check_place(int64_t n, const void *Z, int64_t ldz, const void *dZ, int64_t lddz) {
+  if (n > 1 && dZ == Z && lddz != ldz) return fail(TOC_EINVAL, "dZ is Z, with another row stride");
+  return TOC_OK;
+}
+
 }  // namespace
 }  // namespace logits
 }  // namespace toc
@@ -395,7 +401,7 @@ toc_status toc_logprob_grad(int64_t n, int32_t d, int32_t type, const void *Z, i
   toc_status st = toc_logits_workspace_size(n, d, 0, &need);
   if (st || (st = check_logits(n, d, type, Z, ldz, scale)) ||
       (st = check_score(n, ids, id_bits, logp, lse, entropy)) ||
-      (st = check_rows("dZ", dZ, n, d, lddz, type_size(type))) ||
+      (st = check_rows("dZ", dZ, n, d, lddz, type_size(type))) || (st = check_place(n, Z, ldz, dZ, lddz)) ||
       (st = check_vec("dlogp", dlogp, n, false)) || (st = check_vec("dlse", dlse, n, false)) ||
       (st = check_vec("dentropy", dentropy, n, false)))
     return st;
@@ -424,7 +430,8 @@ toc_status toc_distill_grad(int64_t n, int32_t d, int32_t type, const void *Z, i
   if (st || (st = check_logits(n, d, type, Z, ldz, scale)) ||
       (st = check_teacher(n, type, k, top_ids, id_bits, ldi, t_type, top_z, ldt, top_scale, top_lse)) ||
       (st = check_vec("dloss", dloss, n, true)) || (st = check_vec("loss", loss, n, false)) ||
-      (st = check_rows("dZ", dZ, n, d, lddz, type_size(type))) || (st = check_ws(ws, ws_bytes, need)))
+      (st = check_rows("dZ", dZ, n, d, lddz, type_size(type))) || (st = check_place(n, Z, ldz, dZ, lddz)) ||
+      (st = check_ws(ws, ws_bytes, need)))
     return st;
   if (n == 0) return TOC_OK;
   const Score o{};

@@ -53,6 +53,7 @@ def test_shared_refusals(name, order):
         refused(dZ=None)
         refused(dZ=P + 1)
         refused(lddz=7)
+        refused(lddz=9)                            # Z itself, with other rows
     assert call(name, order, n=0, Z=None, ids=None, logp=None, top_ids=None, top_logp=None, top_z=None, loss=None,
                 dloss=None, dZ=None, dlogp=None, ws=None, ws_bytes=0) == 0        # nothing to do
 
