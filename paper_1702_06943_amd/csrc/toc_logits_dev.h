@@ -559,10 +559,11 @@ __device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
 // where rows are short or enough (us, whole and in parts: log probabilities of 1 x 262,144 f32 17.9,
 // 5.2, of 64 x 262,144 bf16 18.3, 10.3, of 16 x 47,236 bf16 6.1, 6.7, of 200 x 100,000 bf16 10.2,
 // 12.8; gradient of 1 x 100,000 bf16 13.3, 8.7, of 64 x 65,536 bf16 10.1, 11.5).  Alternatives are
-// looked for in each part, so parts are of 4,096 chunks then, and at most 256 come together.
+// looked for in each part, so parts are of 2,048 chunks then (9 x 88,832 f16 with 3, of 4,096 11.3, 2,048 9.5, 1,024
+// 9.5, whole 11.6; with 20 13.6, 12.7, 13.3, 12.9), and at most 256 come together.
 inline int parts_of(int64_t n, int64_t chunks, int k) {
   if (n >= 128 || chunks <= 8192) return 1;
-  const int64_t most = k ? std::min(chunks / 4096, (int64_t)256 / k) : chunks / 1024;
+  const int64_t most = k ? std::min(chunks / 2048, (int64_t)256 / k) : chunks / 1024;
   return (int)std::max<int64_t>(1, std::min({most, (int64_t)kMaxParts, kMaxPieces / n}));
 }
 inline Split split_of(int64_t n, int64_t chunks, int k, void *ws) {
