@@ -38,13 +38,13 @@ __device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const E
   a.top_logp[at] = key ? log_p(key_logit(key), e, scale) : kNone;
 }
 
-// Keys of columns that may be among a row's alternatives, at most.  (As many of equal logits are left:
-// 64 chunks' columns.)
-constexpr int kCand = 512;
+// Keys of columns that may be among a row's alternatives, at most.  Of a row of equal logits and fewer
+// larger ones than the k <= 64 alternatives up to 8 k + k - 1 = 575 are left: top_of().
+constexpr int kCand = 576;
 
 template <int kLanes, bool kOn>
 struct TopLds {
-  alignas(16) uint64_t keys[kOn ? kCand : 1];   // at first those of groups of lanes
+  alignas(16) uint64_t keys[!kOn ? 1 : kLanes > kCand ? kLanes : kCand];   // at first one of each lane
   uint64_t best[(kLanes + 63) / 64];
   uint16_t who[kOn ? kLanes : 1];           // lanes that may hold some
   uint64_t bound;
@@ -214,41 +214,37 @@ __device__ inline void put_largest(uint64_t *keys, int n, int k, int lane, Put p
   if (above < k) put(above, mine);
 }
 
-// A key from another lane of the same four.
-template <int kPerm>
-__device__ inline uint64_t neighbour(uint64_t key) {
-  const int high = (int)(key >> 32), low = (int)key;
-  return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, high, kPerm, 0xf, 0xf, false) << 32 |
-         (uint32_t)__builtin_amdgcn_update_dpp(0, low, kPerm, 0xf, 0xf, false);
-}
-
 // The k largest keys of a part, put(r, key) for the r-th of them (0: there is none).  The sums' pass over
 // the row leaves each lane's largest logit and its chunk.  Such keys are of different columns, so the
 // k-th largest of the largest of some groups of lanes is a lower bound of the k-th largest of all,
 // and lanes whose own largest logit is below it have none of those: the chunks of the other lanes,
 // some k, are dealt out to the group and read again, and the keys from the bound on, little more
 // than k, are left in LDS for the first wave.  (A lane's chunk stands for its last column: the key
-// is then at most the column's own.)  Where more than kCand are left, which takes most of the
+// is then at most the column's own.)  A group's lanes are 64 or 256 apart, so that neighbouring chunks
+// are of different groups: of equal logits, such as those of a mask of the type's lowest value, the
+// groups' keys are the row's first chunks, and no more than the first k chunks' columns and the larger
+// logits pass the bound.  (With groups of neighbouring lanes those of some 16 k chunks did: 64 x 47,236
+// bf16 with 20 alternatives, all columns but 15 masked, 162 us; now 19, as all lanes with the mask's
+// logit are read again, 9.4 without a mask.)  Where more than kCand are left, which takes most of the
 // largest logits in the columns of a few lanes, k searches follow.
 template <typename T, int kLanes, typename Put>
 __device__ inline void top_of(const Part<T> &p, int k, int lane, float m, int most,
                               TopLds<kLanes, true> &lds, Put put) {
   constexpr int N = kCols<T>;
   // groups of lanes with one key each, 256 or 64 of them: the more there are, the nearer the bound
-  constexpr int kGroups = kLanes < 256 ? kLanes : 256, R = kGroups / 64;
-  uint64_t key = key_of(m, min(most + N, p.d) - 1);
-  if (kLanes / kGroups > 1) key = larger(key, neighbour<0xb1>(key));     // lanes 1 apart
-  if (kLanes / kGroups > 2) key = larger(key, neighbour<0x4e>(key));     // 2 apart
-  if (kLanes > 64 && lane % (kLanes / kGroups) == 0) lds.keys[lane / (kLanes / kGroups)] = key;
+  constexpr int R = (kLanes < 256 ? kLanes : 256) / 64;
+  const uint64_t key = key_of(m, min(most + N, p.d) - 1);
+  if (kLanes > 64) lds.keys[lane] = key;
   if (lane == 0) lds.lanes = lds.count = 0;
   group_sync<kLanes>();
   if (lane < 64) {
     uint64_t of[R], one = key;
 #pragma unroll
-    for (int i = 0; i < R; ++i) of[i] = kLanes > 64 ? lds.keys[R * lane + i] : key;
-    if (kLanes > 64) one = of[0];
+    for (int i = 0; i < R; ++i) of[i] = kLanes > 64 ? lds.keys[64 * i + lane] : key;
 #pragma unroll
-    for (int i = 1; i < R; ++i) one = larger(one, of[i]);
+    for (int i = R; i < kLanes / 64; ++i) of[i % R] = larger(of[i % R], lds.keys[64 * i + lane]);
+#pragma unroll
+    for (int i = 0; i < R; ++i) one = larger(one, of[i]);
     const uint64_t bound = k <= 32 ? kth_of_wave(one, k) : kth_largest(of, k);
     if (lane == 0) lds.bound = bound;
   }
