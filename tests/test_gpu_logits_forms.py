@@ -8,7 +8,7 @@ import pytest
 
 import paper_1702_06943_amd as T
 import test_gpu_distill
-from logits_cases import DEV, TYPES, L, Soft, close, grad_tol, given, host, taught_tol, torch, vec, workspace
+from logits_cases import DEV, TYPES, L, Soft, close, gaps_untouched, grad_tol, given, host, taught_tol, torch, vec, workspace
 
 pytestmark = pytest.mark.gpu
 FORMS = [
@@ -112,3 +112,31 @@ def test_teacher_gradient(n, d, kind, k):
     got, far = host(loss)[at], np.isinf(want)
     assert np.array_equal(got[far], want[far])
     close(np.where(far, 0, got), np.where(far, 0, want), tol, "loss")
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("d", [1, 7, 9, 127, 129, 300, 568, 569, 900, 1001, 1135, 1136, 1152])
+def test_short_rows_in_place(d, kind):
+    """So many short rows that 16 lanes have one (64 from 569 binary32 or 1,137 16-bit columns on): the same bits
+    in the logits' own place, with the numbers beside them and without."""
+    rng = np.random.default_rng(d)
+    n, scale = 4096 + 5, 0.9
+    buf = torch.full((n * (d + 3) + 1,), 7.0, device=DEV).to(TYPES[kind])
+    Z = buf[1:].view(n, d + 3)[:, :d]
+    Z.copy_(torch.from_numpy(rng.standard_normal((n, d)) * 3))
+    Z[5], Z[n - 1, ::2] = -float("inf"), -float("inf")
+    ids, idt = given(rng, n, d, 32)
+    g = [vec(x) for x in rng.standard_normal((3, n))]
+    for x in g:
+        x[7] = 0
+    dZ = torch.full((n, d), 7.0, device=DEV).to(TYPES[kind])
+    out, beside = ([torch.full((n,), 7.0, device=DEV) for _ in range(3)] for _ in range(2))
+    T.toc_logprob_grad(Z, dZ, idt, *g, *out, scale, workspace(n, d))
+    again = buf.clone()[1:].view(n, d + 3)[:, :d]
+    T.toc_logprob_grad(again, again, idt, *g, *beside, scale, workspace(n, d))
+    T.toc_logprob_grad(Z, Z, idt, *g, scale=scale, ws=workspace(n, d))
+    for x in (again, Z):
+        assert torch.equal(x, dZ) and gaps_untouched(x)
+    for a, b in zip(out, beside):
+        assert torch.equal(a, b)
+    assert not dZ[5].any() and not dZ[7].any()
