@@ -752,7 +752,9 @@ toc_status toc_rmsnorm_grad(int64_t n, int32_t d, int32_t type, const void *H, i
  * temperature, positive), row by row
  *   p_j = exp(s z_j) / sum_i exp(s z_i)
  * formed from the differences to the row's largest logit, so that s z itself is never
- * formed.  A column at minus infinity is masked: its p is 0.  The conventions are those of
+ * formed.  (A column 3.4e38, the largest binary32 number, or more below that has p = 0, as it has
+ * by the formula too from a scale of 2^-120 on; its log p is the formula's at any scale.)  A column
+ * at minus infinity is masked: its p is 0.  The conventions are those of
  * the rows above; vectors of n are contiguous binary32, token numbers id_bits (32 or 64)
  * signed bits, and one outside 0 .. d-1 (say -1, to pad) is no token.
  *   A row of nothing but minus infinity: p = 0, log p and lse minus infinity, entropy 0, its

@@ -31,7 +31,7 @@ __device__ inline float key_logit(uint64_t key) {
 }
 __device__ inline int key_column(uint64_t key) { return (int)~(uint32_t)key; }
 
-__device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const End &e, float scale) {
+__device__ inline void put_top(const Score &a, int64_t at, uint64_t key, const End &e, const Scale &scale) {
   const int column = key ? key_column(key) : -1;
   if (a.ids.bits == 32) ((int32_t *)a.top_ids)[at] = column;
   else ((int64_t *)a.top_ids)[at] = column;
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 16 ? 6 : 8) void score_
     b.load(z, skew, b.next, p.end, a.d, lane);
     add_batch<kT>(b, a.c, s, most);
   }
-  if ((kWhat & kTeach) && first) x.compare();
+  if ((kWhat & kTeach) && first) x.compare(a.scale);
   const float m = s.m;
   const End e = end_of(group_sums<kLanes, kT>(s, a.c, sums_lds[group]));
   if (first) {
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t,
     x.read(t, Taught::ask(t, row, lane), a.d);
     x.gather(t, z);
     x.learn(t, row);
-    x.compare();
+    x.compare(a.scale);
   }
   if (kWhat & kTop)
     for (int i = lane; i < s.parts * o.k; i += 64) keys[i] = s.keys[row * s.parts * o.k + i];

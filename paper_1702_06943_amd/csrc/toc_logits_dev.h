@@ -305,6 +305,17 @@ __device__ inline int lane_of() {
 
 // --- a row's end -----------------------------------------------------------------
 
+// The scale of the logits.  Two logits' difference, up to twice the largest number, may overflow where
+// scale times it does not: below 1 a quarter of it is formed (a sum of shares that rounds to more than 1
+// times a half would overflow too) and multiplied by four times the scale, both exact.
+struct Scale {
+  float whole, part, by;   // whole = part by
+  __device__ inline float apart(float z, float from) const { return fmaf(part, z, -part * from); }
+};
+inline Scale scale_of(float scale) {
+  return scale < 1.0f ? Scale{scale, 0.25f, 4.0f * scale} : Scale{scale, 1.0f, scale};
+}
+
 // What follows from a whole row's sums.
 struct End {
   float m, log_s, t_s;   // the largest logit, log s, ln 2 t / s
@@ -318,12 +329,12 @@ __device__ inline End end_of(Sums a) {
   e.t_s = e.empty ? 0.0f : kLn2 * a.t / a.s;
   return e;
 }
-__device__ inline float log_p(float z, const End &e, float scale) {
-  return e.empty ? kNone : fmaf(scale, z - e.m, -e.log_s);
+__device__ inline float log_p(float z, const End &e, const Scale &scale) {
+  return e.empty ? kNone : fmaf(scale.by, scale.apart(z, e.m), -e.log_s);
 }
 __device__ inline float entropy(const End &e) { return e.empty ? 0.0f : e.log_s - e.t_s; }
-__device__ inline float log_sum(const End &e, float scale) {
-  return e.empty ? kNone : fmaf(scale, e.m, e.log_s);
+__device__ inline float log_sum(const End &e, const Scale &scale) {
+  return e.empty ? kNone : fmaf(scale.whole, e.m, e.log_s);
 }
 
 struct Ids {
@@ -372,12 +383,13 @@ struct Rows {
   int d;
   const T *Z;
   int64_t ldz;
-  float scale, c;      // c = scale log2(e)
+  Scale scale;
+  float c;             // scale log2(e)
   int chunks;          // of a row that is not skewed
 };
 template <typename T>
 Rows<T> rows_of(int64_t n, int32_t d, const void *Z, int64_t ldz, float scale) {
-  return Rows<T>{(uint32_t)n, d, (const T *)Z, ldz, scale, scale * kLog2e, (int)chunks_of<T>(d)};
+  return Rows<T>{(uint32_t)n, d, (const T *)Z, ldz, scale_of(scale), scale * kLog2e, (int)chunks_of<T>(d)};
 }
 
 // Log probabilities: what is asked for, each but ids may be NULL.
@@ -402,7 +414,7 @@ struct Teacher {
 };
 
 // The numbers of a row's score, by one lane.  z: the given token's logit, if there is one.
-__device__ inline void score_row(const Score &a, int64_t row, int id, float z, const End &e, float scale) {
+__device__ inline void score_row(const Score &a, int64_t row, int id, float z, const End &e, const Scale &scale) {
   if (a.logp) a.logp[row] = id < 0 ? 0.0f : log_p(z, e, scale);
   if (a.lse) a.lse[row] = log_sum(e, scale);
   if (a.entropy) a.entropy[row] = entropy(e);
@@ -412,7 +424,7 @@ __device__ inline void score_row(const Score &a, int64_t row, int id, float z, c
 // are lane, lane + 64 and so on.  The loss is
 //   sum q log q - sum q log p = sum q log q - scale (sum q (z - r) + (r - m) sum q) + log S sum q
 // with r the largest logit of the row at an entry's column: what the entries give is known before the
-// row's own sums are.
+// row's own sums are.  Both differences are Scale's.
 struct Taught {
   static constexpr int kPer = kMaxTeacher / 64;
   int id[kPer];        // -1: none
@@ -420,7 +432,7 @@ struct Taught {
   float z[kPer];       // the row's own logit there
   float q[kPer];
   float sum, sum_log;  // of q and of q log q over the row
-  float r, sum_z;      // r, and the sum of q (z - r)
+  float r, sum_z;      // r, and the sum of q (z - r), a part of it
 
   // The columns and the saved logits as they lie in memory.
   struct Raw {
@@ -501,7 +513,7 @@ struct Taught {
     sum_log = wave_sum(sum_log);
   }
   // An entry with q = 0 adds nothing.  (Where entries of a column were put together, the same.)
-  __device__ inline void compare() {
+  __device__ inline void compare(const Scale &scale) {
     r = kNone;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
@@ -510,13 +522,13 @@ struct Taught {
     sum_z = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (q[i] != 0.0f) sum_z = fmaf(q[i], z[i] - r, sum_z);
+      if (q[i] != 0.0f) sum_z = fmaf(q[i], scale.apart(z[i], r), sum_z);
     sum_z = wave_sum(sum_z);
   }
-  __device__ inline float loss(const End &e, float scale) const {
+  __device__ inline float loss(const End &e, const Scale &scale) const {
     if (sum == 0.0f) return 0.0f;
     if (e.empty) return INFINITY;
-    return sum_log - scale * fmaf(r - e.m, sum, sum_z) + e.log_s * sum;
+    return sum_log - scale.by * fmaf(scale.apart(r, e.m), sum, sum_z) + e.log_s * sum;
   }
 };
 

@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   }
   // (behind the next barrier dZ, which may be Z, is written: all of Z that is not read again has to be there)
   if (kTeach) {
-    if (first) x.compare();
+    if (first) x.compare(a.scale);
   } else {
     asm volatile("" ::"v"(zt));
   }
@@ -244,12 +244,12 @@ __global__ __launch_bounds__(kThreads<kLanes>, kLanes == 1024 && kPer <= 6 ? 8 :
   } else if (lane == 0) {
     score_row(o, row, id, zt, e, a.scale);
   }
-  const Slope k = slope_of<kTeach>(a.scale, s, e, gl, gs, ge);
+  const Slope k = slope_of<kTeach>(a.scale.whole, s, e, gl, gs, ge);
   if (k.none) {
     put_zeros<T>(dz, skew, lane, chunks, kLanes, a.d);
     return;
   }
-  const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
+  const float base = from(e.m), hit = kTeach ? -a.scale.whole * gl : a.scale.whole * gl;
   // the last batch is still there; the others from the last on, the likelier to be in a cache
   for (;;) {
     put_batch<kEntropy>(b, a.c, base, k, id, hit, marks, dz, a.d, g.stream);
@@ -299,12 +299,12 @@ __global__ __launch_bounds__(kPartLanes) void part_grad_kernel(Rows<T> a, Score 
   const End e = end_of(s);
   __syncthreads();
   if constexpr (kTeach) gs = gl == 0.0f ? 0.0f : gl * marks.sum;
-  const Slope k = slope_of<kTeach>(a.scale, s, e, gl, gs, ge);
+  const Slope k = slope_of<kTeach>(a.scale.whole, s, e, gl, gs, ge);
   if (k.none) {
     put_zeros<T>(dz, skew, p.q0 + lane, p.end, kLanes, a.d);
     return;
   }
-  const float base = from(e.m), hit = kTeach ? -a.scale * gl : a.scale * gl;
+  const float base = from(e.m), hit = kTeach ? -a.scale.whole * gl : a.scale.whole * gl;
   Batch<T, kLanes, kPartPer> b;
   for (int q = p.q0; q < p.end; q = b.next) {
     if constexpr (kTeach) {
