@@ -6,7 +6,7 @@
 // parts are put together with the same step.
 //   score_kernel  bound by memory where rows are many: 8,192 x 47,236 bf16 131 us, 5.9 TB/s, with
 //                 entropy and distance from 64 saved logits alike; with 20 alternatives 152 us.  One row 5.1
-//                 us, with 5 alternatives 7.9: the look for them is a chain of some 2.9 us.  18,750 x 900
+//                 us, with 5 alternatives 8.0: the look for them takes some 2.9 us.  18,750 x 900
 //                 f16 9.8 us, 3.5 TB/s, bound by a short row's own instructions.
 //   part_kernel, join_kernel  few long rows: one of 262,144 f32 5.2 us, 64 of bf16 10.4
 #include "toc_logits_dev.h"
@@ -405,11 +405,19 @@ __global__ __launch_bounds__(64) void join_kernel(Rows<T> a, Score o, Teacher t,
 
 template <typename T, int kWhat>
 toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, hipStream_t s) {
-  // Lanes and chunks at once by the length and the number of rows (us: 8,192 x 47,236 bf16 by 256 x 4, 512 x 6,
-  // 1,024 x 6 139, 134, 146, one such row by 512 x 12, 1,024 x 6 7.7, 5.0; 8,000 x 4,001 by 64 x 4, 256 x 4 15.5, 17.8, 64
-  // of them 4.5, 3.6; 64 x 16,000 by 256 x 4, 512 x 6 4.7, 4.2, 3,000 of them 19.8, 20.9; 18,750 x 900 f16 by 16, 64 lanes
-  // 9.8, 11.8, 2,000 of them 4.0, 3.8).  More alternatives than 32 need more groups of lanes than 64 lanes have (18,750 x
-  // 900 f16, 64 of them, by 64 and 256 lanes 187, 108; 100 such rows 91, 12).
+  // Lanes of a row and chunks of a lane at once, by the length and the number of rows (log probabilities of
+  // bf16 but for the last two, us):
+  //    8,192 x 47,236   256 x 4: 139    512 x 6: 134    1,024 x 6: 146
+  //        1 x 47,236   512 x 12: 7.7   1,024 x 6: 5.0
+  //    3,000 x 16,000   256 x 4: 19.8   512 x 6: 20.9
+  //       64 x 16,000   256 x 4: 4.7    512 x 6: 4.2
+  //    8,000 x 4,001    64 x 4: 15.5    256 x 4: 17.8
+  //       64 x 4,001    64 x 4: 4.5     256 x 4: 3.6
+  //   18,750 x 900 f16  16 x 8: 9.8     64 x 4: 11.8
+  //    2,000 x 900 f16  16 x 8: 4.0     64 x 4: 3.8
+  // More alternatives than 32 need more groups of lanes than 64 lanes have (f16 with 64 of them, us):
+  //   18,750 x 900      64 x 4: 187     256 x 4: 108
+  //      100 x 900      64 x 4: 91      256 x 4: 12
 #define TOC_SCORE(L, K)                                                                              \
   hipLaunchKernelGGL((score_kernel<T, L, K, kWhat>), grid_of<L>(a.n), dim3(kThreads<L>), 0, s, a, o, t)
   if constexpr ((kWhat & (kTop | kTeach)) == 0) {

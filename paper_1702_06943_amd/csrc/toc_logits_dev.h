@@ -568,11 +568,19 @@ __device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
 }
 
 // The split of n rows of `chunks` chunks, k alternatives, into parts of 1,024 chunks or more; 1
-// where rows are short or enough (us, whole and in parts: log probabilities of 1 x 262,144 f32 17.9,
-// 5.2, of 64 x 262,144 bf16 18.3, 10.3, of 16 x 47,236 bf16 6.1, 6.7, of 200 x 100,000 bf16 10.2,
-// 12.8; gradient of 1 x 100,000 bf16 13.3, 8.7, of 64 x 65,536 bf16 10.1, 11.5).  Alternatives are
-// looked for in each part, so parts are of 2,048 chunks then (9 x 88,832 f16 with 3, of 4,096 11.3, 2,048 9.5, 1,024
-// 9.5, whole 11.6; with 20 13.6, 12.7, 13.3, 12.9), and at most 256 come together.
+// where rows are short or enough (us):
+//   log p     1 x 262,144 f32     whole 17.9   in parts 5.2
+//            64 x 262,144 bf16    whole 18.3   in parts 10.3
+//            16 x 47,236 bf16     whole 6.1    in parts 6.7
+//           200 x 100,000 bf16    whole 10.2   in parts 12.8
+//   gradient  1 x 100,000 bf16    whole 13.3   in parts 8.7
+//            64 x 65,536 bf16     whole 10.1   in parts 11.5
+// The limit of 128 rows goes by the last of log p.  On either side of it, 127 rows in parts and 128 whole:
+// log p of 262,144 bf16 18.6, 20.2, of 1,048,576 50, 65; gradient 37.7, 39.7, 131, 146: longer rows than
+// some 300,000 columns would gain from parts beyond it too.
+// Alternatives are looked for in each part, so parts are of 2,048 chunks then, and at most 256 keys come
+// together (9 x 88,832 f16, parts of 1,024, 2,048 and 4,096 chunks and whole: 3 alternatives 9.5, 9.5,
+// 11.3, 11.6; 20 alternatives 13.3, 12.7, 13.6, 12.9).
 inline int parts_of(int64_t n, int64_t chunks, int k) {
   if (n >= 128 || chunks <= 8192) return 1;
   const int64_t most = k ? std::min(chunks / 2048, (int64_t)256 / k) : chunks / 1024;

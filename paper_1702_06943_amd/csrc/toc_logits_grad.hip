@@ -328,14 +328,23 @@ toc_status launch(const Rows<T> &a, const Score &o, const Teacher &t, const Grad
                        dim3(kPartLanes), 0, s, a, o, t, g, split);
     return launched("part_grad_kernel");
   }
-  // The fewest lanes that hold a row, so that a CU has several rows in turns of reading and writing, where there are
-  // that many (us, bf16 gradients): 64 x 4,000 by 64 x 8, 256 x 2 lanes and chunks 6.1, 4.3, 2,000 of them 8.5, 9.5; 64 x
-  // 16,000 by 256 x 8, 512 x 6 6.4, 5.8; 40,000 x 1,800 by 64 x 8, 256 x 8 52, 102; 10,000 x 8,003 by 256 x 8, 1,024 x 2
-  // 52, 99; 8,000 x 16,384 by 512 x 6, 256 x 8 80, 86; but 8,192 x 47,236 by 1,024 x 6, 512 x 12, 256 x 24 270, 302,
-  // 315, whose rows in flight are fewer at once; 2,000 x 65,536 by 512 x 20, 1,024 x 12 85, 95, and the other
-  // way with binary32: 4,000 x 47,236 by 1,024 x 12, 512 x 24 291, 309.  Longer rows are read twice, by 1,024 x 6
-  // rather than 1,024 x 16, which holds more of them but has a row a CU (512 x 200,003 84, 89).  Many
-  // short rows: 18,750 x 900 f16 by 16, 64 lanes 16.8, 18.9, of 100 bf16 6.1, 13.1; 2,000 of 900 6.4, 5.3.
+  // Lanes of a row and chunks of a lane: the fewest lanes that hold a row, so that a CU has several rows in turns
+  // of reading and writing, where there are that many rows (gradients of log p, bf16 unless said, us):
+  //   18,750 x 100         16 x 8: 6.1      64 x 2: 13.1
+  //   18,750 x 900 f16     16 x 8: 16.8     64 x 2: 18.9
+  //    2,000 x 900 f16     16 x 8: 6.4      64 x 2: 5.3
+  //   40,000 x 1,800       64 x 8: 52       256 x 8: 102
+  //    2,000 x 4,000       64 x 8: 8.5      256 x 2: 9.5
+  //       64 x 4,000       64 x 8: 6.1      256 x 2: 4.3
+  //   10,000 x 8,003       256 x 8: 52      1,024 x 2: 99
+  //       64 x 16,000      256 x 8: 6.4     512 x 6: 5.8
+  //    8,000 x 16,384      256 x 8: 86      512 x 6: 80
+  // but by 1,024 x 6 where fewer lanes would have fewer rows in flight, and by 512 x 20 of 16 bits only:
+  //    8,192 x 47,236      256 x 24: 315    512 x 12: 302     1,024 x 6: 270
+  //    2,000 x 65,536      512 x 20: 85     1,024 x 12: 95
+  //    4,000 x 47,236 f32  512 x 24: 309    1,024 x 12: 291
+  // Longer rows are read twice, by 1,024 x 6 rather than 1,024 x 16, which holds more of a row but has one a CU:
+  //      512 x 200,003     1,024 x 6: 84    1,024 x 16: 89
   const auto fits = [&](int lanes, int per) { return a.chunks + 1 < lanes * (per + 1); };
   if constexpr (!kTeach) {
     if (a.n >= kShortRows && fits(16, 8)) {
