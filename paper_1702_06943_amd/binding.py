@@ -703,10 +703,25 @@ def _row_opt(t, name, n, d, dev, kind):
     return (None, d) if t is None else _row_mat(t, name, n, d, dev, (kind,))[:2]
 
 
+# The most columns, and the largest number of anything, that the calls' 32-bit arguments hold:
+# ctypes cuts a larger one to its low bits.
+_ROW_MOST = (1 << 31) - 1
+
+
 def _row_shape(t, name):
     if t.dim() != 2:
         raise TocError(TOC_EINVAL, f"{name} must be a matrix")
+    if t.shape[1] > _ROW_MOST:
+        raise TocError(TOC_EUNSUPPORTED, f"{name} has {t.shape[1]} columns")
     return t.shape
+
+
+def _row_sizes(*sizes):
+    """The sizes as numbers that the calls' arguments hold."""
+    for s in sizes:
+        if not 0 <= s <= _ROW_MOST:
+            raise TocError(TOC_EINVAL if s < 0 else TOC_EUNSUPPORTED, f"a size of {s}")
+    return [int(s) for s in sizes]
 
 
 def _row_vec(t, name, n, dev):
@@ -762,7 +777,7 @@ def toc_embed(ids, E, out, scale=1.0, drop=None, stream=None):
 
 def toc_embed_grad_workspace_size(n, n_vocab, d):
     b = C.c_size_t()
-    _check(lib().toc_embed_grad_workspace_size(int(n), int(n_vocab), int(d), C.byref(b)))
+    _check(lib().toc_embed_grad_workspace_size(*_row_sizes(n, n_vocab, d), C.byref(b)))
     return b.value
 
 
@@ -806,7 +821,7 @@ def toc_rmsnorm(X, Y, R=None, H=None, w=None, eps=1e-5, drop=None, y_scale=None,
 
 def toc_rmsnorm_grad_workspace_size(n, d):
     b = C.c_size_t()
-    _check(lib().toc_rmsnorm_grad_workspace_size(int(n), int(d), C.byref(b)))
+    _check(lib().toc_rmsnorm_grad_workspace_size(*_row_sizes(n, d), C.byref(b)))
     return b.value
 
 
@@ -835,7 +850,7 @@ def toc_rmsnorm_grad(H, dY, dH, ws, w=None, eps=1e-5, dR=None, dX=None, dw=None,
 def toc_logits_workspace_size(n, d, k=0):
     """For the four calls below; k: toc_logprob's alternatives."""
     b = C.c_size_t()
-    _check(lib().toc_logits_workspace_size(int(n), int(d), int(k), C.byref(b)))
+    _check(lib().toc_logits_workspace_size(*_row_sizes(n, d, k), C.byref(b)))
     return b.value
 
 
