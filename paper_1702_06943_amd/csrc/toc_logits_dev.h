@@ -306,14 +306,16 @@ __device__ inline int lane_of() {
 // --- a row's end -----------------------------------------------------------------
 
 // The scale of the logits.  Two logits' difference, up to twice the largest number, may overflow where
-// scale times it does not: below 1 a quarter of it is formed (a sum of shares that rounds to more than 1
-// times a half would overflow too) and multiplied by four times the scale, both exact.
+// scale times it, or times a small share of it, does not: a quarter of it is formed (a sum of shares that rounds to
+// more than 1 times a half would overflow too) and multiplied by four times the scale, both exact.
+// (From a scale of 2^100 on, four times which may overflow, the whole: a share below 2^-100 would be
+// needed there.)
 struct Scale {
   float whole, part, by;   // whole = part by
   __device__ inline float apart(float z, float from) const { return fmaf(part, z, -part * from); }
 };
 inline Scale scale_of(float scale) {
-  return scale < 1.0f ? Scale{scale, 0.25f, 4.0f * scale} : Scale{scale, 1.0f, scale};
+  return scale < 0x1p100f ? Scale{scale, 0.25f, 4.0f * scale} : Scale{scale, 1.0f, scale};
 }
 
 // What follows from a whole row's sums.
@@ -576,8 +578,8 @@ __device__ inline Sums parts_sums(const Split &s, int64_t row, float c) {
 //   gradient  1 x 100,000 bf16    whole 13.3   in parts 8.7
 //            64 x 65,536 bf16     whole 10.1   in parts 11.5
 // The limit of 128 rows goes by the last of log p.  On either side of it, 127 rows in parts and 128 whole:
-// log p of 262,144 bf16 18.6, 20.2, of 1,048,576 50, 65; gradient 37.7, 39.7, 131, 146: longer rows than
-// some 300,000 columns would gain from parts beyond it too.
+// log p of 262,144 bf16 18.6, 20.2, of 1,048,576 50, 65; gradient 37.7, 39.7, 131, 146: rows as
+// long as these would gain from parts beyond it too.
 // Alternatives are looked for in each part, so parts are of 2,048 chunks then, and at most 256 keys come
 // together (9 x 88,832 f16, parts of 1,024, 2,048 and 4,096 chunks and whole: 3 alternatives 9.5, 9.5,
 // 11.3, 11.6; 20 alternatives 13.3, 12.7, 13.6, 12.9).

@@ -53,3 +53,27 @@ def test_far(n, d, kind, scale):
             # largest number or one step more, which is infinity
             past = np.isinf(got) & (away + tol > np.finfo(np.float32).max)
             close(np.where(past, away, got), away, tol, "loss")
+
+
+@pytest.mark.parametrize("scale", [0.7, 1.0, 2.5, 1e6])
+@pytest.mark.parametrize("n,d,kind", [(5, 9, "f32"), (5, 700, "bf16"), (300, 9001, "f32"), (2, 140001, "bf16")])
+def test_far_entries_of_little_weight(n, d, kind, scale):
+    """The share of an entry that far off is so small that its part of the distance is a number again."""
+    rng = np.random.default_rng(d)
+    big = torch.finfo(TYPES[kind]).max
+    Z = torch.full((n, d), -big, device=DEV).to(TYPES[kind])
+    Z[:, d // 2] = big
+    Z64, scale = Z.double().cpu().numpy(), float(np.float32(scale))
+    s = Soft(Z64, scale)
+    ids = np.tile([d // 2, 0, 3], (n, 1))
+    t = np.tile([0.0, -40.0, -20.0], (n, 1)) + rng.random((n, 3))
+    t = t.astype(np.float32)
+    loss, beside, dZ = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV), torch.empty_like(Z)
+    idt, one = torch.from_numpy(ids).to(DEV), vec(np.ones(n))
+    T.toc_distill(Z, idt, vec(t), loss, scale, ws=workspace(n, d))
+    T.toc_distill_grad(Z, dZ, idt, vec(t), one, beside, scale, ws=workspace(n, d))
+    want = L.distill(Z64, ids, t.astype(np.float64), scale)
+    assert (want < 1e37).all() and (want > 1e20).all()
+    tol, _ = taught_tol(s, ids, t.astype(np.float64), 1.0, None)
+    for got in (loss, beside):
+        close(got, want, tol, "loss")
